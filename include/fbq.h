@@ -61,6 +61,12 @@ typedef enum {
     FBQ_KERNEL_PREFILL = 2    /* tcgen05 / TMEM tensor-core kernel, one launch (named from M = 9, or 5 outside the streaming kernels' domain) */
 } fbq_kernel;
 
+/* The gate of a gated layer. */
+typedef enum {
+    FBQ_GATE_SILU = 0,        /* f(v) = v / (1 + e^-v) */
+    FBQ_GATE_GELU = 1         /* f(v) = v / 2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) */
+} fbq_gate;
+
 /* Number of uint32 words of a packed N x K code matrix: N*K/8 (4 bits) or
  * 3*N*K/32 (3 bits).  Returns 0 for unsupported arguments (bits not 3/4, K not
  * a multiple of 8 resp. 32). */
@@ -259,6 +265,61 @@ int fbq_linear_batch(const fbq_problem *problems, int count, int M, int group, i
  * before reading it).  The end-to-end path of the benchmark. */
 int fbq_linear_batch_hostio(const fbq_problem *problems, int count, int M, int group, int bits, int rank,
                             int act_is_bf16, void *stream);
+
+/* ---- The feed-forward block of a decoder layer, and what training its sub-branches needs ----
+ *
+ * A gated layer is an FBQuant layer of N = 2 F rows (a multiple of 16) that holds the gate's and the up projection's F rows: eight of
+ * the gate, eight of the up projection, and so on.  Its rank is twice the branches': A holds the gate's rows, then those of the
+ * up projection; a row of B holds its own branch's values in that branch's half and zeros in the other.  With the layer's products
+ *     p = x . dequant(Q, s, z)^T + (x . A^T) . B^T
+ * the block's hidden activations are
+ *     h[m][8 i + j] = f(p[m][16 i + j]) * p[m][16 i + 8 + j],      j = 0 .. 7,   f = SiLU or GELU (fbq_gate)
+ * fbq_gated_layer lays two projections of [F][K] and one rank (of each branch) out so: a step at load time.  It is an ordinary layer to
+ * fbq_linear, fbq_dequant and fbq_linear_backward as well.  qweight, scales, zeros: [2F] rows; A [2 rank][K]; B [2F][2 rank].
+ * Domain of the gated calls: group 128, N and (the layer's) rank multiples of 16, rank <= 256; anything else FBQ_ERR_UNSUPPORTED.
+ * Every pointer is 16-byte aligned. */
+int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void *gate_zeros, const void *gate_A, const void *gate_B,
+                    const uint32_t *up_q, const void *up_scales, const void *up_zeros, const void *up_A, const void *up_B, uint32_t *qweight,
+                    void *scales, void *zeros, void *A, void *B, int F, int K, int group, int bits, int rank, void *stream);
+
+/* h [M][N/2] of a gated layer, in one launch: p is gated in single precision where its sums are and rounded to the activation
+ * type never (h is, once).  x, A, B, h: fp16 or bf16 (act_is_bf16).  At most 2 tokens run on the streaming kernel, 3 to 16 on the split
+ * kernel (layer rank up to 128, and where fbq_split_plan has a plan for N rows), the rest on the prompts' kernels; each computes p as it
+ * does for fbq_linear.  "gemv" = 0 and "force_kernel" >= 0 leave all of it to the prompts' kernels.
+ *   kept, kept_scales   NULL, or what the backward pass needs of p in 8 bits: codes [M][N] and one scale per 128 columns of a row,
+ *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M run on the prompts' dense kernel
+ *       (scratch: a 16-bit copy of the weights, up to 512 MB per stream). */
+int fbq_gated(const void *x, const uint32_t *qweight, const void *scales, const void *zeros, const void *A, const void *B, void *h,
+              int8_t *kept, float *kept_scales, int M, int N, int K, int group, int bits, int rank, int gate, int act_is_bf16, void *stream);
+
+/* Activations in 8 bits.  x [M][K], fp16 or bf16; codes [M][K]; scales fp32 [M][ceil(K/128)], one per 128 consecutive columns of a row:
+ *     scale = max|x| / 127,   code = rint(x * (127 / max|x|)),   x stands for code * scale
+ * each step one IEEE operation in single precision, ties to even.  Groups whose largest |x| is below 2^-100 are kept as zeros, groups that
+ * hold an Inf or a NaN as NaN (scale NaN, codes 0).  Any K.  fbq_act8_unpack rounds code * scale once. */
+int fbq_act8_pack(const void *x, int8_t *codes, float *scales, int M, int K, int act_is_bf16, void *stream);
+int fbq_act8_unpack(const int8_t *codes, const float *scales, void *x, int M, int K, int act_is_bf16, void *stream);
+
+/* Backward pass of a layer whose codes, scales and zero points stay as they are (Section 4.2 trains A and B):
+ *     s = dy . B,  t = x . A^T:    dx = dy . dequant(Q, s, z) + s . A,    dA = s^T . x,    dB = dy^T . t
+ * dy [M][N], x and dx [M][K], dA [rank][K], dB [N][rank], all in the activation type (act_is_bf16).  x is given so or, with x == NULL, as
+ * x8 [M][K] with x8_scales (fbq_act8_pack).  dx may be NULL, and dA and dB may both be (x then as well); rank == 0 has neither.
+ * M == 0: dA and dB are set to zero.  Sums are fp32; s, t and the dequantised weights are rounded once to the activation type where they
+ * become operands.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, rank <= 256; else
+ * FBQ_ERR_UNSUPPORTED.  Every pointer is 16-byte aligned; outputs overlap no input and not each other.
+ * Scratch per stream: a 16-bit copy of the weights (up to 512 MB), M x (2 rank, rounded up to 64) and, for x8, M x K values of 16 bits, and
+ * partial sums of dA and dB; it grows as described at fbq_linear, and a call that would grow it during a capture returns
+ * FBQ_ERR_UNSUPPORTED and queues nothing.  Graphs captured on one stream share its scratch: replay them one after another. */
+int fbq_linear_backward(const void *dy, const void *x, const int8_t *x8, const float *x8_scales, const uint32_t *qweight,
+                        const void *scales, const void *zeros, const void *A, const void *B, void *dx, void *dA, void *dB, int M, int N, int K,
+                        int group, int bits, int rank, int act_is_bf16, void *stream);
+
+/* Backward pass of fbq_gated for dh [M][N/2], from the products it kept:
+ *     dp[gate] = dh * p[up] * f'(p[gate]),   dp[up] = dh * f(p[gate])
+ * (rounded once to the activation type, M x N more values of scratch), and from there as fbq_linear_backward with dy = dp.  Where B holds
+ * the other branch's zeros dB is 0, so that a step along it leaves them. */
+int fbq_gated_backward(const void *dh, const int8_t *kept, const float *kept_scales, const void *x, const int8_t *x8, const float *x8_scales,
+                       const uint32_t *qweight, const void *scales, const void *zeros, const void *A, const void *B, void *dx, void *dA,
+                       void *dB, int M, int N, int K, int group, int bits, int rank, int gate, int act_is_bf16, void *stream);
 
 /* Comparator, not a product path: the UNFUSED low-rank sub-branch of the paper's Section 3.2 / Fig. "kernel-fusion"
  * (the quantised main path plus separate launches for the branch), which Section 4.3's fused kernel replaces.

@@ -14,7 +14,12 @@ from .binding import (  # noqa: F401
     KERNEL_PREFILL,
     Problem,
     STATUS,
+    act8_pack,
+    act8_unpack,
     dequant,
+    gated,
+    gated_backward,
+    gated_layer,
     get_option,
     gram,
     launch_count,
@@ -22,6 +27,7 @@ from .binding import (  # noqa: F401
     library_path,
     make_batch,
     linear,
+    linear_backward,
     linear_batch,
     linear_hostio,
     linear_noalloc,

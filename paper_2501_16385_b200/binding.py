@@ -63,6 +63,12 @@ def lib() -> ctypes.CDLL:
         L.fbq_reconstruct_workspace_floats.argtypes = [i32, i32, i32]
         L.fbq_gram.argtypes = [vp, vp, i32, i32, vp]
         L.fbq_reconstruct_step.argtypes = [vp, vp, vp, vp, ctypes.c_float, vp, vp, i32, i32, i32, i32, i32, vp]
+        L.fbq_gated_layer.argtypes = [vp] * 15 + [i32] * 5 + [vp]
+        L.fbq_gated.argtypes = [vp] * 9 + [i32] * 8 + [vp]
+        for name in ("fbq_act8_pack", "fbq_act8_unpack"):
+            getattr(L, name).argtypes = [vp] * 3 + [i32] * 3 + [vp]
+        L.fbq_linear_backward.argtypes = [vp] * 12 + [i32] * 7 + [vp]
+        L.fbq_gated_backward.argtypes = [vp] * 14 + [i32] * 8 + [vp]
         L.fbq_linear_batch.argtypes = [ctypes.POINTER(Problem), i32, i32, i32, i32, i32, i32, vp]
         L.fbq_linear_batch_hostio.argtypes = [ctypes.POINTER(Problem), i32, i32, i32, i32, i32, i32, vp]
         L.fbq_select_kernel.argtypes = [i32] * 7
@@ -233,6 +239,169 @@ def reconstruct_step(W, H, A, B, lr: float, group: int, bits: int, workspace=Non
     _check(lib().fbq_reconstruct_step(_ptr(W), _ptr(H), _ptr(A), _ptr(B), float(lr), _ptr(loss), _ptr(workspace), N, K,
                                       group, bits, rank, _stream(stream)), "fbq_reconstruct_step")
     return loss, workspace
+
+
+GATES = {"silu": 0, "gelu": 1}
+KEPT_GROUP = 128
+
+
+def _operand(t, shape, dtype, device, what):
+    """Checks one tensor argument of the calls below: they take addresses, so what is not as the C ABI says must not get there."""
+    if not t.is_cuda or t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on %s, got %s %s on %s%s" %
+                         (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", not contiguous"))
+
+
+def _current_device():
+    import torch
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def _act_type(t, what):
+    import torch
+    if t.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("%s must be float16 or bfloat16, got %s" % (what, t.dtype))
+    return 1 if t.dtype == torch.bfloat16 else 0
+
+
+def _gate(fn: str) -> int:
+    if fn not in GATES:
+        raise ValueError("fn must be one of %s, got %r" % (sorted(GATES), fn))
+    return GATES[fn]
+
+
+def _layer_operands(qweight, scales, zeros, A, B, N, K, group, bits, act, device):
+    """Checks a layer's tensors against N, K; returns its rank."""
+    import torch
+    if group < 1 or K % group != 0:
+        raise ValueError("K = %d is not a multiple of group = %d" % (K, group))
+    _operand(qweight.reshape(-1), (packed_words(N, K, bits),), torch.int32, device, "qweight")
+    if not qweight.is_contiguous():
+        raise ValueError("qweight must be contiguous")
+    for t, what in ((scales, "scales"), (zeros, "zeros")):
+        _operand(t, (N, K // group), torch.float16, device, what)
+    if (A is None) != (B is None):
+        raise ValueError("A and B belong together")
+    if A is None:
+        return 0
+    _operand(A, (A.shape[0], K), act, device, "A")
+    _operand(B, (N, A.shape[0]), act, device, "B")
+    return A.shape[0]
+
+
+def gated_layer(gate, up, group: int, bits: int, stream=None):
+    """fbq_gated_layer: two projections (qweight, scales, zeros, A, B) of F rows each (A = B = None for rank 0) as the
+    gated layer's (qweight, scales, zeros, A, B)."""
+    import torch
+    F, K = gate[1].shape[0], gate[1].shape[1] * group
+    dev, act = _current_device(), (torch.float16 if gate[3] is None else gate[3].dtype)
+    if gate[3] is not None:
+        _act_type(gate[3], "A")
+    ranks = [_layer_operands(*branch, F, K, group, bits, act, dev) for branch in (gate, up)]
+    if ranks[0] != ranks[1]:
+        raise ValueError("both branches have one rank, got %d and %d" % tuple(ranks))
+    r = ranks[0]
+    q = torch.empty(packed_words(2 * F, K, bits), dtype=torch.int32, device=dev)
+    s, z = (torch.empty((2 * F, K // group), dtype=torch.float16, device=dev) for _ in range(2))
+    A = torch.empty((2 * r, K), dtype=act, device=dev) if r else None
+    B = torch.empty((2 * F, 2 * r), dtype=act, device=dev) if r else None
+    _check(lib().fbq_gated_layer(*(_ptr(t) for t in (*gate, *up, q, s, z, A, B)), F, K, group, bits, r, _stream(stream)), "fbq_gated_layer")
+    return q, s, z, A, B
+
+
+def gated(x, qweight, scales, zeros, A, B, N: int, group: int, bits: int, fn: str = "silu", save: bool = False, h=None, stream=None):
+    """fbq_gated: h [M, N/2] of a gated layer of N rows, fn "silu" or "gelu".  With save returns (h, codes, scales): the layer's
+    products in 8 bits, for gated_backward."""
+    import torch
+    gate, dev, bf16 = _gate(fn), _current_device(), _act_type(x, "x")
+    M, K = x.shape
+    _operand(x, (M, K), x.dtype, dev, "x")
+    rank = _layer_operands(qweight, scales, zeros, A, B, N, K, group, bits, x.dtype, dev)
+    if h is None:
+        h = torch.empty((M, N // 2), dtype=x.dtype, device=dev)
+    else:
+        _operand(h, (M, N // 2), x.dtype, dev, "h")
+    codes = torch.empty((M, N), dtype=torch.int8, device=dev) if save else None
+    kept = torch.empty((M, -(-N // KEPT_GROUP)), dtype=torch.float32, device=dev) if save else None
+    _check(lib().fbq_gated(_ptr(x), _ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(A), _ptr(B), _ptr(h), _ptr(codes), _ptr(kept), M, N, K, group, bits, rank,
+                           gate, bf16, _stream(stream)), "fbq_gated")
+    return (h, codes, kept) if save else h
+
+
+def act8_pack(x, stream=None):
+    """fbq_act8_pack: x [M, K] fp16 or bf16 -> (codes int8 [M, K], scales float32 [M, ceil(K/128)])."""
+    import torch
+    bf16, dev = _act_type(x, "x"), _current_device()
+    M, K = x.shape
+    _operand(x, (M, K), x.dtype, dev, "x")
+    codes = torch.empty((M, K), dtype=torch.int8, device=dev)
+    scales = torch.empty((M, -(-K // KEPT_GROUP)), dtype=torch.float32, device=dev)
+    _check(lib().fbq_act8_pack(_ptr(x), _ptr(codes), _ptr(scales), M, K, bf16, _stream(stream)), "fbq_act8_pack")
+    return codes, scales
+
+
+def _kept_operands(codes, scales, shape, device, what):
+    import torch
+    _operand(codes, shape, torch.int8, device, what + " codes")
+    _operand(scales, (shape[0], -(-shape[1] // KEPT_GROUP)), torch.float32, device, what + " scales")
+
+
+def act8_unpack(codes, scales, dtype, stream=None):
+    """fbq_act8_unpack: what act8_pack's codes stand for, as dtype (torch.float16 or torch.bfloat16)."""
+    import torch
+    dev = _current_device()
+    _kept_operands(codes, scales, codes.shape, dev, "kept")
+    x = torch.empty(codes.shape, dtype=dtype, device=dev)
+    _check(lib().fbq_act8_unpack(_ptr(codes), _ptr(scales), _ptr(x), codes.shape[0], codes.shape[1], _act_type(x, "dtype"), _stream(stream)), "fbq_act8_unpack")
+    return x
+
+
+def _backward_operands(x, qweight, scales, zeros, A, B, M, N, K, group, bits, act, dev, want_dx, want_factors):
+    """Checks the operands that the two backward passes share; returns rank, the addresses of x, and the outputs."""
+    import torch
+    rank = _layer_operands(qweight, scales, zeros, A, B, N, K, group, bits, act, dev)
+    if isinstance(x, (tuple, list)):
+        codes, x_scales = x
+        _kept_operands(codes, x_scales, (M, K), dev, "x")
+        xs = (None, _ptr(codes), _ptr(x_scales))
+    elif x is not None:
+        _operand(x, (M, K), act, dev, "x")
+        xs = (_ptr(x), None, None)
+    else:
+        xs = (None, None, None)
+    dx = torch.empty((M, K), dtype=act, device=dev) if want_dx else None
+    dA = torch.empty((rank, K), dtype=act, device=dev) if want_factors and rank else None
+    dB = torch.empty((N, rank), dtype=act, device=dev) if want_factors and rank else None
+    return rank, xs, dx, dA, dB
+
+
+def linear_backward(dy, x, qweight, scales, zeros, A, B, group: int, bits: int, want_dx: bool = True, want_factors: bool = True, stream=None):
+    """fbq_linear_backward: (dx, dA, dB) of a layer for dy [M, N].  x: [M, K] as in the forward pass, or (codes, scales) of
+    act8_pack; None without want_factors.  What is not wanted, and the factors' gradients at rank 0, are None."""
+    dev, bf16 = _current_device(), _act_type(dy, "dy")
+    M, N = dy.shape
+    K = scales.shape[1] * group
+    _operand(dy, (M, N), dy.dtype, dev, "dy")
+    rank, xs, dx, dA, dB = _backward_operands(x, qweight, scales, zeros, A, B, M, N, K, group, bits, dy.dtype, dev, want_dx, want_factors)
+    _check(lib().fbq_linear_backward(_ptr(dy), *xs, _ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(A), _ptr(B), _ptr(dx), _ptr(dA), _ptr(dB), M, N, K, group, bits,
+                                     rank, bf16, _stream(stream)), "fbq_linear_backward")
+    return dx, dA, dB
+
+
+def gated_backward(dh, kept, x, qweight, scales, zeros, A, B, group: int, bits: int, fn: str = "silu", want_dx: bool = True, want_factors: bool = True,
+                   stream=None):
+    """fbq_gated_backward: (dx, dA, dB) of a gated layer for dh [M, N/2]; kept: the (codes, scales) that gated(save=True)
+    returned.  x and the results are as in linear_backward."""
+    gate, dev, bf16 = _gate(fn), _current_device(), _act_type(dh, "dh")
+    M, N = dh.shape[0], 2 * dh.shape[1]
+    K = scales.shape[1] * group
+    _operand(dh, (M, N // 2), dh.dtype, dev, "dh")
+    codes, kept_scales = kept
+    _kept_operands(codes, kept_scales, (M, N), dev, "kept")
+    rank, xs, dx, dA, dB = _backward_operands(x, qweight, scales, zeros, A, B, M, N, K, group, bits, dh.dtype, dev, want_dx, want_factors)
+    _check(lib().fbq_gated_backward(_ptr(dh), _ptr(codes), _ptr(kept_scales), *xs, _ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(A), _ptr(B), _ptr(dx), _ptr(dA),
+                                    _ptr(dB), M, N, K, group, bits, rank, gate, bf16, _stream(stream)), "fbq_gated_backward")
+    return dx, dA, dB
 
 
 def make_batch(problems):

@@ -247,7 +247,7 @@ int run_split(const LinearArgs *a, int count, const GemvTuning &gt, Workspace *w
 // At one and two tokens the streaming kernel's integer form is ahead: 4096 -> 4096 rank 64 4.8 / 7.1 and 5.7 / 7.1.
 bool split_takes(const LinearArgs &a, int kernel)
 {
-    return g_opt.use_gemv && a.M > kGemvMaxM && split_supported(a) && (kernel == FBQ_KERNEL_DECODE || (kernel == FBQ_KERNEL_PREFILL && g_opt.force_kernel < 0));
+    return g_opt.use_gemv && !a.kept && a.M > kGemvMaxM && split_supported(a) && (kernel == FBQ_KERNEL_DECODE || (kernel == FBQ_KERNEL_PREFILL && g_opt.force_kernel < 0));
 }
 
 // Several problems as one launch of the streaming or the split kernel on `s`; FBQ_ERR_UNSUPPORTED where they cannot share one.
@@ -278,6 +278,13 @@ int run_gemv_batch(const LinearArgs *a, int count, cudaStream_t s)
     return FBQ_OK;
 }
 
+// Gated layers are the streaming kernel's at one and two tokens, and the split kernel's at 3 to 16 where it has a plan (split_takes);
+// everything else is a prompt's.
+int gated_kernel(const LinearArgs &a)
+{
+    return g_opt.use_gemv && !a.kept && a.M <= kGemvMaxM && g_opt.force_kernel < 0 && gemv_supported(a) ? FBQ_KERNEL_DECODE : FBQ_KERNEL_PREFILL;
+}
+
 // decode_ctas > 0 overrides the decode kernel's grid-size bound for this call.
 int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
 {
@@ -289,7 +296,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
 
     Workspace *ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
-    int kernel = select_kernel(a.M, a.N, a.K, a.group, a.bits, a.rank, a.bf16);
+    int kernel = a.gate < 0 ? select_kernel(a.M, a.N, a.K, a.group, a.bits, a.rank, a.bf16) : gated_kernel(a);
     if (kernel == FBQ_KERNEL_NONE) return FBQ_ERR_UNSUPPORTED;
     int launches = 0;
     cudaError_t e = cudaSuccess;
@@ -324,6 +331,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         }
         if (e != cudaErrorInvalidConfiguration) return FBQ_ERR_CUDA;
         (void)cudaGetLastError();                 // no plan fits: the other decode kernel
+        if (a.gate >= 0) kernel = FBQ_KERNEL_PREFILL;
     }
     if (kernel == FBQ_KERNEL_DECODE) {
         size_t pf = 0;
@@ -358,7 +366,8 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         prefill_workspace_need(a, &need_c, &need_t, &need_p);
         // The dense kernel's matrix of weights is the largest scratch by far and the other kernel computes the same call without
         // it: where it cannot be had (device memory is used up, or the stream is being captured) that one runs.
-        bool dense = !g_opt.prefill_pair && prefill_dense(a);
+        // (What is kept of a gated layer's products is written by the dense kernel alone.)
+        bool dense = a.kept || (!g_opt.prefill_pair && prefill_dense(a));
         if (dense) {
             size_t need_w = 0, need_tags = 0, tf = 0;
             dense_workspace_need(a, &need_w, &need_tags, &tf);
@@ -369,6 +378,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
             dense = e == cudaSuccess;
             if (e == cudaErrorMemoryAllocation) (void)cudaGetLastError();
             else if (!dense && e != cudaErrorStreamCaptureUnsupported) return FBQ_ERR_CUDA;
+            if (!dense && a.kept) return grow_status(e);
             if (dense) need_t = std::max(need_t, tf);
         }
         if ((e = grow(ws->counters, have_c, (size_t)need_c, sizeof(int), s)) != cudaSuccess) return grow_status(e);
@@ -378,6 +388,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         e = launch_prefill(a, dense, *ws, s, &launches);
         if (e == cudaErrorInvalidConfiguration) {
             (void)cudaGetLastError();
+            if (a.gate >= 0) return FBQ_ERR_UNSUPPORTED;
             kernel = FBQ_KERNEL_GENERIC;
         } else if (e != cudaSuccess) {
             return FBQ_ERR_CUDA;
@@ -389,6 +400,71 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
             return FBQ_ERR_CUDA;
         if ((e = launch_generic(a, *ws, s, &launches)) != cudaSuccess) return FBQ_ERR_CUDA;
     }
+    g_launches += launches;
+    return FBQ_OK;
+}
+
+// Backward pass of a layer: `x` in the activation type or `x8` with its scales, dy in `g`, or where `kept` is given made from dh.
+struct Backward {
+    GradArgs g{};
+    const int8_t *x8 = nullptr;
+    const float *x8_scales = nullptr;
+    const void *dh = nullptr;
+    const int8_t *kept = nullptr;
+    const float *kept_scales = nullptr;
+    int gate = -1;
+    void *dA = nullptr, *dB = nullptr;
+};
+int run_backward(Backward &b, cudaStream_t s)
+{
+    GradArgs &g = b.g;
+    const bool factors = g.rank > 0 && b.dA, unpack = factors && b.x8;
+    if (!factors && !g.dx) return FBQ_OK;
+    Workspace *ws = workspace_for(s);
+    if (!ws) return FBQ_ERR_CUDA;
+    size_t need = 0;
+    auto place = [&](size_t bytes) {
+        const size_t at = need;
+        need += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const size_t M = g.M, thin = M * ((g.rank + 63) / 64 * 64) * 2;
+    const size_t x_at = place(unpack ? M * g.K * 2 : 0), dy_at = place(b.kept ? M * g.N * 2 : 0), s_at = place(thin), t_at = place(factors ? thin : 0),
+                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0);
+    cudaError_t e;
+    size_t have_c = (size_t)ws->n_counters, need_w = 0, need_tags = 0;
+    char *scratch = static_cast<char *>(ws->grad), *w16 = static_cast<char *>(ws->w16);
+    e = grow(scratch, ws->grad_bytes, std::max<size_t>(need, 256), 1, s);
+    ws->grad = scratch;
+    if (e != cudaSuccess) return grow_status(e);
+    grad_workspace_need(g, &need_w, &need_tags);
+    e = grow(w16, ws->w16_bytes, need_w, 1, s);
+    ws->w16 = w16;
+    if (e != cudaSuccess) return grow_status(e);
+    if ((e = grow(ws->tags, ws->n_tags, need_tags, sizeof(uint32_t), s)) != cudaSuccess) return grow_status(e);
+    if ((e = grow(ws->counters, have_c, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
+    ws->n_counters = (int)have_c;
+    int launches = 0;
+    if (unpack) {
+        if (launch_act8_unpack(b.x8, b.x8_scales, scratch + x_at, g.M, g.K, g.bf16, s) != cudaSuccess) return FBQ_ERR_CUDA;
+        g.x = scratch + x_at;
+        ++launches;
+    }
+    if (b.kept) {
+        if (launch_gate_grad(b.dh, b.kept, b.kept_scales, scratch + dy_at, g.M, g.N, b.gate, g.bf16, s) != cudaSuccess) return FBQ_ERR_CUDA;
+        g.dy = scratch + dy_at;
+        ++launches;
+    }
+    g.s16 = scratch + s_at;
+    g.t16 = factors ? scratch + t_at : nullptr;
+    PrefillTuning tune;
+    tune.pdl = g_opt.decode.pdl;
+    tune.flag_polls = g_opt.prefill_flag_polls;
+    tune.test_skip_flag = g_opt.test_prefill_skip_flag;
+    if (launch_grad(g, *ws, tune, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (factors && launch_factor_grads(g.dy, g.x, g.s16, g.t16, b.dA, b.dB, g.M, g.N, g.K, g.rank, b.kept != nullptr, g.bf16, scratch + part_at,
+                                       ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess)
+        return FBQ_ERR_CUDA;
     g_launches += launches;
     return FBQ_OK;
 }
@@ -621,6 +697,152 @@ int fbq_linear_bf16(const void *x, const uint32_t *qweight, const void *scales, 
                     const void *B, void *y, int M, int N, int K, int group, int bits, int rank, void *stream)
 {
     return linear_common(x, qweight, scales, zeros, A, B, y, M, N, K, group, bits, rank, true, stream);
+}
+
+// The domain of gated layers: what the kernels that gate have in common.
+static int check_gated(int M, int N, int K, int group, int bits, int rank, int gate)
+{
+    if (!well_formed(M, N, K, group, bits, rank) || (gate != FBQ_GATE_SILU && gate != FBQ_GATE_GELU) || N % 2 || rank % 2) return FBQ_ERR_BADARG;
+    return group == kGroupFast && N % 16 == 0 && rank % 16 == 0 && rank <= kMaxRank && M <= (1 << 22) ? FBQ_OK : FBQ_ERR_UNSUPPORTED;
+}
+
+static bool any_misaligned(std::initializer_list<const void *> ps)
+{
+    return std::any_of(ps.begin(), ps.end(), misaligned16);
+}
+
+int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void *gate_zeros, const void *gate_A, const void *gate_B, const uint32_t *up_q,
+                    const void *up_scales, const void *up_zeros, const void *up_A, const void *up_B, uint32_t *qweight, void *scales, void *zeros, void *A, void *B,
+                    int F, int K, int group, int bits, int rank, void *stream)
+{
+    if (F < 1 || rank < 0 || F > (1 << 29) || rank > (1 << 29)) return FBQ_ERR_BADARG;
+    if (const int rc = check_gated(1, 2 * F, K, group, bits, 2 * rank, FBQ_GATE_SILU); rc != FBQ_OK) return rc;
+    if (!gate_q || !gate_scales || !gate_zeros || !up_q || !up_scales || !up_zeros || !qweight || !scales || !zeros) return FBQ_ERR_BADARG;
+    if (rank > 0 && (!gate_A || !gate_B || !up_A || !up_B || !A || !B)) return FBQ_ERR_BADARG;
+    if (any_misaligned({gate_q, gate_scales, gate_zeros, up_q, up_scales, up_zeros, qweight, scales, zeros})) return FBQ_ERR_ALIGN;
+    if (rank > 0 && any_misaligned({gate_A, gate_B, up_A, up_B, A, B})) return FBQ_ERR_ALIGN;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const size_t sc = (size_t)(K / group) * 2, a_bytes = (size_t)rank * K * 2;
+    if (launch_interleave(gate_q, up_q, qweight, F, (size_t)K / 8 * bits, false, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (launch_interleave(gate_scales, up_scales, scales, F, sc, false, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (launch_interleave(gate_zeros, up_zeros, zeros, F, sc, false, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    g_launches += 3;
+    if (rank == 0) return FBQ_OK;
+    if (cudaMemcpyAsync(A, gate_A, a_bytes, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (cudaMemcpyAsync(static_cast<char *>(A) + a_bytes, up_A, a_bytes, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (launch_interleave(gate_B, up_B, B, F, (size_t)rank * 2, true, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    ++g_launches;
+    return FBQ_OK;
+}
+
+int fbq_gated(const void *x, const uint32_t *qweight, const void *scales, const void *zeros, const void *A, const void *B, void *h, int8_t *kept,
+              float *kept_scales, int M, int N, int K, int group, int bits, int rank, int gate, int act_is_bf16, void *stream)
+{
+    if (const int rc = check_gated(M, N, K, group, bits, rank, gate); rc != FBQ_OK) return rc;
+    if (M == 0) return FBQ_OK;
+    if (!kept != !kept_scales) return FBQ_ERR_BADARG;
+    LinearArgs a{};
+    a.x = x; a.qw = qweight;
+    a.scales = static_cast<const __half *>(scales);
+    a.zeros = static_cast<const __half *>(zeros);
+    a.A = rank > 0 ? A : nullptr;
+    a.B = rank > 0 ? B : nullptr;
+    a.y = h;
+    a.M = M; a.N = N; a.K = K; a.group = group; a.bits = bits; a.rank = rank; a.bf16 = act_is_bf16 != 0;
+    a.gate = gate; a.kept = kept; a.kept_scales = kept_scales;
+    if (const int rc = check_args(a); rc != FBQ_OK) return rc;
+    if (any_misaligned({scales, zeros, kept, kept_scales})) return FBQ_ERR_ALIGN;
+    apply_kernel_options();
+    return run_linear(a, static_cast<cudaStream_t>(stream));
+}
+
+// Of no tokens dx is empty and the factors' gradients are sums of nothing.
+static int backward_or_zero(Backward &b, cudaStream_t s)
+{
+    const GradArgs &g = b.g;
+    if (g.M > 0) return run_backward(b, s);
+    if (!b.dA && !b.dB) return FBQ_OK;
+    if (!b.dA || !b.dB) return FBQ_ERR_BADARG;
+    if (any_misaligned({b.dA, b.dB})) return FBQ_ERR_ALIGN;
+    if (cudaMemsetAsync(b.dA, 0, (size_t)g.rank * g.K * 2, s) != cudaSuccess || cudaMemsetAsync(b.dB, 0, (size_t)g.N * g.rank * 2, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    return FBQ_OK;
+}
+
+// What the two backward passes check alike; dy_or_dh: the gradient that comes in.
+static int check_backward(const Backward &b, const void *dy_or_dh, int group)
+{
+    const GradArgs &g = b.g;
+    if (!grad_supported(g.M, g.N, g.K, group, g.rank)) return FBQ_ERR_UNSUPPORTED;
+    if (!dy_or_dh || !g.qw || !g.scales || !g.zeros || (g.rank > 0 && (!g.A || !g.B)) || !b.dA != !b.dB) return FBQ_ERR_BADARG;
+    if (b.dA && ((!g.x && !b.x8) || (b.x8 && (g.x || !b.x8_scales)))) return FBQ_ERR_BADARG;
+    if (any_misaligned({dy_or_dh, g.qw, g.scales, g.zeros, g.A, g.B, g.x, b.x8, b.x8_scales, b.kept, b.kept_scales, g.dx, b.dA, b.dB})) return FBQ_ERR_ALIGN;
+    return FBQ_OK;
+}
+static Backward backward_args(const void *x, const int8_t *x8, const float *x8_scales, const uint32_t *qweight, const void *scales, const void *zeros, const void *A,
+                              const void *B, void *dx, void *dA, void *dB, int M, int N, int K, int bits, int rank, int act_is_bf16)
+{
+    Backward b;
+    b.g.x = x; b.g.qw = qweight;
+    b.g.scales = static_cast<const __half *>(scales);
+    b.g.zeros = static_cast<const __half *>(zeros);
+    b.g.A = rank > 0 ? A : nullptr;
+    b.g.B = rank > 0 ? B : nullptr;
+    b.g.dx = dx;
+    b.g.M = M; b.g.N = N; b.g.K = K; b.g.bits = bits; b.g.rank = rank; b.g.bf16 = act_is_bf16 != 0;
+    b.x8 = x8; b.x8_scales = x8_scales;
+    b.dA = rank > 0 ? dA : nullptr;
+    b.dB = rank > 0 ? dB : nullptr;
+    return b;
+}
+
+int fbq_linear_backward(const void *dy, const void *x, const int8_t *x8, const float *x8_scales, const uint32_t *qweight, const void *scales, const void *zeros,
+                        const void *A, const void *B, void *dx, void *dA, void *dB, int M, int N, int K, int group, int bits, int rank, int act_is_bf16,
+                        void *stream)
+{
+    if (!well_formed(M, N, K, group, bits, rank)) return FBQ_ERR_BADARG;
+    Backward b = backward_args(x, x8, x8_scales, qweight, scales, zeros, A, B, dx, dA, dB, M, N, K, bits, rank, act_is_bf16);
+    b.g.dy = dy;
+    if (M > 0)
+        if (const int rc = check_backward(b, dy, group); rc != FBQ_OK) return rc;
+    return backward_or_zero(b, static_cast<cudaStream_t>(stream));
+}
+
+int fbq_gated_backward(const void *dh, const int8_t *kept, const float *kept_scales, const void *x, const int8_t *x8, const float *x8_scales,
+                       const uint32_t *qweight, const void *scales, const void *zeros, const void *A, const void *B, void *dx, void *dA, void *dB, int M, int N, int K,
+                       int group, int bits, int rank, int gate, int act_is_bf16, void *stream)
+{
+    if (const int rc = check_gated(M, N, K, group, bits, rank, gate); rc != FBQ_OK) return rc;
+    Backward b = backward_args(x, x8, x8_scales, qweight, scales, zeros, A, B, dx, dA, dB, M, N, K, bits, rank, act_is_bf16);
+    b.dh = dh; b.kept = kept; b.kept_scales = kept_scales; b.gate = gate;
+    if (M > 0) {
+        if (!kept || !kept_scales) return FBQ_ERR_BADARG;
+        if (const int rc = check_backward(b, dh, group); rc != FBQ_OK) return rc;
+    }
+    return backward_or_zero(b, static_cast<cudaStream_t>(stream));
+}
+
+int fbq_act8_pack(const void *x, int8_t *codes, float *scales, int M, int K, int act_is_bf16, void *stream)
+{
+    if (M < 0 || K < 1) return FBQ_ERR_BADARG;
+    if (M == 0) return FBQ_OK;
+    if (!x || !codes || !scales) return FBQ_ERR_BADARG;
+    if (any_misaligned({x, codes, scales})) return FBQ_ERR_ALIGN;
+    const cudaError_t e = launch_act8_pack(x, codes, scales, M, K, act_is_bf16 != 0, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return e == cudaErrorInvalidConfiguration ? FBQ_ERR_UNSUPPORTED : FBQ_ERR_CUDA;
+    ++g_launches;
+    return FBQ_OK;
+}
+
+int fbq_act8_unpack(const int8_t *codes, const float *scales, void *x, int M, int K, int act_is_bf16, void *stream)
+{
+    if (M < 0 || K < 1) return FBQ_ERR_BADARG;
+    if (M == 0) return FBQ_OK;
+    if (!x || !codes || !scales) return FBQ_ERR_BADARG;
+    if (any_misaligned({x, codes, scales})) return FBQ_ERR_ALIGN;
+    const cudaError_t e = launch_act8_unpack(codes, scales, x, M, K, act_is_bf16 != 0, static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return e == cudaErrorInvalidConfiguration ? FBQ_ERR_UNSUPPORTED : FBQ_ERR_CUDA;
+    ++g_launches;
+    return FBQ_OK;
 }
 
 // Side streams and events of fbq_linear_batch, per device, created on first use and kept.
@@ -1032,6 +1254,7 @@ int fbq_release_workspaces(void)
         cudaFree(w.w16);
         cudaFree(w.tags);
         cudaFree(w.split);
+        cudaFree(w.grad);
         cudaFree(w.rec);
     }
     for (auto it = g_ws.begin(); it != g_ws.end();) {            // what is left of a stream are its options

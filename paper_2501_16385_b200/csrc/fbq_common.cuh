@@ -49,6 +49,8 @@ struct Workspace {
     void *split = nullptr;        // the split kernel's launch number and words of t, which carry it (starts at zero)
     size_t split_bytes = 0;
     int gemv_ctas = 0;            // option of the stream (fbq_set_stream_option); outlives the buffers
+    void *grad = nullptr;         // backward passes: x and dp in the activation type, s, t, partial sums (no invariant)
+    size_t grad_bytes = 0;
     void *rec = nullptr;          // split operands of the Gram matrix and the reconstruction step (no invariant)
     size_t rec_bytes = 0;
 };
@@ -64,12 +66,21 @@ struct LinearArgs {
     void *y;
     int M, N, K, group, bits, rank;
     bool bf16;
+    // The gated block: rows are eight of the gate, eight of the up projection, and so on, and y is h [M][N / 2].
+    int gate = -1;                // fbq_gate, or -1: a plain linear
+    int8_t *kept = nullptr;       // [M][N] codes and [M][ceil(N / 128)] scales of the products themselves, or none
+    float *kept_scales = nullptr;
 };
 
 // Launchers implemented in the kernel files.  Each returns a cudaError_t from
 // the launch and adds the number of kernels it launched to *launches.
 cudaError_t launch_pack(const uint8_t *codes, uint32_t *qw, int N, int K, int bits, cudaStream_t s);
 cudaError_t launch_unpack(const uint32_t *qw, uint8_t *codes, int N, int K, int bits, cudaStream_t s);
+cudaError_t launch_act8_pack(const void *x, int8_t *codes, float *scales, int M, int K, bool bf16, cudaStream_t s);
+cudaError_t launch_act8_unpack(const int8_t *codes, const float *scales, void *x, int M, int K, bool bf16, cudaStream_t s);
+// dp [M][N] of the gated block from dh [M][N / 2] and p in 8 bits.
+cudaError_t launch_gate_grad(const void *dh, const int8_t *codes, const float *scales, void *dp, int M, int N, int fn, bool bf16, cudaStream_t s);
+cudaError_t launch_interleave(const void *gate, const void *up, void *out, int F, size_t bytes, bool padded, cudaStream_t s);
 cudaError_t launch_dequant(const uint32_t *qw, const __half *sc, const __half *ze, float *W, int N,
                            int K, int group, int bits, cudaStream_t s);
 cudaError_t launch_generic(const LinearArgs &a, Workspace &ws, cudaStream_t s, int *launches);
@@ -138,6 +149,25 @@ struct PrefillTuning {
     int flag_polls = 0;        // 0: waits for t end by time, else after this many looks
     int test_skip_flag = 0;    // test switch: t is not announced (the wait for it must run out)
 };
+// Backward pass of a layer: s = dy.B, dx = dy.W + s.A and t = x.A^T (fbq_dense.cu), dA = s^T.x and dB = dy^T.t (fbq_grad.cu).
+struct GradArgs {
+    const void *dy;               // [M][N]
+    const void *x;                // [M][K], or none: no t
+    const uint32_t *qw;
+    const __half *scales, *zeros;
+    const void *A, *B;
+    void *dx;                     // [M][K] or none
+    void *s16, *t16;              // scratch [M][rank rounded up to 64]: s and t in the activation type
+    int M, N, K, bits, rank;
+    bool bf16;
+};
+bool grad_supported(int M, int N, int K, int group, int rank);
+void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags);
+cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);
+size_t factor_grad_scratch_bytes(int M, int N, int K, int rank);
+cudaError_t launch_factor_grads(const void *dy, const void *x, const void *s16, const void *t16, void *dA, void *dB, int M, int N, int K, int rank, bool gated,
+                                bool bf16, void *scratch, int *status, bool pdl, cudaStream_t s, int *launches);
+
 void dense_workspace_need(const LinearArgs &a, size_t *w16_bytes, size_t *tags, size_t *t_floats);
 cudaError_t launch_dense(const LinearArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);
 

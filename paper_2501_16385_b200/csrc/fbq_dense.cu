@@ -36,9 +36,11 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "fbq_common.cuh"
 #include "fbq_dequant.cuh"
+#include "fbq_gate.cuh"
 #include "fbq_maps.h"
 #include "fbq_umma.cuh"
 
@@ -65,6 +67,14 @@ constexpr uint32_t kBarOff = kYOff + 4u * kYBytes;
 constexpr uint32_t kNumBars = 2 * kStages + 4 + 2 * kClaims + kTiles + 1;   // full, empty, accumulator full and free, claims full and taken, tiles, next tile wanted
 static_assert(kTiles >= kStages + 2 + 3, "a slot of the tile ring must have been read when it is written again");
 constexpr size_t kSmem = kBarOff + kNumBars * 8u + (2 + kClaims + kTiles) * 4u;
+constexpr int kAmaxOff = (int)((kSmem + 15) / 16 * 16);          // Kept: the largest |p| of 32 tokens over each epilogue warp's rows
+constexpr size_t kSmemKept = kAmaxOff + 4 * 32 * 4;
+static_assert(kSmemKept <= 227 * 1024, "");
+// What a launch computes.  Linear: y.  Gated: h of a gated layer; Kept: h, and its products in 8 bits as well.  Grad: dx = dy.W + s.A, s = dy.B,
+// and t = x.A^T, for the backward pass of a layer: the features are W's columns, the contraction runs over its rows, so W16, A and B are
+// multiplied as they lie with their rows along the contraction (MN-major operands).
+enum Mode { kLinear, kGated, kKept, kGrad };
+constexpr uint32_t kBoxBytes = 64u * kBK * 2u;                   // a box of an MN-major operand
 // words of the tag scratch: launch number, CTAs that have left, next item, next tile; then tags of items and of t tiles
 constexpr int kTagEpoch = 0, kTagDone = 1, kTagNext = 2, kTagTile = 3, kTagFirst = 4;
 
@@ -81,7 +91,13 @@ struct DenseParams {
     int nft, ntt, tok;        // feature tiles, token tiles, tokens per tile
     int n_t;                  // t tiles (0 without a sub-branch)
     int rank, a_rows;         // rows of A that a CTA of a t tile loads
-    int nkc;                  // items along K
+    int nkc;                  // items along K (Grad: along N)
+    int gate;                 // Gated, Kept: the gate
+    float *kept_scales;       // Kept: [M][ceil of all rows / 128], from this launch's first row on
+    int kept_pitch;
+    int K_all, k_first;       // Grad: columns of W, the first of this launch's K
+    int n_t2;                 // Grad: tiles of t = x.A^T
+    void *t2;                 // Grad: [M][rank_pad]
     int wave_ft;              // feature tiles that are in work at the same time
     uint32_t wait_looks;      // 0: waits for tags end by time; else after this many looks
     int test_skip_flag;       // test switch: the t tiles do not tag themselves
@@ -194,11 +210,11 @@ __device__ __forceinline__ int tile_at(uint32_t i, uint32_t tfull0, const volati
 // A dequantising warp does its unit (kUnitRows rows x kItemK k) of every item of its CTA.  Alone on its latencies (codes
 // from HBM, the arithmetic, the fence behind its stores) it would take 3 us per unit, so the next item's codes are
 // requested before this one's are turned.
-template <int BITS, typename T>
+template <int BITS, typename T, int MODE>
 __device__ __forceinline__ bool dequantise(const DenseParams &p, uint32_t tag, uint32_t cfull0, uint32_t cempty0, volatile int *ring)
 {
     const int lane = threadIdx.x & 31;
-    const int n_items = p.nft * p.nkc, G = p.K / kGroupFast, wave = p.wave_ft * p.nkc, sub = (threadIdx.x >> 5) - kDqWarp;
+    const int n_items = p.nft * p.nkc, K_all = MODE == kGrad ? p.K_all : p.K, k_first = MODE == kGrad ? p.k_first : 0, G = K_all / kGroupFast, wave = p.wave_ft * p.nkc, sub = (threadIdx.x >> 5) - kDqWarp;
     constexpr int NW = (BITS == 4) ? 4 : 3, NP = kUnitRows / kPassRows;
     struct Codes {
         uint32_t w[NP][NW];
@@ -209,8 +225,8 @@ __device__ __forceinline__ bool dequantise(const DenseParams &p, uint32_t tag, u
         const int group = item / wave, fts = min(p.wave_ft, p.nft - group * p.wave_ft), r = item - group * wave;
         const int kc = r / fts, ft = group * p.wave_ft + r % fts;
         word = (ft * p.nkc + kc) * kUnits + sub;
-        row = ft * kFeat + sub * kUnitRows + lane / kRowLanes;
-        k0 = kc * kItemK + lane % kRowLanes * 32;
+        row = (MODE == kGrad ? kc : ft) * kFeat + sub * kUnitRows + lane / kRowLanes;
+        k0 = (MODE == kGrad ? ft : kc) * kItemK + lane % kRowLanes * 32;
     };
     auto load = [&](int item, Codes &c) {
         int word, row, k0;
@@ -218,8 +234,8 @@ __device__ __forceinline__ bool dequantise(const DenseParams &p, uint32_t tag, u
 #pragma unroll
         for (int i = 0; i < NP; ++i, row += kPassRows) {
             const bool in = row < p.N && k0 < p.K;
-            const uint32_t *src = p.qw + (in ? ((size_t)row * p.K + k0) / 32 * NW : 0);
-            const size_t g = in ? (size_t)row * G + k0 / kGroupFast : 0;
+            const uint32_t *src = p.qw + (in ? ((size_t)row * K_all + (k_first + k0)) / 32 * NW : 0);
+            const size_t g = in ? (size_t)row * G + (k_first + k0) / kGroupFast : 0;
             if constexpr (BITS == 4) {
                 const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
                 c.w[i][0] = v.x; c.w[i][1] = v.y; c.w[i][2] = v.z; c.w[i][3] = v.w;
@@ -285,13 +301,17 @@ __device__ __forceinline__ bool dequantise(const DenseParams &p, uint32_t tag, u
 
 // xmap: x [M][K], boxes of tok / 2 rows; xtmap: boxes of kTTok / 2 rows; wmap: W16 [N][K]; amap: A [rank][K];
 // bmap: B [N][rank]; tmap: t16 [M][rank_pad], boxes of tok / 2 rows.  All these boxes are 64 elements wide, operand boxes
-// of weights 128 rows (of A a_rows), 128-byte swizzle.  ymap: y [M][N], boxes of 16 rows x 128 elements, no swizzle.
-template <int BITS, typename T>
+// of weights 128 rows (of A a_rows), 128-byte swizzle.  ymap: y [M][N], boxes of 16 rows x 128 elements (Gated: h [M][N / 2], 64), no
+// swizzle.  ex0, Kept: the codes [M][N], boxes of 16 rows x 128.
+// Grad: xmap, xtmap: dy [M][N]; wmap: W16 [N][K], bmap: B, ex0: A [rank][K_all], boxes of 64 rows, all three MN-major; ex1: x [M][K_all]
+// like xtmap; ymap: dx [M][K_all] from its column k_first on.
+template <int BITS, typename T, int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap xtmap, const __grid_constant__ CUtensorMap wmap,
              const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap, const __grid_constant__ CUtensorMap tmap,
-             const __grid_constant__ CUtensorMap ymap, const DenseParams p)
+             const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap ex0, const __grid_constant__ CUtensorMap ex1, const DenseParams p)
 {
+    constexpr bool GRAD = MODE == kGrad;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     const uint32_t full0 = sbase + kBarOff, empty0 = full0 + 8u * kStages, accf0 = empty0 + 8u * kStages, acce0 = accf0 + 16u,
@@ -300,8 +320,9 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1), *ring = quit + 1, *tiles = ring + kClaims;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t cr = cluster_ctarank();                       // 0: leader
-    const int kbx = p.K / kBK, slab = p.rank_pad / kBK;
-    const int n_all = p.n_t + p.nft * p.ntt;
+    // blocks of the contraction (Grad: an even number of them, like K's: a stage holds none of both operands)
+    const int kbx = GRAD ? (p.N + 2 * kBK - 1) / (2 * kBK) * 2 : p.K / kBK, slab = p.rank_pad / kBK;
+    const int n_main = p.n_t + p.nft * p.ntt, n_all = GRAD ? n_main + p.n_t2 : n_main;
     uint32_t *const t_tags = p.tags + kTagFirst + p.nft * p.nkc * kUnits;
 
     pdl_launch_dependents();
@@ -337,8 +358,8 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
     }
     // The first pass over codes and x would otherwise meet HBM's latency at every block: with all stages in flight that is
     // 0.43 us per block of K against 0.27 of MMAs.  (Where they are larger, a small part of the time is spent on first passes.)
-    if (warp == 3) {
-        const size_t cells = (size_t)p.N * p.K, groups = (size_t)p.N * (p.K / kGroupFast) * 2, x_bytes = (size_t)p.M * p.K * 2;
+    if (GRAD ? warp == 3 && p.nft > 0 && p.K == p.K_all : warp == 3) {
+        const size_t cells = (size_t)p.N * p.K, groups = (size_t)p.N * (p.K / kGroupFast) * 2, x_bytes = (size_t)p.M * (GRAD ? p.N : p.K) * 2;
         if (cells <= (size_t)64 << 20) {
             prefetch_share(p.scales, groups);
             prefetch_share(p.zeros, groups);
@@ -365,16 +386,17 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
             const int q = tile_at(it, tfull0, tiles, quit);
             if (q < 0) ok = false;
             if (!__all_sync(0xffffffffu, q >= 0 && q < n_all)) break;
-            const bool t_role = q < p.n_t;
+            const bool t2_role = GRAD && q >= n_main, t_role = q < p.n_t || t2_role;
             const int ft = t_role ? 0 : (q - p.n_t) / p.ntt, tt = t_role ? 0 : (q - p.n_t) % p.ntt;
             const int wrow = t_role ? 128 * (int)cr : ft * kFeat + 128 * (int)cr;
-            const int xrow = t_role ? q * kTTok + (kTTok / 2) * (int)cr : tt * p.tok + (p.tok >> 1) * (int)cr;
+            const int xrow = t_role ? (t2_role ? q - n_main : q) * kTTok + (kTTok / 2) * (int)cr : tt * p.tok + (p.tok >> 1) * (int)cr;
             // a t tile's rows beyond the rank are left out (whatever they hold reaches only rows nobody reads); boxes that
             // are mostly out of bounds are slow
             const bool w_load = !t_role || (int)cr * 128 < p.rank_pad;
-            const uint32_t bytes = t_role ? (uint32_t)p.a_rows * (p.rank_pad > 128 ? 2u : 1u) * (kBK * 2u) + kTTok * (kBK * 2u)
+            const uint32_t bytes = GRAD && q < p.n_t ? (uint32_t)slab * kBoxBytes + kTTok * (kBK * 2u)
+                                 : t_role ? (uint32_t)p.a_rows * (p.rank_pad > 128 ? 2u : 1u) * (kBK * 2u) + kTTok * (kBK * 2u)
                                           : 2u * kHalfBytes + (uint32_t)p.tok * (kBK * 2u);
-            const int nkb = t_role ? kbx : kbx + slab;
+            const int nkb = t2_role ? p.K_all / kBK : t_role ? kbx : kbx + slab, kb_slab = t2_role ? nkb : kbx;
             const int half_way = nkb / (2 * kPer) * kPer;
             int ready = 0;                                       // items of this feature tile known to be there
 #pragma unroll 1
@@ -383,16 +405,16 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                 if (kb == half_way && cr == 0 && lane == 0) mbar_arrive(want);
                 if (!t_role && kb < kbx && kb / (kItemK / kBK) >= ready) {
                     // a lane looks at four of the kUnits / 2 tags of this CTA's rows: sixteen items at a time (a look takes
-                    // about as long as the copies run ahead, so there should be few)
-                    constexpr int group = kUnits / 2 / 4;
+                    // about as long as the copies run ahead, so there should be few).  Grad: all units of an item hold rows of a block
+                    constexpr int group = (GRAD ? kUnits : kUnits / 2) / 4;
                     const int kc = ready + lane / group;
-                    const uint32_t *word = p.tags + kTagFirst + (ft * p.nkc + kc) * kUnits + (int)cr * (kUnits / 2) + lane % group * 4;
+                    const uint32_t *word = p.tags + kTagFirst + (ft * p.nkc + kc) * kUnits + (GRAD ? 0 : (int)cr * (kUnits / 2)) + lane % group * 4;
                     const int n = wait_tags(p, [&] { return kc < p.nkc && tags_are(word, tag); }, group, quit);
                     if (n == 0) { ok = false; break; }
                     ready += n;
                     if (lane == 0) asm volatile("fence.proxy.async;" ::: "memory");
                 }
-                if (kb == kbx) {                                 // t of this tile's tokens, from both CTAs of each t tile
+                if (kb == kb_slab) {                             // t of this tile's tokens, from both CTAs of each t tile
                     const int t0 = tt * p.tok / kTTok, t1 = (min(p.M, (tt + 1) * p.tok) + kTTok - 1) / kTTok;
                     for (int i = 2 * t0; i < 2 * t1;) {
                         const int n = wait_tags(p, [&] { return i + lane < 2 * t1 && load_acquire(t_tags + i + lane) == tag; }, 1, quit);
@@ -408,12 +430,20 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                     } else {
                         const uint32_t bar = lfull0 + 8u * s;
                         if (cr == 0) mbar_expect_tx(full0 + 8u * s, bytes * nb);
-                        const bool is_slab = kb >= kbx;
+                        const bool is_slab = kb >= kb_slab;
                         for (int j = 0; j < nb; ++j) {
                             const uint32_t wt = sbase + s * kStageBytes + j * kBlockBytes, xt = wt + kHalfBytes;
-                            const int k0 = ((is_slab ? kb - kbx : kb) + j) * kBK;
-                            if (w_load) umma::tma_load_2d_pair(wt, t_role ? &amap : is_slab ? &bmap : &wmap, k0, wrow, bar);
-                            umma::tma_load_2d_pair(xt, t_role ? &xtmap : is_slab ? &tmap : &xmap, k0, xrow, bar);
+                            const int k0 = ((is_slab ? kb - kb_slab : kb) + j) * kBK;
+                            if (GRAD && !t2_role) {
+                                // boxes of 64 features x 64 of the contraction
+                                const CUtensorMap *map = t_role ? &bmap : is_slab ? &ex0 : &wmap;
+                                for (int b = 0; b < 2; ++b)
+                                    if (!t_role || wrow + 64 * b < p.rank_pad)
+                                        umma::tma_load_2d_pair(wt + b * kBoxBytes, map, wrow + 64 * b + (is_slab ? p.k_first : 0), k0, bar);
+                            } else if (w_load) {
+                                umma::tma_load_2d_pair(wt, t_role ? &amap : is_slab ? &bmap : &wmap, k0, wrow, bar);
+                            }
+                            umma::tma_load_2d_pair(xt, t2_role ? &ex1 : t_role ? &xtmap : is_slab ? &tmap : &xmap, k0, xrow, bar);
                         }
                     }
                 }
@@ -431,9 +461,12 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                 const int q = tile_at(it, tfull0, tiles, quit);
                 if (q < 0) ok = false;
                 if (q < 0 || q >= n_all) break;
-                const bool t_role = q < p.n_t;
-                const int nkb = t_role ? kbx : kbx + slab;
-                const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, 2 * 128, (uint32_t)(t_role ? kTTok : p.tok));
+                const bool t2_role = GRAD && q >= n_main, t_role = q < p.n_t || t2_role, mn = GRAD && !t2_role;
+                const int nkb = t2_role ? p.K_all / kBK : t_role ? kbx : kbx + slab;
+                const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, 2 * 128, (uint32_t)(t_role ? kTTok : p.tok)) | (mn ? umma::kIdescMnA : 0u);
+                // 16 of the contraction on, in the weights' operand (MN-major: 16 rows; else 32 bytes)
+                const uint32_t wstep = mn ? 2048u >> 4 : 2u;
+                const uint64_t wdesc0 = mn ? umma::desc_mn128(sbase, kBoxBytes) : desc0;
                 const uint32_t buf = it & 1u, d = tmem + buf * 256u;
                 if (it >= 2 && !umma::wait_cluster(acce0 + 8u * buf, ((it >> 1) - 1u) & 1u, quit)) { ok = false; break; }
                 umma::fence_after();
@@ -442,16 +475,16 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                 for (int kb = 0; kb < nkb; kb += kPer) {
                     if (!there && !umma::wait_cluster(full0 + 8u * s, phase, quit)) { ok = false; break; }
                     umma::fence_after();
-                    const uint64_t wd = desc0 + s * (kStageBytes >> 4), xd = wd + (kHalfBytes >> 4);
+                    const uint64_t wd = wdesc0 + s * (kStageBytes >> 4), xd = desc0 + s * (kStageBytes >> 4) + (kHalfBytes >> 4);
                     const uint32_t freed = empty0 + 8u * s;
                     if (++s == kStages) { s = 0; phase ^= 1u; }
                     umma::mma_pair(d, wd, xd, idesc, kb ? 1u : 0u);
 #pragma unroll
-                    for (int j = 1; j < kBK / 16; ++j) umma::mma_pair(d, wd + 2 * j, xd + 2 * j, idesc, 1u);
+                    for (int j = 1; j < kBK / 16; ++j) umma::mma_pair(d, wd + wstep * j, xd + 2 * j, idesc, 1u);
                     if (kb + 1 < nkb) {
                         const uint64_t w2 = wd + (kBlockBytes >> 4), x2 = xd + (kBlockBytes >> 4);
 #pragma unroll
-                        for (int j = 0; j < kBK / 16; ++j) umma::mma_pair(d, w2 + 2 * j, x2 + 2 * j, idesc, 1u);
+                        for (int j = 0; j < kBK / 16; ++j) umma::mma_pair(d, w2 + wstep * j, x2 + 2 * j, idesc, 1u);
                     }
                     umma::commit_pair(freed);
                     there = mbar_try_wait(full0 + 8u * s, phase) != 0;
@@ -477,8 +510,8 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
             const uint32_t buf = it & 1u;
             if (!umma::wait_cluster(accf0 + 8u * buf, (it >> 1) & 1u, quit)) { ok = false; break; }
             umma::fence_after();
-            const bool t_role = q < p.n_t;
-            const int tt = t_role ? q : (q - p.n_t) % p.ntt, cols = t_role ? kTTok : p.tok;
+            const bool t2_role = GRAD && q >= n_main, t_role = q < p.n_t || t2_role;
+            const int tt = t2_role ? q - n_main : t_role ? q : (q - p.n_t) % p.ntt, cols = t_role ? kTTok : p.tok;
             const int m0 = tt * cols, m_end = min(p.M, m0 + cols);
             const int n = (t_role ? 0 : (q - p.n_t) / p.ntt * kFeat) + 128 * (int)cr + 32 * wq + lane;
             const uint32_t lanes = tmem + buf * 256u + ((uint32_t)(32 * wq) << 16);
@@ -494,7 +527,7 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                 }
                 if (t_role) {
                     if (n < p.rank_pad) {
-                        unsigned short *dst = static_cast<unsigned short *>(p.t16) + (size_t)(m0 + c) * p.rank_pad + n;
+                        unsigned short *dst = static_cast<unsigned short *>(t2_role ? p.t2 : p.t16) + (size_t)(m0 + c) * p.rank_pad + n;
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
                             if (j < m_end - (m0 + c)) dst[(size_t)j * p.rank_pad] = n < p.rank ? to_bits16<T>(__uint_as_float(v[j])) : (unsigned short)0;
@@ -505,23 +538,54 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                 // clips the edges of y): stores straight from the lanes took 9 us of a launch
                 const uint32_t at = (staged & 3u) * kYBytes;
                 if (tid == 4 * 32) asm volatile("cp.async.bulk.wait_group.read 3;" ::: "memory");
-                named_barrier_sync(1, 128);                      // the buffer's last copy has been read
-                unsigned short *row = reinterpret_cast<unsigned short *>(smem + kYOff + at) + 32 * wq + lane;
+                float *amax = reinterpret_cast<float *>(smem + kAmaxOff);
+                if constexpr (MODE == kKept) {                   // the largest |p| of each token over this warp's rows, lane = token
+                    uint32_t mine = 0u;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) row[j * 128] = to_bits16<T>(__uint_as_float(v[j]));
+                    for (int j = 0; j < 32; ++j) {
+                        const uint32_t top = __reduce_max_sync(0xffffffffu, v[j] & 0x7FFFFFFFu);
+                        if (lane == j) mine = top;
+                    }
+                    amax[32 * wq + lane] = __uint_as_float(mine);
+                }
+                named_barrier_sync(1, 128);                      // the buffer's last copy has been read
+                if constexpr (MODE == kGated || MODE == kKept)
+                    gate_chunk<T>(p.gate, v, reinterpret_cast<T *>(smem + kYOff + at) + 16 * wq);
+                if constexpr (MODE == kKept) {                   // a CTA's 128 rows are the columns that share a scale
+                    uint32_t top = 0u;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) top = max(top, __float_as_uint(amax[32 * w + lane]));
+                    float scale, inverse;
+                    kept_scale(top, scale, inverse);
+                    if (wq == 0 && n - lane < p.N && lane < m_end - (m0 + c)) p.kept_scales[(size_t)(m0 + c + lane) * p.kept_pitch + (n >> 7)] = scale;
+                    uint8_t *codes = smem + kYOff + at + kYBytes / 2 + 32 * wq + lane;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) codes[j * 128] = (uint8_t)kept_code(__uint_as_float(v[j]), __shfl_sync(0xffffffffu, inverse, j));
+                }
+                if constexpr (MODE == kLinear || MODE == kGrad) {
+                    unsigned short *row = reinterpret_cast<unsigned short *>(smem + kYOff + at) + 32 * wq + lane;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) row[j * 128] = to_bits16<T>(__uint_as_float(v[j]));
+                }
                 fence_proxy_async();
                 named_barrier_sync(1, 128);
                 if (tid == 4 * 32) {
                     const int n_first = n - lane;                // warp 4 holds the CTA's first features
-                    if (n_first < p.N && m0 + c < p.M) {
-                        tma_store_2d(&ymap, sbase + kYOff + at, n_first, m0 + c);
-                        if (c + 16 < cols && m0 + c + 16 < p.M) tma_store_2d(&ymap, sbase + kYOff + at + kYBytes / 2, n_first, m0 + c + 16);
+                    constexpr bool half = MODE == kGated || MODE == kKept;
+                    if (n_first < (GRAD ? p.K : p.N) && m0 + c < p.M) {
+                        const bool both = c + 16 < cols && m0 + c + 16 < p.M;
+                        tma_store_2d(&ymap, sbase + kYOff + at, half ? n_first / 2 : n_first, m0 + c);
+                        if (both) tma_store_2d(&ymap, sbase + kYOff + at + kYBytes / (half ? 4 : 2), half ? n_first / 2 : n_first, m0 + c + 16);
+                        if (MODE == kKept) {
+                            tma_store_2d(&ex0, sbase + kYOff + at + kYBytes / 2, n_first, m0 + c);
+                            if (both) tma_store_2d(&ex0, sbase + kYOff + at + kYBytes / 2 + kYBytes / 4, n_first, m0 + c + 16);
+                        }
                     }
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
                 ++staged;
             }
-            if (t_role) {
+            if (t_role && !t2_role) {
                 asm volatile("fence.proxy.async;" ::: "memory");  // t16 is read by TMA
                 __threadfence();
                 named_barrier_sync(1, 128);
@@ -530,7 +594,7 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
         }
         if (tid == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp >= kDqWarp) {
-        ok = dequantise<BITS, T>(p, tag, cfull0, cempty0, ring);
+        ok = dequantise<BITS, T, MODE>(p, tag, cfull0, cempty0, ring);
     }
     if (!ok) {
         *quit = 1;
@@ -558,6 +622,9 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
 }
 
 // ------------------------------------------------------------------ host side
+constexpr CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
+constexpr CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+
 int pairs_of_device()
 {
     static int n = 0;
@@ -603,9 +670,32 @@ int launch_rows(int N, int K)
     return (int)std::min((size_t)N, ((N + n - 1) / n + kFeat - 1) / kFeat * kFeat);
 }
 
-// a: the rows of one launch; y has rows of `pitch` elements.
-template <int BITS, typename T>
-cudaError_t run(const LinearArgs &a, int pitch, Workspace &ws, const PrefillTuning &tune, cudaStream_t s)
+template <int BITS, typename T, int MODE>
+cudaError_t start(const CUtensorMap (&maps)[9], const DenseParams &p, int n_pairs, bool pdl, cudaStream_t s)
+{
+    auto kern = dense_kernel<BITS, T, MODE>;
+    constexpr size_t smem = MODE == kKept ? kSmemKept : kSmem;
+    static bool attr_set = false;
+    if (!attr_set) {
+        if (const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+        attr_set = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(2 * n_pairs));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = pdl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], maps[6], maps[7], maps[8], p);
+}
+
+// a: the rows of one launch, from row n0 of `rows` on.
+template <int BITS, typename T, int MODE>
+cudaError_t run(const LinearArgs &a, int n0, int rows, Workspace &ws, const PrefillTuning &tune, cudaStream_t s)
 {
     DenseParams p{};
     p.x = a.x; p.qw = a.qw; p.scales = a.scales; p.zeros = a.zeros; p.y = a.y;
@@ -626,13 +716,22 @@ cudaError_t run(const LinearArgs &a, int pitch, Workspace &ws, const PrefillTuni
     p.wave_ft = std::max(1, std::min(p.nft, (n_pairs + p.ntt - 1) / p.ntt));
     p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
     p.test_skip_flag = tune.test_skip_flag;
-    const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
-    const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-    CUtensorMap xmap, xtmap, wmap, amap, bmap, tmap, ymap;
+    CUtensorMap maps[9];
+    CUtensorMap &xmap = maps[0], &xtmap = maps[1], &wmap = maps[2], &amap = maps[3], &bmap = maps[4], &tmap = maps[5], &ymap = maps[6];
     cudaError_t e;
-    MapSpec yspec = matrix_map(a.y, dt, 2, a.N, a.M, 128, 16, CU_TENSOR_MAP_SWIZZLE_NONE);
-    yspec.strides[0] = (cuuint64_t)pitch * 2;
+    constexpr int half = MODE == kLinear ? 1 : 2;
+    MapSpec yspec = matrix_map(a.y, dt, 2, a.N / half, a.M, 128 / half, 16, CU_TENSOR_MAP_SWIZZLE_NONE);
+    yspec.strides[0] = (cuuint64_t)(rows / half) * 2;
     if ((e = encode_map(&ymap, yspec)) != cudaSuccess) return e;
+    maps[7] = maps[8] = ymap;
+    if (MODE != kLinear) p.gate = a.gate;
+    if (MODE == kKept) {
+        MapSpec codes = matrix_map(a.kept + n0, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.N, a.M, 128, 16, CU_TENSOR_MAP_SWIZZLE_NONE);
+        codes.strides[0] = (cuuint64_t)rows;
+        if ((e = encode_map(&maps[7], codes)) != cudaSuccess) return e;
+        p.kept_pitch = (rows + kKeptGroup - 1) / kKeptGroup;
+        p.kept_scales = a.kept_scales + n0 / kKeptGroup;
+    }
     if ((e = encode_map(&xmap, matrix_map(a.x, dt, 2, a.K, a.M, kBK, p.tok / 2, sw))) != cudaSuccess) return e;
     if ((e = cached_map(&wmap, matrix_map(ws.w16, dt, 2, a.K, a.N, kBK, 128, sw))) != cudaSuccess) return e;
     xtmap = amap = bmap = tmap = xmap;
@@ -642,23 +741,64 @@ cudaError_t run(const LinearArgs &a, int pitch, Workspace &ws, const PrefillTuni
         if ((e = cached_map(&amap, matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
         if ((e = cached_map(&bmap, matrix_map(a.B, dt, 2, a.rank, a.N, kBK, 128, sw))) != cudaSuccess) return e;
     }
-    auto kern = dense_kernel<BITS, T>;
-    static bool attr_set = false;
-    if (!attr_set) {
-        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem)) != cudaSuccess) return e;
-        attr_set = true;
+    return start<BITS, T, MODE>(maps, p, n_pairs, tune.pdl != 0, s);
+}
+
+// W16 of a launch of Grad: all rows, as many of its columns as stay within kW16Most, whole tiles of them.
+int launch_columns(int N, int K)
+{
+    const size_t most = kW16Most / ((size_t)N * 2) / kFeat * kFeat;
+    if (most == 0) return 0;
+    const size_t n = (K + most - 1) / most;
+    return (int)std::min((size_t)K, ((K + n - 1) / n + kFeat - 1) / kFeat * kFeat);
+}
+
+// Columns [k_first, k_first + cols) of dx; `first`: and t.
+template <int BITS, typename T>
+cudaError_t run_grad(const GradArgs &a, int k_first, int cols, bool first, Workspace &ws, const PrefillTuning &tune, cudaStream_t s)
+{
+    DenseParams p{};
+    p.x = a.dy; p.qw = a.qw; p.scales = a.scales; p.zeros = a.zeros;
+    p.w16 = ws.w16;
+    p.t16 = a.s16;
+    p.t2 = a.t16;
+    p.tags = ws.tags;
+    p.status = ws.counters + kCtrStatus;
+    p.M = a.M; p.N = a.N; p.K = cols; p.K_all = a.K; p.k_first = k_first;
+    p.rank_pad = (a.rank + kBK - 1) / kBK * kBK;
+    p.rank = a.rank;
+    p.a_rows = std::min(128, p.rank_pad);
+    p.nft = a.dx ? (cols + kFeat - 1) / kFeat : 0;
+    p.tok = token_tile(a.M, p.nft, (a.N + kBK - 1) / kBK);
+    p.ntt = (a.M + p.tok - 1) / p.tok;
+    p.n_t = a.rank > 0 ? (a.M + kTTok - 1) / kTTok : 0;
+    p.n_t2 = a.rank > 0 && a.t16 && first ? p.n_t : 0;
+    p.nkc = (a.N + kItemK - 1) / kItemK;
+    const int n_pairs = std::max(1, std::min(pairs_of_device(), p.n_t + p.nft * p.ntt + p.n_t2));
+    p.wave_ft = std::max(1, std::min(p.nft, (n_pairs + p.ntt - 1) / p.ntt));
+    p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
+    p.test_skip_flag = tune.test_skip_flag;
+    CUtensorMap maps[9];
+    cudaError_t e;
+    if ((e = encode_map(&maps[0], matrix_map(a.dy, dt, 2, a.N, a.M, kBK, p.tok / 2, sw))) != cudaSuccess) return e;
+    for (int i = 1; i < 9; ++i) maps[i] = maps[0];
+    if (a.dx) {
+        MapSpec out = matrix_map(static_cast<uint16_t *>(a.dx) + k_first, dt, 2, cols, a.M, 128, 16, CU_TENSOR_MAP_SWIZZLE_NONE);
+        out.strides[0] = (cuuint64_t)a.K * 2;
+        if ((e = encode_map(&maps[6], out)) != cudaSuccess) return e;
+        if ((e = cached_map(&maps[2], matrix_map(ws.w16, dt, 2, cols, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
     }
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(2 * n_pairs));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = tune.pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, xmap, xtmap, wmap, amap, bmap, tmap, ymap, p);
+    if (a.rank > 0) {
+        if ((e = encode_map(&maps[1], matrix_map(a.dy, dt, 2, a.N, a.M, kBK, kTTok / 2, sw))) != cudaSuccess) return e;
+        if ((e = cached_map(&maps[4], matrix_map(a.B, dt, 2, a.rank, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&maps[5], matrix_map(a.s16, dt, 2, p.rank_pad, a.M, kBK, p.tok / 2, sw))) != cudaSuccess) return e;
+        if ((e = cached_map(&maps[7], matrix_map(a.A, dt, 2, a.K, a.rank, kBK, kBK, sw))) != cudaSuccess) return e;
+    }
+    if (p.n_t2 > 0) {
+        if ((e = cached_map(&maps[3], matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&maps[8], matrix_map(a.x, dt, 2, a.K, a.M, kBK, kTTok / 2, sw))) != cudaSuccess) return e;
+    }
+    return start<BITS, T, kGrad>(maps, p, n_pairs, tune.pdl != 0, s);
 }
 
 }  // namespace
@@ -695,9 +835,38 @@ cudaError_t launch_dense(const LinearArgs &a, Workspace &ws, const PrefillTuning
         c.scales = a.scales + (size_t)n0 * (a.K / kGroupFast);
         c.zeros = a.zeros + (size_t)n0 * (a.K / kGroupFast);
         if (a.rank > 0) c.B = static_cast<const uint16_t *>(a.B) + (size_t)n0 * a.rank;
-        c.y = static_cast<uint16_t *>(a.y) + n0;
-        e = a.bits == 4 ? (a.bf16 ? run<4, __nv_bfloat16>(c, a.N, ws, tune, s) : run<4, __half>(c, a.N, ws, tune, s))
-                        : (a.bf16 ? run<3, __nv_bfloat16>(c, a.N, ws, tune, s) : run<3, __half>(c, a.N, ws, tune, s));
+        c.y = static_cast<uint16_t *>(a.y) + (a.gate < 0 ? n0 : n0 / 2);
+        auto go = [&](auto mode) {
+            constexpr int MODE = decltype(mode)::value;
+            return a.bits == 4 ? (a.bf16 ? run<4, __nv_bfloat16, MODE>(c, n0, a.N, ws, tune, s) : run<4, __half, MODE>(c, n0, a.N, ws, tune, s))
+                               : (a.bf16 ? run<3, __nv_bfloat16, MODE>(c, n0, a.N, ws, tune, s) : run<3, __half, MODE>(c, n0, a.N, ws, tune, s));
+        };
+        e = a.gate < 0 ? go(std::integral_constant<int, kLinear>{}) : a.kept ? go(std::integral_constant<int, kKept>{}) : go(std::integral_constant<int, kGated>{});
+        if (e == cudaSuccess) ++*launches;
+    }
+    return e;
+}
+
+bool grad_supported(int M, int N, int K, int group, int rank)
+{
+    return group == kGroupFast && K % kGroupFast == 0 && N % 8 == 0 && rank % 8 == 0 && rank <= kMaxRank && M <= (1 << 22) && launch_columns(N, K) > 0;
+}
+
+void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags)
+{
+    const size_t cols = launch_columns(a.N, a.K), nft = (cols + kFeat - 1) / kFeat, nkc = (a.N + kItemK - 1) / kItemK;
+    *w16_bytes = a.dx ? (size_t)a.N * cols * 2 : 16;
+    *tags = kTagFirst + nft * nkc * kUnits + 2 * ((size_t)(a.M + kTTok - 1) / kTTok) + 32;
+}
+
+cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches)
+{
+    const int cols = a.dx ? launch_columns(a.N, a.K) : a.K;
+    cudaError_t e = cudaSuccess;
+    for (int k = 0; k < a.K && e == cudaSuccess; k += cols) {             // (each makes s anew: rank of `cols` of its operations)
+        const int n = std::min(cols, a.K - k);
+        e = a.bits == 4 ? (a.bf16 ? run_grad<4, __nv_bfloat16>(a, k, n, k == 0, ws, tune, s) : run_grad<4, __half>(a, k, n, k == 0, ws, tune, s))
+                        : (a.bf16 ? run_grad<3, __nv_bfloat16>(a, k, n, k == 0, ws, tune, s) : run_grad<3, __half>(a, k, n, k == 0, ws, tune, s));
         if (e == cudaSuccess) ++*launches;
     }
     return e;

@@ -35,6 +35,7 @@
 #include <type_traits>
 
 #include "fbq_common.cuh"
+#include "fbq_gate.cuh"
 #include "fbq_maps.h"
 #include "fbq_ptx.cuh"
 
@@ -72,6 +73,7 @@ struct GemvParams {
     int *ctr;           // [1] main CTAs that have read t; zero on entry and exit
     int *status;        // receives FBQ_ERR_TIMEOUT when a bounded wait runs out
     int M, N, K, G, rank;
+    int gate;           // the gate of a gated layer
     int NT;             // tiles
     int n_t, n_main;
     int t_kb;           // blocks of kTKB input channels per t CTA
@@ -663,7 +665,7 @@ __device__ __forceinline__ bool look_slots(const uint32_t *tpart, size_t slot_el
     return mn != 0u;
 }
 
-template <typename T, bool RANKED>
+template <typename T, bool RANKED, bool GATED>
 __device__ __forceinline__ bool epilogue(const GemvParams &p, uint8_t *smem, const CUtensorMap *bmap, int lane, int tile_first, int ntile, int cta)
 {
     const int g = lane >> 2, tq = lane & 3;
@@ -857,7 +859,10 @@ __device__ __forceinline__ bool epilogue(const GemvParams &p, uint8_t *smem, con
             vh = fmaf(sb.y, isc, vh);
         }
         const int n = (tile_first + ts) * kTile + g;
-        if (tq < M) {
+        if constexpr (GATED) {
+            // rows g and g + 8 of the tile: a row of the gate and the one of the up projection that it meets
+            if (tq < M) y[(size_t)tq * (p.N >> 1) + (tile_first + ts) * (kTile / 2) + g] = ActTraits<T>::from_float(gate_value(p.gate, vg) * vh);
+        } else if (tq < M) {
             if (n < p.N) y[(size_t)tq * p.N + n] = ActTraits<T>::from_float(vg);
             if (n + 8 < p.N) y[(size_t)tq * p.N + n + 8] = ActTraits<T>::from_float(vh);
         }
@@ -1032,7 +1037,7 @@ __device__ __forceinline__ void t_cta(const GemvParams &p, uint8_t *smem, const 
 
 // ------------------------------------------------------------------------ kernel
 // Block `block` (t CTAs first, then main CTAs) of one problem, integer form.
-template <int BITS, typename T, int M, bool RANKED>
+template <int BITS, typename T, int M, bool RANKED, bool GATED = false>
 __device__ __forceinline__ void gemv_body(const GemvParams &p, const CUtensorMap *wmap, const CUtensorMap *bmap, const CUtensorMap *amap, int block)
 {
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -1073,7 +1078,7 @@ __device__ __forceinline__ void gemv_body(const GemvParams &p, const CUtensorMap
     if (warp == kProdWarp) {
         if (lane == 0) ok = produce(p, smem, wmap, tile_first, ntile);
     } else if (warp == kEpiWarp) {
-        ok = epilogue<T, RANKED>(p, smem, bmap, lane, tile_first, ntile, cta);
+        ok = epilogue<T, RANKED, GATED>(p, smem, bmap, lane, tile_first, ntile, cta);
     } else {
         pdl_wait();                                  // x may come from the preceding kernel
         mark(p, 2);
@@ -1084,12 +1089,12 @@ __device__ __forceinline__ void gemv_body(const GemvParams &p, const CUtensorMap
     }
     if (!ok && lane == 0) give_up(p);
 }
-template <int BITS, typename T, int M, bool RANKED>
+template <int BITS, typename T, int M, bool RANKED, bool GATED>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 gemv_kernel(const GemvParams p, const __grid_constant__ CUtensorMap wmap,
             const __grid_constant__ CUtensorMap bmap, const __grid_constant__ CUtensorMap amap)
 {
-    gemv_body<BITS, T, M, RANKED>(p, &wmap, &bmap, &amap, (int)blockIdx.x);
+    gemv_body<BITS, T, M, RANKED, GATED>(p, &wmap, &bmap, &amap, (int)blockIdx.x);
 }
 
 // Several problems in one launch: t CTAs of all of them, then the main CTAs.
@@ -1290,11 +1295,11 @@ const Plan &plan_for(const LinearArgs &a, const GemvTuning &tune)
     return e.plan;
 }
 
-template <int BITS, typename T, int M, bool RANKED>
+template <int BITS, typename T, int M, bool RANKED, bool GATED>
 cudaError_t launch_variant(const Plan &pl, const CUtensorMap &wmap, const CUtensorMap &bmap, const CUtensorMap &amap, bool pdl,
                            cudaStream_t s)
 {
-    auto kern = gemv_kernel<BITS, T, M, RANKED>;
+    auto kern = gemv_kernel<BITS, T, M, RANKED, GATED>;
     static bool attr_set = false;
     if (!attr_set) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
@@ -1501,6 +1506,7 @@ cudaError_t launch_gemv(const LinearArgs &a, Workspace &ws, const GemvTuning &tu
     if (!pl.ok) return cudaErrorInvalidConfiguration;
     GemvParams &p = pl.p;
     p.x = a.x; p.scales = a.scales; p.zeros = a.zeros; p.y = a.y;
+    p.gate = a.gate;
     p.tpart = reinterpret_cast<uint32_t *>(ws.tslots);
     p.ctr = ws.counters;
     p.status = ws.counters + kCtrStatus;
@@ -1518,9 +1524,13 @@ cudaError_t launch_gemv(const LinearArgs &a, Workspace &ws, const GemvTuning &tu
     auto go = [&](auto bits, auto type) {
         using T = typename decltype(type)::type;
         constexpr int B = decltype(bits)::value;
-        if (a.rank == 0)
-            return a.M == 1 ? launch_variant<B, T, 1, false>(pl, wmap, bmap, amap, pdl, s) : launch_variant<B, T, 2, false>(pl, wmap, bmap, amap, pdl, s);
-        return a.M == 1 ? launch_variant<B, T, 1, true>(pl, wmap, bmap, amap, pdl, s) : launch_variant<B, T, 2, true>(pl, wmap, bmap, amap, pdl, s);
+        auto by_size = [&](auto gated) {
+            constexpr bool GT = decltype(gated)::value;
+            if (a.rank == 0)
+                return a.M == 1 ? launch_variant<B, T, 1, false, GT>(pl, wmap, bmap, amap, pdl, s) : launch_variant<B, T, 2, false, GT>(pl, wmap, bmap, amap, pdl, s);
+            return a.M == 1 ? launch_variant<B, T, 1, true, GT>(pl, wmap, bmap, amap, pdl, s) : launch_variant<B, T, 2, true, GT>(pl, wmap, bmap, amap, pdl, s);
+        };
+        return a.gate < 0 ? by_size(std::false_type{}) : by_size(std::true_type{});
     };
     if (a.bits == 4)
         e = a.bf16 ? go(std::integral_constant<int, 4>{}, TypeTag<__nv_bfloat16>{}) : go(std::integral_constant<int, 4>{}, TypeTag<__half>{});

@@ -52,6 +52,7 @@
 
 #include "fbq_common.cuh"
 #include "fbq_dequant.cuh"
+#include "fbq_gate.cuh"
 #include "fbq_maps.h"
 #include "fbq_umma.cuh"
 
@@ -96,6 +97,7 @@ struct PrefillParams {
     void *t16;                // [M][rank_pad] t rounded to the activation type, written by the t CTAs and read by the main
                               // CTAs' TMA copies as one more token operand (NULL: t32 and the producers' conversion)
     int rank_pad;             // columns of t16: rank rounded up to whole K blocks of 64 (the padding is zero)
+    int gate;                 // the gate of a gated layer
 };
 
 // ---------------------------------------------------------------- PTX helpers of this file
@@ -163,7 +165,7 @@ template <int TOK> struct Smem {
 // bmap: B [N][rank], boxes of 128 rows x 64 elements, 128-byte swizzle (main CTAs, rank > 0)
 // ymap: y [M][N], boxes of TOK/4 rows x 128 elements, no swizzle (stores)
 // tmap: t16 [M][rank_pad], boxes like xmap's (main CTAs, rank > 0, one K split of t)
-template <int BITS, typename T, int TOK>
+template <int BITS, typename T, int TOK, bool GATED>
 __global__ void __launch_bounds__(kPfThreads, 1)
 prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
                const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
@@ -172,6 +174,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
     using L = Smem<TOK>;
     constexpr uint32_t kXBytes = L::kXBytes, kStageBytes = L::kStageBytes;
     constexpr int WPG = (BITS == 4) ? 16 : 12;                  // packed words per row and group
+    constexpr uint32_t kOutRow = GATED ? kBN : kBN * 2;         // bytes of a token in the staged tile (gated: half as many columns)
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     if (sbase & 1023u) {                                        // swizzle atoms need a 1024-byte aligned base
@@ -445,7 +448,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
                     mbar_arrive(split_bar2);
                 }
                 const bool last = wait_looks(split_bar2, 0) && *split_last != 0;
-                if (last && mine) {
+                bool add = last && mine;
+                if constexpr (GATED) add = __all_sync(0xffffffffu, add);     // (the lanes swap values below)
+                if (add) {
                     __threadfence();
                     float acc[32];
 #pragma unroll
@@ -459,16 +464,22 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
 #pragma unroll
                         for (int j = 0; j < 32; ++j) acc[j] += u[j];
                     }
-                    unsigned short *sp16 = reinterpret_cast<unsigned short *>(smem + (size_t)c_begin * (kBN * 2)) + 32 * q + lane;
+                    if constexpr (GATED) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) sp16[j * kBN] = to_bits16<T>(acc[j]);
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(acc[j]);
+                        gate_chunk<T>(p.gate, v, reinterpret_cast<T *>(smem + (size_t)c_begin * kOutRow) + 16 * q);
+                    } else {
+                        unsigned short *sp16 = reinterpret_cast<unsigned short *>(smem + (size_t)c_begin * (kBN * 2)) + 32 * q + lane;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sp16[j * kBN] = to_bits16<T>(acc[j]);
+                    }
                     fence_proxy_async();                 // staged tile -> visible to the TMA store
                     mbar_arrive(epi0 + 8u * cg);
                     if (q == 0 && lane == 0) {
                         if (wait_looks(epi0 + 8u * cg, 0)) {
                             asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-                                         ::"l"(reinterpret_cast<uint64_t>(&ymap)), "r"(n0), "r"(m0 + c_begin),
-                                           "r"(sbase + (uint32_t)c_begin * (kBN * 2))
+                                         ::"l"(reinterpret_cast<uint64_t>(&ymap)), "r"(GATED ? n0 / 2 : n0), "r"(m0 + c_begin),
+                                           "r"(sbase + (uint32_t)c_begin * kOutRow)
                                          : "memory");
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
@@ -485,9 +496,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
                     umma::ld32(tmem_base + ((uint32_t)(32 * q) << 16) + (uint32_t)c, v);
                     umma::wait_ld();
                     if (!t_role) {
-                        unsigned short *sp = reinterpret_cast<unsigned short *>(smem + (size_t)c * (kBN * 2)) + 32 * q + lane;
+                        if constexpr (GATED) {
+                            gate_chunk<T>(p.gate, v, reinterpret_cast<T *>(smem + (size_t)c * kOutRow) + 16 * q);
+                        } else {
+                            unsigned short *sp = reinterpret_cast<unsigned short *>(smem + (size_t)c * (kBN * 2)) + 32 * q + lane;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) sp[j * kBN] = to_bits16<T>(__uint_as_float(v[j]));
+                            for (int j = 0; j < 32; ++j) sp[j * kBN] = to_bits16<T>(__uint_as_float(v[j]));
+                        }
                     } else if (p.t16) {
                         if (nn < p.rank_pad) {               // rounded once, here; rows of A beyond the rank are zero fill
                             unsigned short *tp = static_cast<unsigned short *>(p.t16) + (size_t)(m0 + c) * p.rank_pad + nn;
@@ -510,8 +525,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
                     if (q == 0 && lane == 0) {
                         if (wait_looks(epi0 + 8u * cg, 0)) {
                             asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-                                         ::"l"(reinterpret_cast<uint64_t>(&ymap)), "r"(n0), "r"(m0 + c_begin),
-                                           "r"(sbase + (uint32_t)c_begin * (kBN * 2))
+                                         ::"l"(reinterpret_cast<uint64_t>(&ymap)), "r"(GATED ? n0 / 2 : n0), "r"(m0 + c_begin),
+                                           "r"(sbase + (uint32_t)c_begin * kOutRow)
                                          : "memory");
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // smem may go once it has been read
@@ -1201,11 +1216,11 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_const
 
 int g_pf_pdl = 1;             // launch with programmatic stream serialisation (prefill_set_pdl)
 
-template <int BITS, typename T, int TOK>
+template <int BITS, typename T, int TOK, bool GATED>
 cudaError_t launch_kernel(const CUtensorMap &xmap, const CUtensorMap &wmap, const CUtensorMap &amap, const CUtensorMap &bmap,
                           const CUtensorMap &ymap, const CUtensorMap &tmap, const PrefillParams &p, unsigned grid, cudaStream_t s)
 {
-    auto kern = prefill_kernel<BITS, T, TOK>;
+    auto kern = prefill_kernel<BITS, T, TOK, GATED>;
     static bool attr_set = false;
     if (!attr_set) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<TOK>::kTotal);
@@ -1322,7 +1337,9 @@ cudaError_t run_prefill(const LinearArgs &a, Workspace &ws, cudaStream_t s, int 
     if ((e = make_map(&qmap, a.qw, true, (size_t)(a.K / kGroupFast) * wpg, (size_t)a.N, wpg, kBN,
                       a.bits == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, true)) != cudaSuccess)
         return e;
-    if ((e = make_map(&ymap, a.y, false, (size_t)a.N, (size_t)a.M, kBN, TOK / 4, CU_TENSOR_MAP_SWIZZLE_NONE, false)) != cudaSuccess) return e;
+    const int half = a.gate < 0 ? 1 : 2;
+    if ((e = make_map(&ymap, a.y, false, (size_t)a.N / half, (size_t)a.M, kBN / half, TOK / 4, CU_TENSOR_MAP_SWIZZLE_NONE, false)) != cudaSuccess) return e;
+    p.gate = a.gate;
     amap = bmap = xmap;
     CUtensorMap tmap = xmap;
     p.t16 = nullptr;
@@ -1340,9 +1357,12 @@ cudaError_t run_prefill(const LinearArgs &a, Workspace &ws, cudaStream_t s, int 
     if (PAIR)
         e = (a.bits == 4) ? launch_pair_kernel<4, T>(xmap, qmap, amap, bmap, ymap, p, grid, s)
                           : launch_pair_kernel<3, T>(xmap, qmap, amap, bmap, ymap, p, grid, s);
+    else if (a.gate < 0)
+        e = (a.bits == 4) ? launch_kernel<4, T, TOK, false>(xmap, qmap, amap, bmap, ymap, tmap, p, grid, s)
+                          : launch_kernel<3, T, TOK, false>(xmap, qmap, amap, bmap, ymap, tmap, p, grid, s);
     else
-        e = (a.bits == 4) ? launch_kernel<4, T, TOK>(xmap, qmap, amap, bmap, ymap, tmap, p, grid, s)
-                          : launch_kernel<3, T, TOK>(xmap, qmap, amap, bmap, ymap, tmap, p, grid, s);
+        e = (a.bits == 4) ? launch_kernel<4, T, TOK, true>(xmap, qmap, amap, bmap, ymap, tmap, p, grid, s)
+                          : launch_kernel<3, T, TOK, true>(xmap, qmap, amap, bmap, ymap, tmap, p, grid, s);
     if (e == cudaSuccess) ++*launches;
     return e;
 }
@@ -1397,7 +1417,7 @@ cudaError_t launch_prefill(const LinearArgs &a, bool dense, Workspace &ws, cudaS
     }
     if (a.M <= 128)
         return a.bf16 ? run_prefill<__nv_bfloat16, 128, false>(a, ws, s, launches) : run_prefill<__half, 128, false>(a, ws, s, launches);
-    if (g_pair)
+    if (g_pair && a.gate < 0)
         return a.bf16 ? run_prefill<__nv_bfloat16, 256, true>(a, ws, s, launches) : run_prefill<__half, 256, true>(a, ws, s, launches);
     return a.bf16 ? run_prefill<__nv_bfloat16, 256, false>(a, ws, s, launches) : run_prefill<__half, 256, false>(a, ws, s, launches);
 }

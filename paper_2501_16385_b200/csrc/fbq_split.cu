@@ -37,6 +37,7 @@
 #include <unordered_map>
 
 #include "fbq_common.cuh"
+#include "fbq_gate.cuh"
 #include "fbq_ptx.cuh"
 #include "fbq_unpack16.cuh"
 
@@ -73,7 +74,7 @@ struct alignas(16) SplitDims {
     int off_px, off_sc, off_b, off_recv, off_t, off_ring, off_trecv, off_tring, tstages;
 };
 struct SplitParams {
-    int n, M, cs_log2, n_tc, poll_limit, skip_t;
+    int n, M, cs_log2, n_tc, poll_limit, skip_t, gate;
     int first_tc[kMostProblems], first_mc[kMostProblems];
     int *status;
     unsigned long long *epoch;               // 2^32 x the number of launches so far, plus the CTAs of this one that are through
@@ -448,7 +449,7 @@ __device__ __forceinline__ void t_program(const SplitParams &sp, const SplitDims
 }
 
 // Returns whether one of this thread's sums is not finite.
-template <int BITS, typename T, int MT>
+template <int BITS, typename T, int MT, bool GATED>
 __device__ __forceinline__ bool main_program(const SplitParams &sp, const SplitDims &p, uint8_t *smem, int lc, int crank, int g0, int Gs)
 {
     constexpr int GB = BITS == 4 ? 64 : 48, kUnits = GB / 16;                 // bytes of a row and group, 16-byte units
@@ -659,11 +660,20 @@ __device__ __forceinline__ bool main_program(const SplitParams &sp, const SplitD
             // rows in order through shared memory (the place of this warp's own sums of the granule), whole 16 bytes per store
             T *ybuf = reinterpret_cast<T *>(rbase + ((((size_t)s << (cs_log2 + wkl)) * MT + b) << 9));
             __syncwarp();
+            if constexpr (GATED) {
+                // rows g and g + 8 of the granule: a row of the gate and the one of the up projection that it meets
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ybuf[(2 * t + (c & 1)) * 16 + g + 8 * (c >> 1)] = ActTraits<T>::from_float(fmaf(m4[c], 1.f / kScaled, sum[c]));
-            __syncwarp();
-            const int m = 8 * b + (lane >> 1), n = row0 + 8 * (lane & 1);
-            if (lane < 16 && m < M && n < N) *reinterpret_cast<uint4 *>(y + (size_t)m * N + n) = *reinterpret_cast<const uint4 *>(ybuf + lane * 8);
+                for (int c = 0; c < 2; ++c)
+                    ybuf[(2 * t + c) * 8 + g] = ActTraits<T>::from_float(gate_value(sp.gate, fmaf(m4[c], 1.f / kScaled, sum[c])) * fmaf(m4[c + 2], 1.f / kScaled, sum[c + 2]));
+                __syncwarp();
+                if (lane < 8 && 8 * b + lane < M) *reinterpret_cast<uint4 *>(y + (size_t)(8 * b + lane) * (N >> 1) + (row0 >> 1)) = *reinterpret_cast<const uint4 *>(ybuf + lane * 8);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) ybuf[(2 * t + (c & 1)) * 16 + g + 8 * (c >> 1)] = ActTraits<T>::from_float(fmaf(m4[c], 1.f / kScaled, sum[c]));
+                __syncwarp();
+                const int m = 8 * b + (lane >> 1), n = row0 + 8 * (lane & 1);
+                if (lane < 16 && m < M && n < N) *reinterpret_cast<uint4 *>(y + (size_t)m * N + n) = *reinterpret_cast<const uint4 *>(ybuf + lane * 8);
+            }
         }
         // Nobody goes on before all sums have arrived: a CTA that left earlier (rows past N, say) would take its shared memory from
         // under stores that are still on their way.
@@ -752,16 +762,13 @@ __device__ __forceinline__ bool main_program(const SplitParams &sp, const SplitD
 // both infinite and their difference is NaN, where a weight times x is infinite; the largest x of bf16 overflow in P alone.
 // (What it costs launches that need none of it: 32 x 7 linears of a 7B model, 8 tokens, bf16, 2121 -> 2175 us, 13B layer, 16 tokens, fp16,
 // 101.4 -> 101.7; with this in `finish`, where a sum turns out so, 2198 and 103.8.)
-template <int BITS, typename T>
-__device__ __noinline__ void redo_rows(const SplitDims &p, const uint8_t *smem, int M, int lc, int crank, int cs_log2)
+template <int BITS, typename T, bool GATED>
+__device__ __noinline__ void redo_rows(const SplitDims &p, const uint8_t *smem, int M, int lc, int crank, int cs_log2, int gate)
 {
     constexpr int NW = BITS == 4 ? 4 : 3;
     const int nrow0 = lc * p.R * kRows, ngran = 2 * min(p.R, p.tiles - lc * p.R);
     T *y = static_cast<T *>(p.y);
-#pragma unroll 1
-    for (int e = threadIdx.x; e < 16 * M * owned(ngran, cs_log2, crank); e += kThr) {
-        const int slot = e / (16 * M), token = e / 16 % M, row = nrow0 + ((slot << cs_log2) + crank) * 16 + e % 16;
-        if (row >= p.N || fabsf(ActTraits<T>::to_float(y[(size_t)token * p.N + row])) <= FLT_MAX) continue;
+    auto product = [&](int slot, int token, int row) {
         const uint32_t *w = reinterpret_cast<const uint32_t *>(p.qw) + (size_t)row * p.G * 4 * NW;
         const unsigned short *x = static_cast<const unsigned short *>(p.x) + (size_t)token * p.K;
         float sum = 0.f, sub = 0.f;
@@ -781,15 +788,24 @@ __device__ __noinline__ void redo_rows(const SplitDims &p, const uint8_t *smem, 
                 sum = fmaf(s * ((q.y - Unpack16<BITS, T>::kMagic) * down - z), ActTraits<T>::to_float(*reinterpret_cast<const T *>(&x1)), sum);
             }
         }
-        const T *b = reinterpret_cast<const T *>(smem + p.off_b + (slot * 16 + e % 16) * (p.rank * 2 + 16));
+        const T *b = reinterpret_cast<const T *>(smem + p.off_b + (slot * 16 + row % 16) * (p.rank * 2 + 16));
         const float *t = reinterpret_cast<const float *>(smem + p.off_t) + token * (p.rank + 16);
 #pragma unroll 1
         for (int j = 0; j < p.rank; ++j) sub = fmaf(t[j], ActTraits<T>::to_float(b[j]), sub);
-        y[(size_t)token * p.N + row] = ActTraits<T>::from_float(sum + sub);
+        return sum + sub;
+    };
+    constexpr int each = GATED ? 8 : 16;                                      // outputs of a granule
+#pragma unroll 1
+    for (int e = threadIdx.x; e < each * M * owned(ngran, cs_log2, crank); e += kThr) {
+        const int slot = e / (each * M), token = e / each % M, row = nrow0 + ((slot << cs_log2) + crank) * 16 + e % each;
+        T *out = GATED ? y + (size_t)token * (p.N >> 1) + (row >> 4) * 8 + (row & 7) : y + (size_t)token * p.N + row;
+        if (row >= p.N || fabsf(ActTraits<T>::to_float(*out)) <= FLT_MAX) continue;
+        if constexpr (GATED) *out = ActTraits<T>::from_float(gate_value(gate, product(slot, token, row)) * product(slot, token, row + 8));
+        else *out = ActTraits<T>::from_float(product(slot, token, row));
     }
 }
 
-template <int BITS, typename T, int MT>
+template <int BITS, typename T, int MT, bool GATED>
 __global__ void __launch_bounds__(kThr, 1) split_kernel(const __grid_constant__ SplitParams sp)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -819,8 +835,8 @@ __global__ void __launch_bounds__(kThr, 1) split_kernel(const __grid_constant__ 
         t_program<T, MT>(sp, p, smem, lc, crank, g0, Gs);
         __syncthreads();
     } else {
-        if (__syncthreads_or(main_program<BITS, T, MT>(sp, p, smem, cluster - p.first_mc, crank, g0, Gs)))
-            redo_rows<BITS, T>(p, smem, sp.M, cluster - p.first_mc, crank, sp.cs_log2);
+        if (__syncthreads_or(main_program<BITS, T, MT, GATED>(sp, p, smem, cluster - p.first_mc, crank, g0, Gs)))
+            redo_rows<BITS, T, GATED>(p, smem, sp.M, cluster - p.first_mc, crank, sp.cs_log2, sp.gate);
     }
     // Every CTA read the launch's number before this; with the last one the count of launches goes up by one.  (The CTAs that are
     // through have 32 bits: grids of wide layers, 4096 -> 8 000 000, say, hold more than 65536 CTAs.)
@@ -1075,9 +1091,9 @@ const Shape &shape_for(const LinearArgs *a, int count, int max_ctas)          //
     return plans.emplace(k, max_ctas > 0 ? make_bounded_shape(a[0], max_ctas) : make_shape(a, count)).first->second;
 }
 
-template <int BITS, typename T, int MT> cudaError_t launch_one(const Shape &s, bool pdl, cudaStream_t st)
+template <int BITS, typename T, int MT, bool GATED> cudaError_t launch_one(const Shape &s, bool pdl, cudaStream_t st)
 {
-    auto kern = split_kernel<BITS, T, MT>;
+    auto kern = split_kernel<BITS, T, MT, GATED>;
     static bool attr_set = false;
     if (!attr_set) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemAll);
@@ -1110,7 +1126,8 @@ template <int BITS, typename T, int MT> cudaError_t launch_one(const Shape &s, b
 
 template <int BITS, typename T> cudaError_t launch_mt(const Shape &s, bool pdl, cudaStream_t st)
 {
-    return s.sp.M <= 8 ? launch_one<BITS, T, 1>(s, pdl, st) : launch_one<BITS, T, 2>(s, pdl, st);
+    if (s.sp.gate >= 0) return s.sp.M <= 8 ? launch_one<BITS, T, 1, true>(s, pdl, st) : launch_one<BITS, T, 2, true>(s, pdl, st);
+    return s.sp.M <= 8 ? launch_one<BITS, T, 1, false>(s, pdl, st) : launch_one<BITS, T, 2, false>(s, pdl, st);
 }
 size_t t_words(const LinearArgs &a) { return ((size_t)a.M * a.rank + 15) / 16 * 16; }
 
@@ -1148,6 +1165,7 @@ cudaError_t launch_split(const LinearArgs *a, int count, Workspace &ws, const Ge
     Shape s = shape_for(a, count, tune.max_ctas);
     s.sp.poll_limit = tune.poll_limit;
     s.sp.skip_t = tune.test_skip_arrive;
+    s.sp.gate = a[0].gate;
     s.sp.status = ws.counters + kCtrStatus;
     s.sp.epoch = reinterpret_cast<unsigned long long *>(ws.split);
     size_t words = 16;

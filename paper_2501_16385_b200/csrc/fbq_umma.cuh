@@ -15,6 +15,14 @@ __device__ __forceinline__ uint64_t desc_k128(uint32_t smem_addr)
 {
     return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (1ull << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
+// The same for a tile whose rows run along the contraction (MN-major): a box of 64 elements of the other dimension x 64 of the
+// contraction, rows of 128 bytes in the 128-byte swizzle.  Eight of the contraction are 1024 bytes, further elements of the other
+// dimension are in further boxes of `box` bytes; 16 of the contraction on is 2048 bytes on.
+__device__ __forceinline__ uint64_t desc_mn128(uint32_t smem_addr, uint32_t box)
+{
+    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | ((uint64_t)(box >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+constexpr uint32_t kIdescMnA = 1u << 15, kIdescMnB = 1u << 16;          // operand A, B is MN-major
 // Instruction descriptor of kind::f16: fp32 accumulators, both operands of format `fmt` (0 fp16, 1 bf16), K-major.
 __device__ __host__ constexpr uint32_t idesc_f16(uint32_t fmt, uint32_t m, uint32_t n)
 {
