@@ -242,7 +242,6 @@ def reconstruct_step(W, H, A, B, lr: float, group: int, bits: int, workspace=Non
 
 
 GATES = {"silu": 0, "gelu": 1}
-KEPT_GROUP = 128
 
 
 def _operand(t, shape, dtype, device, what):
@@ -312,96 +311,50 @@ def gated_layer(gate, up, group: int, bits: int, stream=None):
 def gated(x, qweight, scales, zeros, A, B, N: int, group: int, bits: int, fn: str = "silu", save: bool = False, h=None, stream=None):
     """fbq_gated: h [M, N/2] of a gated layer of N rows, fn "silu" or "gelu".  With save returns (h, codes, scales): the layer's
     products in 8 bits, for gated_backward."""
-    import torch
-    gate, dev, bf16 = _gate(fn), _current_device(), _act_type(x, "x")
-    M, K = x.shape
-    _operand(x, (M, K), x.dtype, dev, "x")
-    rank = _layer_operands(qweight, scales, zeros, A, B, N, K, group, bits, x.dtype, dev)
-    if h is None:
-        h = torch.empty((M, N // 2), dtype=x.dtype, device=dev)
-    else:
-        _operand(h, (M, N // 2), x.dtype, dev, "h")
-    codes = torch.empty((M, N), dtype=torch.int8, device=dev) if save else None
-    kept = torch.empty((M, -(-N // KEPT_GROUP)), dtype=torch.float32, device=dev) if save else None
-    _check(lib().fbq_gated(_ptr(x), _ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(A), _ptr(B), _ptr(h), _ptr(codes), _ptr(kept), M, N, K, group, bits, rank,
-                           gate, bf16, _stream(stream)), "fbq_gated")
-    return (h, codes, kept) if save else h
+    r = (_native or native()).gated(x, qweight, scales, zeros, A, B, N, group, bits, _gate(fn), save, h, stream)
+    if r.__class__ is int:
+        raise FbqError(r, "fbq_gated")
+    return r
 
 
 def act8_pack(x, stream=None):
     """fbq_act8_pack: x [M, K] fp16 or bf16 -> (codes int8 [M, K], scales float32 [M, ceil(K/128)])."""
-    import torch
-    bf16, dev = _act_type(x, "x"), _current_device()
-    M, K = x.shape
-    _operand(x, (M, K), x.dtype, dev, "x")
-    codes = torch.empty((M, K), dtype=torch.int8, device=dev)
-    scales = torch.empty((M, -(-K // KEPT_GROUP)), dtype=torch.float32, device=dev)
-    _check(lib().fbq_act8_pack(_ptr(x), _ptr(codes), _ptr(scales), M, K, bf16, _stream(stream)), "fbq_act8_pack")
-    return codes, scales
-
-
-def _kept_operands(codes, scales, shape, device, what):
-    import torch
-    _operand(codes, shape, torch.int8, device, what + " codes")
-    _operand(scales, (shape[0], -(-shape[1] // KEPT_GROUP)), torch.float32, device, what + " scales")
+    r = (_native or native()).act8_pack(x, stream)
+    if r.__class__ is int:
+        raise FbqError(r, "fbq_act8_pack")
+    return r
 
 
 def act8_unpack(codes, scales, dtype, stream=None):
     """fbq_act8_unpack: what act8_pack's codes stand for, as dtype (torch.float16 or torch.bfloat16)."""
-    import torch
-    dev = _current_device()
-    _kept_operands(codes, scales, codes.shape, dev, "kept")
-    x = torch.empty(codes.shape, dtype=dtype, device=dev)
-    _check(lib().fbq_act8_unpack(_ptr(codes), _ptr(scales), _ptr(x), codes.shape[0], codes.shape[1], _act_type(x, "dtype"), _stream(stream)), "fbq_act8_unpack")
-    return x
+    name = str(dtype)
+    if name not in ("torch.float16", "torch.bfloat16"):
+        raise TypeError("dtype must be torch.float16 or torch.bfloat16, got %s" % name)
+    r = (_native or native()).act8_unpack(codes, scales, name == "torch.bfloat16", stream)
+    if r.__class__ is int:
+        raise FbqError(r, "fbq_act8_unpack")
+    return r
 
 
-def _backward_operands(x, qweight, scales, zeros, A, B, M, N, K, group, bits, act, dev, want_dx, want_factors):
-    """Checks the operands that the two backward passes share; returns rank, the addresses of x, and the outputs."""
-    import torch
-    rank = _layer_operands(qweight, scales, zeros, A, B, N, K, group, bits, act, dev)
-    if isinstance(x, (tuple, list)):
-        codes, x_scales = x
-        _kept_operands(codes, x_scales, (M, K), dev, "x")
-        xs = (None, _ptr(codes), _ptr(x_scales))
-    elif x is not None:
-        _operand(x, (M, K), act, dev, "x")
-        xs = (_ptr(x), None, None)
-    else:
-        xs = (None, None, None)
-    dx = torch.empty((M, K), dtype=act, device=dev) if want_dx else None
-    dA = torch.empty((rank, K), dtype=act, device=dev) if want_factors and rank else None
-    dB = torch.empty((N, rank), dtype=act, device=dev) if want_factors and rank else None
-    return rank, xs, dx, dA, dB
+def _backward(where, gated, dy, kept, x, layer, group, bits, gate, want_dx, want_factors, stream):
+    x, x_scales = x if isinstance(x, (tuple, list)) else (x, None)
+    r = (_native or native()).backward(gated, dy, kept[0], kept[1], x, x_scales, *layer, group, bits, gate, want_dx, want_factors, stream)
+    if r.__class__ is int:
+        raise FbqError(r, where)
+    return r
 
 
 def linear_backward(dy, x, qweight, scales, zeros, A, B, group: int, bits: int, want_dx: bool = True, want_factors: bool = True, stream=None):
     """fbq_linear_backward: (dx, dA, dB) of a layer for dy [M, N].  x: [M, K] as in the forward pass, or (codes, scales) of
     act8_pack; None without want_factors.  What is not wanted, and the factors' gradients at rank 0, are None."""
-    dev, bf16 = _current_device(), _act_type(dy, "dy")
-    M, N = dy.shape
-    K = scales.shape[1] * group
-    _operand(dy, (M, N), dy.dtype, dev, "dy")
-    rank, xs, dx, dA, dB = _backward_operands(x, qweight, scales, zeros, A, B, M, N, K, group, bits, dy.dtype, dev, want_dx, want_factors)
-    _check(lib().fbq_linear_backward(_ptr(dy), *xs, _ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(A), _ptr(B), _ptr(dx), _ptr(dA), _ptr(dB), M, N, K, group, bits,
-                                     rank, bf16, _stream(stream)), "fbq_linear_backward")
-    return dx, dA, dB
+    return _backward("fbq_linear_backward", False, dy, (None, None), x, (qweight, scales, zeros, A, B), group, bits, 0, want_dx, want_factors, stream)
 
 
 def gated_backward(dh, kept, x, qweight, scales, zeros, A, B, group: int, bits: int, fn: str = "silu", want_dx: bool = True, want_factors: bool = True,
                    stream=None):
     """fbq_gated_backward: (dx, dA, dB) of a gated layer for dh [M, N/2]; kept: the (codes, scales) that gated(save=True)
     returned.  x and the results are as in linear_backward."""
-    gate, dev, bf16 = _gate(fn), _current_device(), _act_type(dh, "dh")
-    M, N = dh.shape[0], 2 * dh.shape[1]
-    K = scales.shape[1] * group
-    _operand(dh, (M, N // 2), dh.dtype, dev, "dh")
-    codes, kept_scales = kept
-    _kept_operands(codes, kept_scales, (M, N), dev, "kept")
-    rank, xs, dx, dA, dB = _backward_operands(x, qweight, scales, zeros, A, B, M, N, K, group, bits, dh.dtype, dev, want_dx, want_factors)
-    _check(lib().fbq_gated_backward(_ptr(dh), _ptr(codes), _ptr(kept_scales), *xs, _ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(A), _ptr(B), _ptr(dx), _ptr(dA),
-                                    _ptr(dB), M, N, K, group, bits, rank, gate, bf16, _stream(stream)), "fbq_gated_backward")
-    return dx, dA, dB
+    return _backward("fbq_gated_backward", True, dh, kept, x, (qweight, scales, zeros, A, B), group, bits, _gate(fn), want_dx, want_factors, stream)
 
 
 def make_batch(problems):

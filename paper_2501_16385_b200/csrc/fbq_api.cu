@@ -285,6 +285,47 @@ int gated_kernel(const LinearArgs &a)
     return g_opt.use_gemv && !a.kept && a.M <= kGemvMaxM && g_opt.force_kernel < 0 && gemv_supported(a) ? FBQ_KERNEL_DECODE : FBQ_KERNEL_PREFILL;
 }
 
+// Calls of few hundred tokens: weights dequantised where they are multiplied (fbq_even.cu), the sub-branch's thin products in a launch before.
+constexpr int kEvenMost = 512;
+bool even_takes(int M) { return M <= kEvenMost; }
+size_t padded256(size_t bytes) { return (bytes + 255) / 256 * 256; }
+size_t thin_bytes(int M, int rank) { return padded256((size_t)M * ((rank + 63) / 64 * 64) * 2); }
+PrefillTuning prefill_tuning()
+{
+    PrefillTuning t;
+    t.pdl = g_opt.decode.pdl;
+    t.flag_polls = g_opt.prefill_flag_polls;
+    t.test_skip_flag = g_opt.test_prefill_skip_flag;
+    return t;
+}
+
+int run_gated_even(const LinearArgs &a, Workspace *ws, cudaStream_t s)
+{
+    const size_t thin = thin_bytes(a.M, a.rank);
+    char *scratch = static_cast<char *>(ws->grad);
+    cudaError_t e = grow(scratch, ws->grad_bytes, thin + even_part_bytes(a.M, a.N, a.K), 1, s);
+    ws->grad = scratch;
+    if (e != cudaSuccess) return grow_status(e);
+    size_t have_c = (size_t)ws->n_counters;
+    if ((e = grow(ws->tags, ws->n_tags, even_tags(), sizeof(uint32_t), s)) != cudaSuccess) return grow_status(e);
+    if ((e = grow(ws->counters, have_c, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
+    ws->n_counters = (int)have_c;
+    int launches = 0;
+    if (a.rank > 0) {
+        ThinArgs t{};
+        t.x = a.x; t.A = a.A; t.t = scratch;
+        t.M = a.M; t.N = a.N; t.K = a.K; t.rank = a.rank; t.bf16 = a.bf16;
+        if (launch_thin(t, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+    }
+    EvenArgs v{};
+    v.x = a.x; v.qw = a.qw; v.scales = a.scales; v.zeros = a.zeros; v.factor = a.B; v.thin = scratch; v.y = a.y;
+    v.kept = a.kept; v.kept_scales = a.kept_scales; v.part = scratch + thin;
+    v.M = a.M; v.N = a.N; v.K = a.K; v.bits = a.bits; v.rank = a.rank; v.gate = a.gate; v.bf16 = a.bf16;
+    if (launch_even(v, *ws, prefill_tuning(), s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+    g_launches += launches;
+    return FBQ_OK;
+}
+
 // decode_ctas > 0 overrides the decode kernel's grid-size bound for this call.
 int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
 {
@@ -360,6 +401,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
             return FBQ_ERR_CUDA;
         }
     }
+    if (a.gate >= 0 && kernel == FBQ_KERNEL_PREFILL && even_takes(a.M)) return run_gated_even(a, ws, s);
     if (kernel == FBQ_KERNEL_PREFILL) {
         size_t have_c = (size_t)ws->n_counters, need_t = 0, need_p = 0;
         int need_c = 0;
@@ -425,12 +467,13 @@ int run_backward(Backward &b, cudaStream_t s)
     size_t need = 0;
     auto place = [&](size_t bytes) {
         const size_t at = need;
-        need += (bytes + 255) / 256 * 256;
+        need += padded256(bytes);
         return at;
     };
-    const size_t M = g.M, thin = M * ((g.rank + 63) / 64 * 64) * 2;
+    const bool even = even_takes(g.M);
+    const size_t M = g.M, thin = thin_bytes(g.M, g.rank);
     const size_t x_at = place(unpack ? M * g.K * 2 : 0), dy_at = place(b.kept ? M * g.N * 2 : 0), s_at = place(thin), t_at = place(factors ? thin : 0),
-                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0);
+                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
     cudaError_t e;
     size_t have_c = (size_t)ws->n_counters, need_w = 0, need_tags = 0;
     char *scratch = static_cast<char *>(ws->grad), *w16 = static_cast<char *>(ws->w16);
@@ -438,6 +481,10 @@ int run_backward(Backward &b, cudaStream_t s)
     ws->grad = scratch;
     if (e != cudaSuccess) return grow_status(e);
     grad_workspace_need(g, &need_w, &need_tags);
+    if (even) {
+        need_w = 0;
+        need_tags = even_tags();
+    }
     e = grow(w16, ws->w16_bytes, need_w, 1, s);
     ws->w16 = w16;
     if (e != cudaSuccess) return grow_status(e);
@@ -457,11 +504,22 @@ int run_backward(Backward &b, cudaStream_t s)
     }
     g.s16 = scratch + s_at;
     g.t16 = factors ? scratch + t_at : nullptr;
-    PrefillTuning tune;
-    tune.pdl = g_opt.decode.pdl;
-    tune.flag_polls = g_opt.prefill_flag_polls;
-    tune.test_skip_flag = g_opt.test_prefill_skip_flag;
-    if (launch_grad(g, *ws, tune, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (even) {
+        if (g.rank > 0) {
+            ThinArgs t{};
+            t.x = g.x; t.dy = g.dy; t.A = g.A; t.B = g.B; t.t = g.t16; t.s = g.s16;
+            t.M = g.M; t.N = g.N; t.K = g.K; t.rank = g.rank; t.bf16 = g.bf16;
+            if (launch_thin(t, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+        }
+        if (g.dx) {
+            EvenArgs v{};
+            v.x = g.dy; v.qw = g.qw; v.scales = g.scales; v.zeros = g.zeros; v.factor = g.A; v.thin = g.s16; v.y = g.dx; v.part = scratch + even_at;
+            v.M = g.M; v.N = g.N; v.K = g.K; v.bits = g.bits; v.rank = g.rank; v.gate = -1; v.bf16 = g.bf16;
+            if (launch_even(v, *ws, prefill_tuning(), s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+        }
+    } else if (launch_grad(g, *ws, prefill_tuning(), s, &launches) != cudaSuccess) {
+        return FBQ_ERR_CUDA;
+    }
     if (factors && launch_factor_grads(g.dy, g.x, g.s16, g.t16, b.dA, b.dB, g.M, g.N, g.K, g.rank, b.kept != nullptr, g.bf16, scratch + part_at,
                                        ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess)
         return FBQ_ERR_CUDA;

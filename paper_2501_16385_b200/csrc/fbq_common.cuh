@@ -164,6 +164,30 @@ struct GradArgs {
 bool grad_supported(int M, int N, int K, int group, int rank);
 void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags);
 cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);
+// The same for few hundred tokens, without a copy of the weights: t = x.A^T and s = dy.B (fbq_thin.cu; either may be left out), then dx, or h of a
+// gated layer (fbq_even.cu).
+struct ThinArgs {
+    const void *x, *dy, *A, *B;
+    void *t, *s;                  // [M][rank rounded up to 64] or none
+    int M, N, K, rank;
+    bool bf16;
+};
+cudaError_t launch_thin(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches);
+struct EvenArgs {
+    const void *x;                // x [M][K], or dy [M][N]
+    const uint32_t *qw;
+    const __half *scales, *zeros;
+    const void *factor, *thin;    // B and t, or A and s
+    void *y;                      // h [M][N / 2], or dx [M][K]
+    int8_t *kept;
+    float *kept_scales;
+    void *part;                   // even_part_bytes of scratch
+    int M, N, K, bits, rank, gate;        // gate < 0: dx
+    bool bf16;
+};
+size_t even_part_bytes(int M, int features, int depth);
+size_t even_tags();
+cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);
 size_t factor_grad_scratch_bytes(int M, int N, int K, int rank);
 cudaError_t launch_factor_grads(const void *dy, const void *x, const void *s16, const void *t16, void *dA, void *dB, int M, int N, int K, int rank, bool gated,
                                 bool bf16, void *scratch, int *status, bool pdl, cudaStream_t s, int *launches);

@@ -1,0 +1,225 @@
+// The sub-branch's thin products for few hundred tokens, sm_100a:  t = x.A^T  and  s = dy.B,  [M][rank], rounded once to the activation
+// type (they are tensor-core operands of the launch behind this one).
+//
+// Little arithmetic over long contractions, so what counts is how many SMs read: a cluster of CTAs takes a tile of tokens and up to 128
+// entries of the rank and cuts the contraction (tcgen05.mma, the rank's entries are the rows, tokens the columns; A is K-major, B as
+// it lies MN-major).  Each CTA puts its fp32 sums into its shared memory, and after one cluster barrier every CTA adds an equal share of the
+// tokens from all of them, in order, through distributed shared memory.
+#include <algorithm>
+
+#include "fbq_common.cuh"
+#include "fbq_dequant.cuh"
+#include "fbq_maps.h"
+#include "fbq_umma.cuh"
+
+namespace fbq {
+namespace {
+using namespace ptx;
+
+constexpr int kBK = 64, kRows = 128;
+constexpr int kMostTok = 128, kStages = 4, kMostCluster = 8;
+constexpr uint32_t kABytes = kRows * kBK * 2u, kBox = kABytes / 2;
+constexpr int kThreads = 192;
+constexpr uint32_t kSmem = kStages * (kABytes + kMostTok * kBK * 2u) + 1024;
+static_assert(kMostTok * kRows * 4u <= kStages * (kABytes + kMostTok * kBK * 2u), "the sums take the stages' place");
+
+struct ThinParams {
+    void *t, *s;              // [M][rank_pad]
+    int *status;
+    int M, rank_pad, a_rows;
+    int tok, ntt, nrt;        // tokens of a tile, tiles, tiles of the rank
+    int n_s;                  // clusters of s, before those of t
+    int blocks_t, blocks_s;   // of the contractions
+};
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// xmap: x [M][K], dymap: dy [M][N], boxes of tok rows x 64; amap: A [rank][K], boxes of a_rows x 64; bmap: B [N][rank], boxes of 64 x 64 (MN-major);
+// all in the 128-byte swizzle.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap dymap, const __grid_constant__ CUtensorMap amap,
+            const __grid_constant__ CUtensorMap bmap, const ThinParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kStages + 1];
+    __shared__ uint32_t tmem_slot;
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t sbase = smem_u32(smem), full0 = smem_u32(bars), empty0 = full0 + 8u * kStages, done = empty0 + 8u * kStages;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t cs, crank;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
+    crank = cluster_ctarank();
+    int cluster = (int)(blockIdx.x / cs);
+    const bool of_s = cluster < p.n_s;
+    if (!of_s) cluster -= p.n_s;
+    const int rt = cluster % p.nrt, m0 = cluster / p.nrt * p.tok, row0 = rt * kRows;
+    const int all = of_s ? p.blocks_s : p.blocks_t, b0 = (int)((long long)all * crank / cs), b1 = (int)((long long)all * (crank + 1) / cs);
+    const int boxes = min(2, (p.rank_pad - row0) / 64);
+    const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), stage_bytes = kABytes + xbytes, abytes = of_s ? (uint32_t)boxes * kBox : (uint32_t)p.a_rows * (kBK * 2u);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(full0 + 8u * i, 1);
+            mbar_init(empty0 + 8u * i, 1);
+        }
+        mbar_init(done, 1);
+        fence_barrier_init();
+        prefetch_tensormap(of_s ? &dymap : &xmap);
+        prefetch_tensormap(of_s ? &bmap : &amap);
+    }
+    if (warp == 1) umma::tmem_alloc<1>(smem_u32(&tmem_slot), 128u);
+    umma::fence_before();
+    __syncthreads();
+    umma::fence_after();
+    const uint32_t tmem = tmem_slot;
+    pdl_wait();
+    pdl_launch_dependents();
+    bool ok = true;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t s = 0, phase = 1u;
+#pragma unroll 1
+            for (int b = b0; b < b1; ++b) {
+                if (b - b0 >= kStages && !mbar_wait(empty0 + 8u * s, phase)) { ok = false; break; }
+                const uint32_t bar = full0 + 8u * s, dst = sbase + s * stage_bytes;
+                mbar_expect_tx(bar, abytes + xbytes);
+                if (of_s)
+                    for (int i = 0; i < boxes; ++i) tma_load_2d(dst + i * kBox, &bmap, row0 + 64 * i, b * kBK, bar);
+                else
+                    tma_load_2d(dst, &amap, b * kBK, row0, bar);
+                tma_load_2d(dst + kABytes, of_s ? &dymap : &xmap, b * kBK, m0, bar);
+                if (++s == kStages) { s = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kRows, (uint32_t)p.tok) | (of_s ? umma::kIdescMnA : 0u), astep = of_s ? 2048u >> 4 : 2u;
+            uint32_t s = 0, phase = 0;
+#pragma unroll 1
+            for (int b = b0; b < b1; ++b) {
+                if (!mbar_wait(full0 + 8u * s, phase)) { ok = false; break; }
+                umma::fence_after();
+                const uint32_t at = sbase + s * stage_bytes;
+                const uint64_t ad = of_s ? umma::desc_mn128(at, kBox) : umma::desc_k128(at), xd = umma::desc_k128(at + kABytes);
+#pragma unroll
+                for (int j = 0; j < kBK / 16; ++j) umma::mma(tmem, ad + astep * j, xd + 2 * j, idesc, b > b0 || j > 0);
+                umma::commit(empty0 + 8u * s);
+                if (++s == kStages) { s = 0; phase ^= 1u; }
+            }
+            if (ok) umma::commit(done);
+        }
+    } else {
+        // sums [token][rank entry] into shared memory, where the operands were
+        const int q = warp & 3, j = 32 * q + lane;
+        float *sums = reinterpret_cast<float *>(smem) + j;
+        ok = __all_sync(0xffffffffu, mbar_wait(done, 0u));       // (of no blocks the commit arrives at once)
+        if (ok) {
+            umma::fence_after();
+#pragma unroll 1
+            for (int c = 0; c < p.tok; c += 16) {
+                uint32_t v[16];
+                umma::ld16(tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)c, v);
+                umma::wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[(c + i) * kRows] = b1 > b0 ? __uint_as_float(v[i]) : 0.f;
+            }
+        }
+    }
+    if (!ok) {
+        atomicExch(p.status, (int)FBQ_ERR_TIMEOUT);
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);          // copies in flight land before the CTA leaves
+    }
+    umma::fence_before();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    const int width = min(kRows, p.rank_pad - row0);
+    unsigned short *out = static_cast<unsigned short *>(of_s ? p.s : p.t);
+    for (int e = threadIdx.x; e < p.tok * kRows; e += kThreads) {
+        const int c = e / kRows, j = e % kRows;
+        if (c % (int)cs != (int)crank || m0 + c >= p.M || j >= width) continue;
+        float v = 0.f;
+        for (uint32_t k = 0; k < cs; ++k) v += ld_cluster(mapa_shared(sbase + (uint32_t)e * 4u, k));
+        out[(size_t)(m0 + c) * p.rank_pad + row0 + j] = to_bits16<T>(v);
+    }
+    cluster_arrive();
+    cluster_wait();                                              // nobody reads this CTA's sums any more
+    if (warp == 1) {
+        umma::fence_after();
+        umma::tmem_free<1>(tmem, 128u);
+    }
+}
+
+template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
+{
+    const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+    ThinParams p{};
+    p.t = a.t; p.s = a.s; p.status = status;
+    p.M = a.M;
+    p.rank_pad = (a.rank + kBK - 1) / kBK * kBK;
+    p.a_rows = std::min(kRows, p.rank_pad);
+    p.nrt = (p.rank_pad + kRows - 1) / kRows;
+    p.blocks_t = a.t ? (a.K + kBK - 1) / kBK : 0;
+    p.blocks_s = a.s ? (a.N + kBK - 1) / kBK : 0;
+    const int kinds = (a.t ? 1 : 0) + (a.s ? 1 : 0), deep = std::max(p.blocks_t, p.blocks_s);
+    int cs = 1;
+    while (2 * cs <= std::min(kMostCluster, deep / 2)) cs *= 2;
+    // tiles of tokens: as many as clusters are resident at once (15 of eight CTAs), of 16 tokens at least
+    const int room = std::max(1, 120 / (cs * p.nrt * kinds));
+    p.tok = std::min(kMostTok, ((a.M + room - 1) / room + 15) / 16 * 16);
+    p.ntt = (a.M + p.tok - 1) / p.tok;
+    p.n_s = a.s ? p.ntt * p.nrt : 0;
+    const int clusters = p.n_s + (a.t ? p.ntt * p.nrt : 0);
+    CUtensorMap xmap, dymap, amap, bmap;
+    cudaError_t e;
+    if (a.t) {
+        if ((e = encode_map(&xmap, matrix_map(a.x, dt, 2, a.K, a.M, kBK, p.tok, sw))) != cudaSuccess) return e;
+        if ((e = cached_map(&amap, matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
+    }
+    if (a.s) {
+        if ((e = encode_map(&dymap, matrix_map(a.dy, dt, 2, a.N, a.M, kBK, p.tok, sw))) != cudaSuccess) return e;
+        if ((e = cached_map(&bmap, matrix_map(a.B, dt, 2, a.rank, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
+    }
+    if (!a.t) { xmap = dymap; amap = bmap; }
+    if (!a.s) { dymap = xmap; bmap = amap; }
+    auto kern = thin_kernel<T>;
+    static bool attr_set = false;
+    if (!attr_set) {
+        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem)) != cudaSuccess) return e;
+        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+        attr_set = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(clusters * cs));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cs;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = pdl ? 2 : 1;
+    if ((e = cudaLaunchKernelEx(&cfg, kern, xmap, dymap, amap, bmap, p)) == cudaSuccess) ++*launches;
+    return e;
+}
+
+}  // namespace
+
+cudaError_t launch_thin(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
+{
+    return a.bf16 ? run<__nv_bfloat16>(a, status, pdl, s, launches) : run<__half>(a, status, pdl, s, launches);
+}
+
+}  // namespace fbq

@@ -5,7 +5,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+
+#include <initializer_list>
+#include <sstream>
 
 #include "../../include/fbq.h"
 
@@ -124,7 +128,248 @@ PyObject *py_linear_batch(PyObject *, PyObject *const *v, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-PyMethodDef methods[] = {{"linear", (PyCFunction)(void (*)(void))py_linear, METH_FASTCALL, nullptr},
+// ---- the feed-forward block's calls: every tensor is checked, for what gets past here is an address ----
+struct BadOperand {};            // a Python exception is set
+
+const char *type_name(at::ScalarType t) { return at::toString(t); }
+
+// A contiguous tensor of the current device with the given type and shape; returns its address.
+void *operand(PyObject *o, const char *what, at::ScalarType type, at::IntArrayRef shape)
+{
+    if (!THPVariable_Check(o)) {
+        PyErr_Format(PyExc_TypeError, "%s must be a tensor", what);
+        throw BadOperand();
+    }
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.scalar_type() != type || t.sizes() != shape || !t.is_contiguous() || t.get_device() != c10::cuda::current_device()) {
+        std::ostringstream msg;
+        msg << what << " must be a contiguous " << type_name(type) << " tensor of shape " << shape << " on the current CUDA device, got " << type_name(t.scalar_type())
+            << " of shape " << t.sizes() << " on " << t.device() << (t.is_contiguous() ? "" : ", not contiguous");
+        PyErr_SetString(PyExc_ValueError, msg.str().c_str());
+        throw BadOperand();
+    }
+    return t.data_ptr();
+}
+const at::Tensor &tensor_of(PyObject *o, const char *what, int dims)
+{
+    if (!THPVariable_Check(o) || THPVariable_Unpack(o).dim() != dims) {
+        PyErr_Format(PyExc_TypeError, "%s must be a tensor of %d dimensions", what, dims);
+        throw BadOperand();
+    }
+    return THPVariable_Unpack(o);
+}
+at::ScalarType act_type(const at::Tensor &t, const char *what)
+{
+    const at::ScalarType s = t.scalar_type();
+    if (s != at::kHalf && s != at::kBFloat16) {
+        PyErr_Format(PyExc_TypeError, "%s must be float16 or bfloat16", what);
+        throw BadOperand();
+    }
+    return s;
+}
+[[noreturn]] void bad_value(const char *text)
+{
+    PyErr_SetString(PyExc_ValueError, text);
+    throw BadOperand();
+}
+int int_arg(PyObject *o)
+{
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) throw BadOperand();
+    if (v > 0x7FFFFFFF || v < -0x7FFFFFFFl) bad_value("a size does not fit 32 bits");
+    return (int)v;
+}
+int size_arg(int64_t n)
+{
+    if (n > 0x7FFFFFFF) bad_value("a size does not fit 31 bits");
+    return (int)n;
+}
+int64_t groups_of(int64_t columns) { return (columns + 127) / 128; }
+
+struct Layer {
+    void *q, *s, *z, *A = nullptr, *B = nullptr;
+    int rank = 0;
+};
+// v: qweight, scales, zeros, A, B
+Layer layer_of(PyObject *const *v, int64_t N, int64_t K, int group, int bits, at::ScalarType act)
+{
+    Layer l;
+    if (group < 1 || K % group != 0) bad_value("K is not a multiple of group");
+    const at::Tensor &q = THPVariable_Check(v[0]) ? THPVariable_Unpack(v[0]) : tensor_of(v[0], "qweight", 1);
+    if (q.numel() != (int64_t)fbq_packed_words(size_arg(N), size_arg(K), bits)) bad_value("qweight does not hold the packed words of this layer");
+    l.q = operand(v[0], "qweight", at::kInt, q.sizes());
+    l.s = operand(v[1], "scales", at::kHalf, {N, K / group});
+    l.z = operand(v[2], "zeros", at::kHalf, {N, K / group});
+    if ((v[3] == Py_None) != (v[4] == Py_None)) bad_value("A and B belong together");
+    if (v[3] != Py_None) {
+        const int64_t r = tensor_of(v[3], "A", 2).size(0);
+        l.A = operand(v[3], "A", act, {r, K});
+        l.B = operand(v[4], "B", act, {N, r});
+        l.rank = size_arg(r);
+    }
+    return l;
+}
+
+template <typename F> PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F f)
+{
+    if (n != want) {
+        PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+        return nullptr;
+    }
+    try {
+        return f();
+    } catch (const BadOperand &) {
+        return nullptr;
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+template <typename F> int without_gil(F f)
+{
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = f();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+void *stream_arg(PyObject *o)
+{
+    void *s;
+    if (!stream_of(o, &s)) throw BadOperand();
+    return s;
+}
+// New references of `t` (None where it is undefined), as a tuple; or the one alone.
+PyObject *results(std::initializer_list<at::Tensor> ts)
+{
+    PyObject *tuple = PyTuple_New((Py_ssize_t)ts.size());
+    if (!tuple) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor &t : ts) {
+        PyObject *o = t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None);
+        if (!o) {
+            Py_DECREF(tuple);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(tuple, i++, o);
+    }
+    return tuple;
+}
+
+// gated(x, qweight, scales, zeros, A, B, N, group, bits, gate, save, h, stream) -> h or (h, codes, scales), or the error code of the call
+PyObject *py_gated(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return guarded(n, 13, [&]() -> PyObject * {
+        const at::Tensor &x = tensor_of(v[0], "x", 2);
+        const at::ScalarType act = act_type(x, "x");
+        const int64_t M = x.size(0), K = x.size(1);
+        const int N = int_arg(v[6]), group = int_arg(v[7]), bits = int_arg(v[8]), gate = int_arg(v[9]);
+        const bool save = PyObject_IsTrue(v[10]) == 1;
+        if (N < 2) bad_value("N must be positive");
+        void *px = operand(v[0], "x", act, {M, K});
+        const Layer l = layer_of(v + 1, N, K, group, bits, act);
+        void *stream = stream_arg(v[12]);
+        at::Tensor h, codes, scales;
+        if (v[11] == Py_None) {
+            h = at::empty({M, N / 2}, x.options());
+        } else {
+            operand(v[11], "h", act, {M, N / 2});
+            h = THPVariable_Unpack(v[11]);
+        }
+        if (save) {
+            codes = at::empty({M, N}, x.options().dtype(at::kChar));
+            scales = at::empty({M, groups_of(N)}, x.options().dtype(at::kFloat));
+        }
+        const int m = size_arg(M), k = size_arg(K);
+        const int rc = without_gil([&] {
+            return fbq_gated(px, (const uint32_t *)l.q, l.s, l.z, l.A, l.B, h.data_ptr(), save ? (int8_t *)codes.data_ptr() : nullptr,
+                             save ? (float *)scales.data_ptr() : nullptr, m, N, k, group, bits, l.rank, gate, act == at::kBFloat16, stream);
+        });
+        if (rc != FBQ_OK) return PyLong_FromLong(rc);
+        return save ? results({h, codes, scales}) : THPVariable_Wrap(h);
+    });
+}
+
+// act8_pack(x, stream) -> (codes, scales), or the error code
+PyObject *py_act8_pack(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return guarded(n, 2, [&]() -> PyObject * {
+        const at::Tensor &x = tensor_of(v[0], "x", 2);
+        const at::ScalarType act = act_type(x, "x");
+        const int64_t M = x.size(0), K = x.size(1);
+        void *px = operand(v[0], "x", act, {M, K}), *stream = stream_arg(v[1]);
+        const at::Tensor codes = at::empty({M, K}, x.options().dtype(at::kChar)), scales = at::empty({M, groups_of(K)}, x.options().dtype(at::kFloat));
+        const int m = size_arg(M), k = size_arg(K);
+        const int rc = without_gil([&] { return fbq_act8_pack(px, (int8_t *)codes.data_ptr(), (float *)scales.data_ptr(), m, k, act == at::kBFloat16, stream); });
+        return rc == FBQ_OK ? results({codes, scales}) : PyLong_FromLong(rc);
+    });
+}
+
+// act8_unpack(codes, scales, bf16, stream) -> x, or the error code
+PyObject *py_act8_unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return guarded(n, 4, [&]() -> PyObject * {
+        const at::Tensor &codes = tensor_of(v[0], "codes", 2);
+        const int64_t M = codes.size(0), K = codes.size(1);
+        void *pc = operand(v[0], "codes", at::kChar, {M, K}), *ps = operand(v[1], "scales", at::kFloat, {M, groups_of(K)});
+        const bool bf16 = PyObject_IsTrue(v[2]) == 1;
+        void *stream = stream_arg(v[3]);
+        const at::Tensor x = at::empty({M, K}, codes.options().dtype(bf16 ? at::kBFloat16 : at::kHalf));
+        const int m = size_arg(M), k = size_arg(K);
+        const int rc = without_gil([&] { return fbq_act8_unpack((const int8_t *)pc, (const float *)ps, x.data_ptr(), m, k, bf16, stream); });
+        return rc == FBQ_OK ? THPVariable_Wrap(x) : PyLong_FromLong(rc);
+    });
+}
+
+// backward(gated, dy or dh, kept codes, kept scales, x or codes, x's scales or None, qweight, scales, zeros, A, B, group, bits, gate, want dx, want factors, stream)
+// -> (dx, dA, dB), or the error code
+PyObject *py_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return guarded(n, 17, [&]() -> PyObject * {
+        const bool gated = PyObject_IsTrue(v[0]) == 1, want_dx = PyObject_IsTrue(v[14]) == 1, want_factors = PyObject_IsTrue(v[15]) == 1;
+        const char *what = gated ? "dh" : "dy";
+        const at::Tensor &dy = tensor_of(v[1], what, 2);
+        const at::ScalarType act = act_type(dy, what);
+        const int group = int_arg(v[11]), bits = int_arg(v[12]), gate = int_arg(v[13]);
+        const int64_t M = dy.size(0), N = gated ? 2 * dy.size(1) : dy.size(1), K = tensor_of(v[7], "scales", 2).size(1) * group;
+        void *pdy = operand(v[1], what, act, dy.sizes());
+        const Layer l = layer_of(v + 6, N, K, group, bits, act);
+        void *kept = nullptr, *kept_scales = nullptr, *x = nullptr, *x8 = nullptr, *x8_scales = nullptr;
+        if (gated) {
+            kept = operand(v[2], "kept codes", at::kChar, {M, N});
+            kept_scales = operand(v[3], "kept scales", at::kFloat, {M, groups_of(N)});
+        }
+        if (v[5] != Py_None) {
+            x8 = operand(v[4], "x codes", at::kChar, {M, K});
+            x8_scales = operand(v[5], "x scales", at::kFloat, {M, groups_of(K)});
+        } else if (v[4] != Py_None) {
+            x = operand(v[4], "x", act, {M, K});
+        }
+        void *stream = stream_arg(v[16]);
+        at::Tensor dx, dA, dB;
+        if (want_dx) dx = at::empty({M, K}, dy.options());
+        if (want_factors && l.rank > 0) {
+            dA = at::empty({l.rank, K}, dy.options());
+            dB = at::empty({N, l.rank}, dy.options());
+        }
+        auto at_of = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+        const int m = size_arg(M), nn = size_arg(N), k = size_arg(K);
+        const int rc = without_gil([&] {
+            if (gated)
+                return fbq_gated_backward(pdy, (const int8_t *)kept, (const float *)kept_scales, x, (const int8_t *)x8, (const float *)x8_scales, (const uint32_t *)l.q, l.s, l.z,
+                                          l.A, l.B, at_of(dx), at_of(dA), at_of(dB), m, nn, k, group, bits, l.rank, gate, act == at::kBFloat16, stream);
+            return fbq_linear_backward(pdy, x, (const int8_t *)x8, (const float *)x8_scales, (const uint32_t *)l.q, l.s, l.z, l.A, l.B, at_of(dx), at_of(dA), at_of(dB), m, nn,
+                                       k, group, bits, l.rank, act == at::kBFloat16, stream);
+        });
+        return rc == FBQ_OK ? results({dx, dA, dB}) : PyLong_FromLong(rc);
+    });
+}
+
+PyMethodDef methods[] = {{"gated", (PyCFunction)(void (*)(void))py_gated, METH_FASTCALL, nullptr},
+                         {"act8_pack", (PyCFunction)(void (*)(void))py_act8_pack, METH_FASTCALL, nullptr},
+                         {"act8_unpack", (PyCFunction)(void (*)(void))py_act8_unpack, METH_FASTCALL, nullptr},
+                         {"backward", (PyCFunction)(void (*)(void))py_backward, METH_FASTCALL, nullptr},
+                         {"linear", (PyCFunction)(void (*)(void))py_linear, METH_FASTCALL, nullptr},
                          {"linear_batch", (PyCFunction)(void (*)(void))py_linear_batch, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fbq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

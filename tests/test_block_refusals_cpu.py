@@ -103,3 +103,21 @@ def test_without_a_device():
 def test_names_of_gates():
     with pytest.raises(ValueError):
         fbq.gated(torch.zeros((1, 128), dtype=torch.float16), None, None, None, None, None, 32, 128, 4, fn="relu")
+
+
+def test_tensors_that_are_not_on_a_device():
+    x, layer = torch.zeros((1, 128), dtype=torch.float16), (torch.zeros(512, dtype=torch.int32), *(torch.zeros((32, 1), dtype=torch.float16) for _ in range(2)), None, None)
+    with pytest.raises(ValueError):
+        fbq.gated(x, *layer, 32, 128, 4)
+    with pytest.raises(ValueError):
+        fbq.act8_pack(x)
+    with pytest.raises(ValueError):
+        fbq.act8_unpack(torch.zeros((1, 4), dtype=torch.int8), torch.zeros((1, 1)), torch.float16)
+    with pytest.raises(ValueError):
+        fbq.linear_backward(torch.zeros((1, 32), dtype=torch.float16), x, *layer, 128, 4)
+    with pytest.raises(TypeError):
+        fbq.gated(x.float(), *layer, 32, 128, 4)
+    with pytest.raises(TypeError):
+        fbq.gated(None, *layer, 32, 128, 4)
+    with pytest.raises(TypeError):
+        fbq.act8_unpack(torch.zeros((1, 4), dtype=torch.int8), torch.zeros((1, 1)), torch.float32)
