@@ -7,10 +7,10 @@
 // Up to a few hundred tokens a weight is used too seldom to be dequantised in a pass of its own (the dense kernel's 16-bit copy costs 4
 // bytes a weight through L2 beside the half byte of its code), and tiles of 128 features are about as many as SMs, which leaves a second
 // wave nearly empty.  So a CTA takes all tokens of a tile (up to 512: 128 lanes x 512 columns are the whole tensor memory), turns codes
-// into the operand in shared memory, and the blocks of all tiles, in order, are cut into equal ranges, one per CTA:
+// into the operand in shared memory, and the pairs of blocks of all tiles, in order, are cut into equal ranges, one per CTA:
 //
-//   warps 8-23   two groups of eight dequantise every other block, 32 codes a thread; codes come straight from global memory into registers,
-//                three blocks ahead of their use (what is in flight needs no shared memory and no barrier)
+//   warps 2, 3   bring the packed codes of a pair of blocks, 128 rows x one quantisation group, by TMA, and its scales and zero points
+//   warps 8-23   two groups of eight dequantise every other pair, 64 codes a thread, into two stages of the operands
 //   warp 0       copies x (dy) by TMA, and both operands of the sub-branch's blocks
 //   warp 1       issues tcgen05.mma 128 x tokens x 16
 //   warps 4-7    epilogue: of a tile that several CTAs share all but one store their fp32 sums; the CTA that holds its first block owns it, adds the
@@ -22,8 +22,8 @@
 // Sums do not depend on timing.  Tags of finished sums carry the launch's number (as in fbq_dense.cu, with the same words): nothing is cleared.
 // All waits are bounded.
 //
-// Forward, features are rows of W and the operand is K-major; Grad, features are its columns, a block is 64 rows x 128 columns, one group
-// of each row, and the operand is MN-major: rows are written as they lie.
+// Forward, features are rows of W and the operand is K-major: a pair of blocks is one group of 128 rows.  Grad, features are its columns,
+// 128 of them one group; a pair is 128 rows of it, and the operand is MN-major: rows are written as they lie.
 #include <algorithm>
 #include <type_traits>
 
@@ -41,61 +41,45 @@ constexpr int kBK = 64, kFeat = 128;
 constexpr uint32_t kWBytes = kFeat * kBK * 2u, kBox = kWBytes / 2;
 constexpr int kMostTok = 512, kMostStages = 8;
 constexpr int kDqWarp = 8, kGroupWarps = 8, kThreads = (kDqWarp + 2 * kGroupWarps) * 32;
-constexpr int kAhead = 3;                        // blocks of its own that a dequantising thread has requested
+constexpr int kRing = 4;                         // pairs of blocks whose codes and scales are there or on their way
+constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = kCodeBytes + 512u;      // codes (INT3: 48 of 64 bytes a row), scales and zero points
+constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
-constexpr uint32_t kFixed = 2 * kYBytes + 512 + 256;     // staging, largest |p|, barriers
+constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 256;     // ring, staging, largest |p|, barriers
 constexpr uint32_t kSmemMost = 227 * 1024 - 1024;        // (the base is moved up to 1024 bytes)
 constexpr int kTagEpoch = 0, kTagDone = 1, kTagFirst = 4;        // words of the tag scratch, shared with fbq_dense.cu
 
 enum Mode { kGated, kKept, kGrad };
 
 struct EvenParams {
-    const uint32_t *qw;
     const __half *scales, *zeros;
     float *part;              // [CTA][tok][kFeat] sums of the tile that a range begins with and does not own
     uint32_t *tags;           // see above; a word per range
     float *kept_scales;
     int *status;
     int M, F, D, K;           // tokens, features, contraction, columns of W
-    int tok, ntt, nkb, slab;  // tokens of a tile, token tiles, blocks of the contraction, of the sub-branch
+    int tok, ntt, nkp, slab;  // tokens of a tile, token tiles, pairs of blocks of the contraction, blocks of the sub-branch
     int stages, gate, kept_pitch;
-    long long blocks;         // of all tiles
+    long long pairs;          // of all tiles
     uint32_t wait_looks;
     int test_skip_flag;
 };
 
-// The pieces of a CTA's range: blocks [kb0, kb1) of a tile, and whether the tile is its own.
+// The pieces of a CTA's range: pairs of blocks [kp0, kp1) of a tile, and whether the tile is its own.
 struct Pieces {
     long long at, end;
-    int nkb, tile, kb0, kb1;
-    __device__ __forceinline__ Pieces(const EvenParams &p, int range) : at(p.blocks * range / gridDim.x), end(p.blocks * (range + 1) / gridDim.x), nkb(p.nkb) {}
+    int nkp, tile, kp0, kp1;
+    __device__ __forceinline__ Pieces(const EvenParams &p, int range) : at(p.pairs * range / gridDim.x), end(p.pairs * (range + 1) / gridDim.x), nkp(p.nkp) {}
     __device__ __forceinline__ bool next()
     {
         if (at >= end) return false;
-        tile = (int)(at / nkb);
-        kb0 = (int)(at - (long long)tile * nkb);
-        kb1 = (int)min((long long)nkb, kb0 + (end - at));
-        at += kb1 - kb0;
+        tile = (int)(at / nkp);
+        kp0 = (int)(at - (long long)tile * nkp);
+        kp1 = (int)min((long long)nkp, kp0 + (end - at));
+        at += kp1 - kp0;
         return true;
     }
-    __device__ __forceinline__ bool owner() const { return kb0 == 0; }
-};
-// The same block by block, the sub-branch's included (kb >= kb1).
-struct Blocks {
-    Pieces pc;
-    int kb, last, slab;
-    bool on;
-    __device__ __forceinline__ Blocks(const EvenParams &p, int range) : pc(p, range), slab(p.slab) { open(); }
-    __device__ __forceinline__ void open()
-    {
-        on = pc.next();
-        kb = pc.kb0;
-        last = pc.kb1 + (pc.owner() ? slab : 0);
-    }
-    __device__ __forceinline__ void step()
-    {
-        if (on && ++kb == last) open();
-    }
+    __device__ __forceinline__ bool owner() const { return kp0 == 0; }
 };
 
 __device__ __forceinline__ void store_release(uint32_t *p, uint32_t v) { asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory"); }
@@ -126,106 +110,200 @@ __device__ __forceinline__ bool wait_tag(const EvenParams &p, const uint32_t *wo
     }
 }
 
-// A thread's 32 codes of a block, with their scale and zero point.
-template <int BITS> struct Raw {
-    uint32_t w[BITS == 4 ? 4 : 3];
-    __half s, z;
-};
+__device__ __forceinline__ uint32_t ldg_u16(const __half *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.nc.u16 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 lds_v2(uint32_t a)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
 
-template <int BITS, typename T, int MODE>
-__device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint32_t sbase, uint32_t stage_bytes, uint32_t full0, uint32_t empty0, volatile int *quit)
+// Warps 2 and 3: the ring.  Scales and zero points lie 2 bytes here and there (an instruction touches as many lines as it has lanes),
+// so each is loaded once per row and pair, kScaleAhead pairs before it is stored.
+template <int BITS, int MODE>
+__device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMap *qmap, int range, uint32_t ring, uint32_t rfull0, uint32_t rempty0, volatile int *quit)
 {
     constexpr bool GRAD = MODE == kGrad;
-    constexpr int NW = BITS == 4 ? 4 : 3;
-    const int warp = (threadIdx.x >> 5) - kDqWarp, group = warp / kGroupWarps, lane = threadIdx.x & 31, tid = (int)(threadIdx.x - (kDqWarp + group * kGroupWarps) * 32);
-    const int G = p.K / kGroupFast;
-    // Forward: two lanes per row of 64 k.  Grad: four per row of 128 columns, so that any eight neighbouring lanes store to four rows and
-    // both halves of a box's (different banks in the 128-byte swizzle).
-    const int row = GRAD ? (warp % kGroupWarps) * 8 + ((lane >> 1) & 7) : tid >> 1, part = GRAD ? (lane >> 4) * 2 + (lane & 1) : tid & 1;
-    const uint32_t dst = GRAD ? (uint32_t)(part >> 1) * kBox + (uint32_t)row * 128u : (uint32_t)row * 128u;
-    const uint32_t chunk = (uint32_t)(part & 1) * 4u;
-    auto load = [&](const Blocks &b, Raw<BITS> &r) {
-        if (!b.on || b.kb >= b.pc.kb1) return;
-        const int ft = b.pc.tile / p.ntt;
-        const int n = GRAD ? b.kb * kBK + row : ft * kFeat + row, k = GRAD ? ft * kFeat + part * 32 : b.kb * kBK + part * 32;
-        const bool in = n < (GRAD ? p.D : p.F);
-        const uint32_t *src = p.qw + (in ? ((size_t)n * p.K + k) / 32 * NW : 0);
-        if constexpr (BITS == 4) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
-            r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
-        } else {
+    constexpr uint32_t kWords = BITS == 4 ? 16 : 12;
+    const int lane = threadIdx.x & 31, half = (int)(threadIdx.x >> 5) - 2, G = p.K / kGroupFast, rows = GRAD ? p.D : p.F;
+    struct Scales {
+        uint32_t v[4];
+        bool on;
+    };
+    Pieces ahead(p, range);
+    int kp = 0;
+    bool on = ahead.next();
+    kp = ahead.kp0;
+    auto request = [&](Scales &c) {
+        c.on = on;
+        if (!on) return;
+        const int ft = ahead.tile / p.ntt, n0 = (GRAD ? kp : ft) * 128 + 64 * half + lane, g = GRAD ? ft : kp;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) r.w[i] = __ldg(src + i);
+        for (int i = 0; i < 2; ++i) {
+            const size_t at = (size_t)(n0 + 32 * i) * G + g;
+            c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros
+            if (n0 + 32 * i < rows) {
+                c.v[2 * i] = ldg_u16(p.scales + at);
+                c.v[2 * i + 1] = ldg_u16(p.zeros + at);
+            }
         }
-        const size_t g = in ? (size_t)n * G + k / kGroupFast : 0;
-        r.s = in ? p.scales[g] : __half(0.f);                    // what lies outside is a row of zeros
-        r.z = in ? p.zeros[g] : __half(0.f);
+        if (++kp == ahead.kp1) {
+            on = ahead.next();
+            kp = ahead.kp0;
+        }
     };
-    Blocks cur(p, range), ahead(p, range);
-    uint32_t s = 0, phase = 1u;                                  // stage of `cur`, parity of its previous use
-    bool first = true;
-    auto skip = [&]() {
-        if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
-    };
-    if (group) {
-        cur.step();
-        ahead.step();
-        skip();
-    }
-    Raw<BITS> r[kAhead];
+    Scales c[kScaleAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-        load(ahead, r[i]);
-        ahead.step();
-        ahead.step();
-    }
+    for (int i = 0; i < kScaleAhead; ++i) request(c[i]);
+    Pieces cur(p, range);
+    cur.next();
+    int ck = cur.kp0;
+    uint32_t slot = 0, phase = 1u;
+    bool first = true;
 #pragma unroll 1
     for (;;) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            if (!cur.on) return true;
-            const bool main = cur.kb < cur.pc.kb1;
-            uint32_t out[16];
-            if (main) {
-                uint32_t d[16];
-                Dequant<BITS, T>::run(r[i].w, __half2float(r[i].s), __half2float(r[i].z), d);
-                natural_pairs<BITS>(d, out);
+        for (int i = 0; i < kScaleAhead; ++i) {
+            if (!c[i].on) return true;
+            if (!__all_sync(0xffffffffu, first || umma::wait_cluster(rempty0 + 8u * slot, phase, quit))) return false;
+            const uint32_t dst = ring + slot * kSlotBytes, bar = rfull0 + 8u * slot;
+            if (half == 0 && lane == 0) {
+                const int ft = cur.tile / p.ntt;
+                mbar_expect_tx(bar, 128u * kWords * 4u);
+                tma_load_2d(dst, qmap, (GRAD ? ft : ck) * (int)kWords, (GRAD ? ck : ft) * 128, bar);
             }
-            if (!__all_sync(0xffffffffu, first || umma::wait_cluster(empty0 + 8u * s, phase, quit))) return false;
-            if (main) {
-                const uint32_t at = sbase + s * stage_bytes + dst;
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) sts128(at + (((chunk + j) ^ ((uint32_t)row & 7u)) << 4), out + 4 * j);
-                fence_proxy_async();
-            }
+            for (int k = 0; k < 2; ++k)
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kCodeBytes + (uint32_t)(64 * half + lane + 32 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16)
+                             : "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(full0 + 8u * s);
-            load(ahead, r[i]);
-            ahead.step();
-            ahead.step();
-            cur.step();
-            cur.step();
-            skip();
-            skip();
+            if (lane == 0) mbar_arrive(bar);
+            request(c[i]);
+            if (++ck == cur.kp1) {
+                cur.next();
+                ck = cur.kp0;
+            }
+            if (++slot == kRing) { slot = 0; phase ^= 1u; first = false; }
         }
     }
 }
 
+template <int BITS, typename T, int MODE>
+__device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint32_t sbase, uint32_t stage_bytes, uint32_t ring, uint32_t full0, uint32_t empty0,
+                                           uint32_t rfull0, uint32_t rempty0, volatile int *quit)
+{
+    constexpr bool GRAD = MODE == kGrad;
+    constexpr int NW = BITS == 4 ? 4 : 3;
+    const int warp = (threadIdx.x >> 5) - kDqWarp, group = warp / kGroupWarps, w = warp % kGroupWarps, lane = threadIdx.x & 31;
+    // A thread's row of the pair and its 64 of the row's 128 codes.  Forward those are the pair's block and the row the operand's; Grad the
+    // row's half chooses the block and the codes a box of the operand.  Eight neighbouring lanes store to eight rows: different banks in the
+    // 128-byte swizzle, as they load them from different banks (INT4: the 64-byte swizzle of the copy).
+    const int row = 32 * (w & 3) + lane, part = w >> 2, blk = GRAD ? row >> 6 : part;
+    const uint32_t r = GRAD ? row & 63 : row;
+    const uint32_t dst = sbase + (GRAD ? (uint32_t)part * kBox : 0u) + r * 128u + ((r & 7u) << 4);          // unit j: ^ (j << 4)
+    const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u + (uint32_t)part * 24u;
+    Pieces pc(p, range);
+    uint32_t s = 0, use = 0;                                     // stage of the next block, times it has been used
+    uint32_t q = 0;                                              // pairs so far
+    const uint32_t stages = (uint32_t)p.stages;
+    auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait_cluster(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
+    while (pc.next()) {
+        const int n = pc.kp1 - pc.kp0;
+#pragma unroll 1
+        for (int k = 0; k < n; ++k, ++q) {
+            // the stage of this thread's block, and its use before this one.  The other group's pairs and the sub-branch's blocks are waited
+            // for as well: a wait tells one phase of a barrier from the next, not from the one after that.
+            uint32_t st = s + (uint32_t)blk, u = use;
+            if (st >= stages) {
+                st -= stages;
+                ++u;
+            }
+            if ((q & 1u) != (uint32_t)group) {
+                if (!free_again(st, u)) return false;
+            } else {
+                const uint32_t slot = q % kRing, at = ring + slot * kSlotBytes;
+                if (!__all_sync(0xffffffffu, umma::wait_cluster(rfull0 + 8u * slot, (q / kRing) & 1u, quit))) return false;
+                uint32_t c[2 * NW];
+                if constexpr (BITS == 4) {
+                    const uint4 a = lds128(at + (src ^ (uint32_t)(part << 5))), b = lds128(at + (src ^ (uint32_t)(part << 5 | 16)));
+                    c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
+                    c[4] = b.x; c[5] = b.y; c[6] = b.z; c[7] = b.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) {
+                        const uint2 a = lds_v2(at + src + 8u * i);
+                        c[2 * i] = a.x;
+                        c[2 * i + 1] = a.y;
+                    }
+                }
+                uint32_t sz;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(at + kCodeBytes + (uint32_t)row * 4u) : "memory");
+                const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
+                const uint32_t to = dst + st * stage_bytes;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t d[16], out[16];
+                    Dequant<BITS, T>::run(c + NW * i, fs, fz, d);
+                    natural_pairs<BITS>(d, out);
+                    if (i == 0) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(rempty0 + 8u * slot);         // (this warp has its codes in registers)
+                        if (!free_again(st, u)) return false;
+                    }
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) sts128(to ^ ((4u * i + j) << 4), out + 4 * j);
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full0 + 8u * st);
+            }
+            s += 2;
+            if (s >= stages) {
+                s -= stages;
+                ++use;
+            }
+        }
+        if (pc.owner()) {                                        // the sub-branch's stages are made by copies
+            for (int k = 0; k < p.slab; ++k) {
+                if (!free_again(s, use)) return false;
+                if (++s == stages) {
+                    s = 0;
+                    ++use;
+                }
+            }
+        }
+    }
+    return true;
+}
+
 // xmap: x (Grad: dy) [M][D], boxes of 64 x tok rows (tok / 2 above 256); tmap: t (s) [M][rank_pad], the same boxes; bmap: B [F][rank], boxes 64 x 128 rows
 // (Grad: A [rank][F], 64 x 64, MN-major); all in the 128-byte swizzle.  ymap: h [M][F / 2], boxes of 16 rows x 64 columns (Grad: dx [M][F], x 128);
-// cmap, Kept: codes [M][F], 16 rows x 128.
+// cmap, Kept: codes [M][F], 16 rows x 128.  qmap: packed codes [rows of W][words], boxes of 128 rows x one group (INT4: 64-byte swizzle).
 template <int BITS, typename T, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap bmap,
-            const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap cmap, const EvenParams p)
+            const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap qmap, const EvenParams p)
 {
     constexpr bool GRAD = MODE == kGrad;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t sbase = smem_u32(smem), stage_bytes = kWBytes + (uint32_t)p.tok * (kBK * 2u), y_off = (uint32_t)p.stages * stage_bytes;
-    const uint32_t full0 = sbase + y_off + 2 * kYBytes + 512u, empty0 = full0 + 8u * kMostStages, accf0 = empty0 + 8u * kMostStages, acce0 = accf0 + 16u;
-    float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + 512u + 16u * kMostStages + 32u);
+    const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = kRing * kSlotBytes + 512u;
+    const uint32_t full0 = ring + bars, empty0 = full0 + 8u * kMostStages, accf0 = empty0 + 8u * kMostStages, acce0 = accf0 + 16u, rfull0 = acce0 + 16u,
+                   rempty0 = rfull0 + 8u * kRing;
+    float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + kRing * kSlotBytes);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = (int)(gridDim.x - 1 - blockIdx.x);
     const int halves = p.tok > 256 ? 2 : 1, cols = p.tok / halves;     // an MMA has 256 columns at most
@@ -234,8 +312,12 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) {
-            mbar_init(full0 + 8u * i, 1 + kGroupWarps);
+            mbar_init(full0 + 8u * i, 1 + kGroupWarps / 2);      // the copies' lane, and the four warps that make a block
             mbar_init(empty0 + 8u * i, 1);
+        }
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(rfull0 + 8u * i, 3);                       // the copy's lane and both loading warps
+            mbar_init(rempty0 + 8u * i, kGroupWarps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(accf0 + 8u * i, 1);
@@ -249,6 +331,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             prefetch_tensormap(&tmap);
             prefetch_tensormap(&bmap);
         }
+        prefetch_tensormap(&qmap);
     }
     if (warp == 1) umma::tmem_alloc<1>(smem_u32(tmem_slot), 512u);
     umma::fence_before();
@@ -266,51 +349,58 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             bool first = true;
             const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u);
 #pragma unroll 1
-            for (Blocks b(p, range); b.on && ok; b.step()) {
-                if (!first && !umma::wait_cluster(empty0 + 8u * s, phase, quit)) { ok = false; break; }
-                const bool main = b.kb < b.pc.kb1;
-                const int ft = b.pc.tile / p.ntt, m0 = (b.pc.tile - ft * p.ntt) * p.tok, c0 = (main ? b.kb : b.kb - b.pc.kb1) * kBK;
-                const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes, xt = wt + kWBytes;
-                mbar_expect_tx(bar, main ? xbytes : xbytes + kWBytes);
-                for (int h = 0; h < halves; ++h) tma_load_2d(xt + (uint32_t)(h * cols) * (kBK * 2u), main ? &xmap : &tmap, c0, m0 + h * cols, bar);
-                if (!main) {
-                    if (GRAD) {
-                        for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
-                    } else {
-                        tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
+            for (Pieces pc(p, range); ok && pc.next();) {
+                const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, main = 2 * (pc.kp1 - pc.kp0), n = main + (pc.owner() ? p.slab : 0);
+#pragma unroll 1
+                for (int i = 0; i < n; ++i) {
+                    if (!first && !umma::wait_cluster(empty0 + 8u * s, phase, quit)) { ok = false; break; }
+                    const bool mine = i < main;
+                    const int c0 = (mine ? 2 * pc.kp0 + i : i - main) * kBK;
+                    const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes, xt = wt + kWBytes;
+                    mbar_expect_tx(bar, mine ? xbytes : xbytes + kWBytes);
+                    for (int h = 0; h < halves; ++h) tma_load_2d(xt + (uint32_t)(h * cols) * (kBK * 2u), mine ? &xmap : &tmap, c0, m0 + h * cols, bar);
+                    if (!mine) {
+                        if (GRAD) {
+                            for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
+                        } else {
+                            tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
+                        }
+                        for (int k = 0; k < kGroupWarps / 2; ++k) mbar_arrive(bar);      // (for the warps that have nothing to make)
                     }
+                    if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
                 }
-                if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
             }
         }
         __syncwarp();
     } else if (warp == 1) {
         // =================================================== MMAs
-        if (lane == 0) {
-            const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kFeat, (uint32_t)cols) | (GRAD ? umma::kIdescMnA : 0u);
-            const uint32_t wstep = GRAD ? 2048u >> 4 : 2u;
-            uint32_t s = 0, phase = 0, it = 0;
+        // The whole warp walks the loop and one elected lane issues: the MMAs' operands stay in uniform registers.
+        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kFeat, (uint32_t)cols) | (GRAD ? umma::kIdescMnA : 0u);
+        const uint32_t wstep = GRAD ? 2048u >> 4 : 2u, xhalf = (uint32_t)cols * (kBK * 2u >> 4);
+        const uint64_t wd0 = GRAD ? umma::desc_mn128(sbase, kBox) : umma::desc_k128(sbase), xd0 = umma::desc_k128(sbase + kWBytes);
+        uint32_t s = 0, phase = 0, it = 0;
 #pragma unroll 1
-            for (Pieces pc(p, range); ok && pc.next(); ++it) {
-                const uint32_t buf = nbuf == 2 ? it & 1u : 0u, use = nbuf == 2 ? it >> 1 : it, d = tmem + buf * 256u;
-                if (use > 0 && !umma::wait_cluster(acce0 + 8u * buf, (use - 1u) & 1u, quit)) { ok = false; break; }
+        for (Pieces pc(p, range); ok && pc.next(); ++it) {
+            const uint32_t buf = nbuf == 2 ? it & 1u : 0u, use = nbuf == 2 ? it >> 1 : it, d = tmem + buf * 256u;
+            ok = __all_sync(0xffffffffu, use == 0 || umma::wait_cluster(acce0 + 8u * buf, (use - 1u) & 1u, quit));
+            umma::fence_after();
+            const int n = 2 * (pc.kp1 - pc.kp0) + (pc.owner() ? p.slab : 0);
+#pragma unroll 1
+            for (int i = 0; i < n && ok; ++i) {
+                ok = __all_sync(0xffffffffu, umma::wait_cluster(full0 + 8u * s, phase, quit));
                 umma::fence_after();
-                const int n = pc.kb1 - pc.kb0 + (pc.owner() ? p.slab : 0);
-#pragma unroll 1
-                for (int i = 0; i < n; ++i) {
-                    if (!umma::wait_cluster(full0 + 8u * s, phase, quit)) { ok = false; break; }
-                    umma::fence_after();
-                    const uint32_t wt = sbase + s * stage_bytes;
-                    const uint64_t wd = GRAD ? umma::desc_mn128(wt, kBox) : umma::desc_k128(wt), xd = umma::desc_k128(wt + kWBytes);
+                if (ok && umma::elect_one()) {
+                    const uint64_t wd = wd0 + s * (stage_bytes >> 4), xd = xd0 + s * (stage_bytes >> 4);
 #pragma unroll
                     for (int j = 0; j < kBK / 16; ++j) {
                         umma::mma(d, wd + wstep * j, xd + 2 * j, idesc, i > 0 || j > 0);
-                        if (halves == 2) umma::mma(d + (uint32_t)cols, wd + wstep * j, xd + 2 * j + (uint32_t)cols * (kBK * 2u >> 4), idesc, i > 0 || j > 0);
+                        if (halves == 2) umma::mma(d + (uint32_t)cols, wd + wstep * j, xd + 2 * j + xhalf, idesc, i > 0 || j > 0);
                     }
                     umma::commit(empty0 + 8u * s);
-                    if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; }
+                    if (i + 1 == n) umma::commit(accf0 + 8u * buf);
                 }
-                if (ok) umma::commit(accf0 + 8u * buf);
+                __syncwarp();
+                if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; }
             }
         }
         __syncwarp();
@@ -348,9 +438,9 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 continue;
             }
             // ranges behind this one that hold blocks of the tile
-            const long long tile_end = (long long)(pc.tile + 1) * p.nkb;
+            const long long tile_end = (long long)(pc.tile + 1) * p.nkp;
             int others = 0;
-            while (range + others + 1 < (int)gridDim.x && p.blocks * (range + others + 1) / gridDim.x < tile_end) ++others;
+            while (range + others + 1 < (int)gridDim.x && p.pairs * (range + others + 1) / gridDim.x < tile_end) ++others;
             for (int o = 1; o <= others && ok; ++o) ok = wait_tag(p, p.tags + kTagFirst + range + o, tag, quit);
             if (others) ok = named_barrier_and(1, 128, ok);
             if (!ok) break;
@@ -422,7 +512,9 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp >= kDqWarp) {
-        ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, full0, empty0, quit);
+        ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, ring, full0, empty0, rfull0, rempty0, quit);
+    } else {
+        ok = load_codes<BITS, MODE>(p, &qmap, range, ring, rfull0, rempty0, quit);
     }
     if (!ok) {
         *quit = 1;
@@ -462,11 +554,11 @@ void token_tiles(int M, int *tok, int *ntt)
     const int m = (M + *ntt - 1) / *ntt;
     *tok = m <= 256 ? (m + 15) / 16 * 16 : (m + 31) / 32 * 32;
 }
-long long all_blocks(int ntt, int F, int D) { return (long long)((F + kFeat - 1) / kFeat) * ntt * ((D + kBK - 1) / kBK); }
-int ctas_for(long long blocks) { return (int)std::min<long long>(sms_of_device(), blocks); }
+long long all_pairs(int ntt, int F, int D) { return (long long)((F + kFeat - 1) / kFeat) * ntt * ((D + 2 * kBK - 1) / (2 * kBK)); }
+int ctas_for(long long pairs) { return (int)std::min<long long>(sms_of_device(), pairs); }
 
 template <int BITS, typename T, int MODE>
-cudaError_t start(const CUtensorMap (&maps)[5], const EvenParams &p, bool pdl, cudaStream_t s)
+cudaError_t start(const CUtensorMap (&maps)[6], const EvenParams &p, bool pdl, cudaStream_t s)
 {
     auto kern = even_kernel<BITS, T, MODE>;
     static bool attr_set = false;
@@ -475,7 +567,7 @@ cudaError_t start(const CUtensorMap (&maps)[5], const EvenParams &p, bool pdl, c
         attr_set = true;
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)ctas_for(p.blocks));
+    cfg.gridDim = dim3((unsigned)ctas_for(p.pairs));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = (size_t)p.stages * (kWBytes + p.tok * (kBK * 2u)) + kFixed + 1024;
     cfg.stream = s;
@@ -484,7 +576,7 @@ cudaError_t start(const CUtensorMap (&maps)[5], const EvenParams &p, bool pdl, c
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], p);
+    return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], p);
 }
 
 }  // namespace
@@ -493,7 +585,7 @@ size_t even_part_bytes(int M, int F, int D)
 {
     int tok, ntt;
     token_tiles(M, &tok, &ntt);
-    return (size_t)ctas_for(all_blocks(ntt, F, D)) * tok * kFeat * sizeof(float);
+    return (size_t)ctas_for(all_pairs(ntt, F, D)) * tok * kFeat * sizeof(float);
 }
 size_t even_tags() { return (size_t)kTagFirst + sms_of_device(); }
 
@@ -501,7 +593,7 @@ cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &t
 {
     const bool grad = a.gate < 0;
     EvenParams p{};
-    p.qw = a.qw; p.scales = a.scales; p.zeros = a.zeros;
+    p.scales = a.scales; p.zeros = a.zeros;
     p.part = static_cast<float *>(a.part);
     p.tags = ws.tags;
     p.status = ws.counters + kCtrStatus;
@@ -509,21 +601,25 @@ cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &t
     p.F = grad ? a.K : a.N;
     p.D = grad ? a.N : a.K;
     token_tiles(a.M, &p.tok, &p.ntt);
-    p.nkb = (p.D + kBK - 1) / kBK;
+    p.nkp = (p.D + 2 * kBK - 1) / (2 * kBK);
     const int rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.slab = rank_pad / kBK;
     p.stages = (int)std::min<uint32_t>(kMostStages, (kSmemMost - kFixed) / (kWBytes + p.tok * (kBK * 2u)));
     p.gate = a.gate;
     p.kept_scales = a.kept_scales;
     p.kept_pitch = (p.F + kKeptGroup - 1) / kKeptGroup;
-    p.blocks = all_blocks(p.ntt, p.F, p.D);
+    p.pairs = all_pairs(p.ntt, p.F, p.D);
     p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
     p.test_skip_flag = tune.test_skip_flag;
     const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
     const int box = p.tok > 256 ? p.tok / 2 : p.tok;
-    CUtensorMap maps[5];
+    CUtensorMap maps[6];
     cudaError_t e;
+    const int words = a.bits == 4 ? 16 : 12;
+    if ((e = cached_map(&maps[5], matrix_map(a.qw, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, (size_t)(a.K / kGroupFast) * words, a.N, words, 128,
+                                             a.bits == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : none))) != cudaSuccess)
+        return e;
     if ((e = encode_map(&maps[0], matrix_map(a.x, dt, 2, p.D, a.M, kBK, box, sw))) != cudaSuccess) return e;
     maps[1] = maps[2] = maps[0];
     if (a.rank > 0) {

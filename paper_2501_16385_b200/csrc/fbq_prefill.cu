@@ -116,12 +116,7 @@ __device__ __forceinline__ bool wait_looks_cluster(uint32_t bar, uint32_t parity
         if (umma::try_wait_cluster(bar, parity)) return true;
     return false;
 }
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t on;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
-    return on != 0u;
-}
+using umma::elect_one;
 // Shared-memory loads that stay behind the waits before them (the ones in ptx order themselves with other asm only).
 __device__ __forceinline__ uint32_t lds32(uint32_t addr)
 {

@@ -29,6 +29,14 @@ __device__ __host__ constexpr uint32_t idesc_f16(uint32_t fmt, uint32_t m, uint3
     return (1u << 4) | (fmt << 7) | (fmt << 10) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
+// One lane of a converged warp, known to the compiler as one: what it passes to an MMA or a copy stays in uniform registers.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0u;
+}
+
 // D[tmem] (+)= A[smem] * B[smem]^T.  One CTA: 128 x n x 16.
 __device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {

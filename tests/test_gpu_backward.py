@@ -43,7 +43,7 @@ SHAPES = [
 ]
 
 
-@pytest.mark.parametrize("M", [1, 2, 15, 64, 65, 127, 129, 300, 1000])
+@pytest.mark.parametrize("M", [1, 2, 15, 64, 65, 127, 129, 300, 497, 1000])
 @pytest.mark.parametrize("N,K,bits,rank,dtype", SHAPES)
 def test_linear(M, N, K, bits, rank, dtype):
     dt = TYPES[dtype]
@@ -56,7 +56,7 @@ def test_linear(M, N, K, bits, rank, dtype):
     check_gradients(got, layer_gradients(layer, dy.double(), torch.zeros_like(dy, dtype=torch.float64), x64, off, None), rank)
 
 
-@pytest.mark.parametrize("M", [1, 3, 16, 63, 130, 700])
+@pytest.mark.parametrize("M", [1, 3, 16, 63, 130, 512, 700])
 @pytest.mark.parametrize("N,K,bits,rank,dtype,fn", [
     (16, 128, 4, 0, "f16", "silu"),
     (48, 256, 3, 16, "bf16", "gelu"),

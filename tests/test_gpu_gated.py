@@ -18,7 +18,7 @@ def inputs(M, K, dtype, seed, outliers=False):
 
 
 # One token to a few tiles of tokens; rows of one granule, ragged tiles, more than one tile; every kernel that gates.
-@pytest.mark.parametrize("M", [1, 2, 3, 8, 9, 16, 17, 77, 128, 129, 300])
+@pytest.mark.parametrize("M", [1, 2, 3, 8, 9, 16, 17, 77, 128, 129, 300, 500])
 @pytest.mark.parametrize("N,K,bits,rank,dtype,fn", [
     (16, 128, 4, 0, "f16", "silu"),
     (48, 128, 3, 16, "bf16", "gelu"),
@@ -49,7 +49,7 @@ def test_prompts_of_many_tiles(M, N, K, bits, rank, dtype):
     check(h, *hidden("silu", *layer.products(x), dt), "h")
 
 
-@pytest.mark.parametrize("M", [1, 5, 16, 33, 257, 1030])
+@pytest.mark.parametrize("M", [1, 5, 16, 33, 257, 481, 1030])
 @pytest.mark.parametrize("N,K,bits,rank,dtype,fn", [(16, 128, 3, 16, "f16", "gelu"), (144, 256, 4, 0, "bf16", "silu"), (656, 384, 4, 64, "f16", "silu"),
                                                     (4112, 512, 3, 128, "bf16", "gelu")])
 def test_products_kept_in_8_bits(M, N, K, bits, rank, dtype, fn):
