@@ -5,25 +5,28 @@
 //   dx = dy.dequant(Q,s,z) + s.A                               (Grad; s = dy.B from there)
 //
 // Up to a few hundred tokens a weight is used too seldom to be dequantised in a pass of its own (the dense kernel's 16-bit copy costs 4
-// bytes a weight through L2 beside the half byte of its code), and tiles of 128 features are about as many as SMs, which leaves a second
-// wave nearly empty.  So a CTA takes all tokens of a tile (up to 512: 128 lanes x 512 columns are the whole tensor memory), turns codes
-// into the operand in shared memory, and the pairs of blocks of all tiles, in order, are cut into equal ranges, one per CTA:
+// bytes a weight through L2 beside the half byte of its code), and tiles are fewer than SMs or fill a second wave badly.  So a CTA turns
+// codes into the operand in shared memory, 256 features for up to 192 tokens (128 features would read x twice as often, 64 bytes a clock and SM:
+// more than L2 gives all of them), and the pairs of blocks of all tiles, in order, are cut into equal ranges, one per CTA:
 //
-//   warps 2, 3   bring the packed codes of a pair of blocks, 128 rows x one quantisation group, by TMA, and its scales and zero points
-//   warps 8-23   two groups of eight dequantise every other pair, 64 codes a thread, into two stages of the operands
-//   warp 0       copies x (dy) by TMA, and both operands of the sub-branch's blocks
-//   warp 1       issues tcgen05.mma 128 x tokens x 16
-//   warps 4-7    epilogue: of a tile that several CTAs share all but one store their fp32 sums; the CTA that holds its first block owns it, adds the
+//   warps 2, 3   bring the packed codes of a pair of blocks, 2 x 128 rows x one quantisation group, by TMA, and their scales and zero points
+//   warps 8-23   dequantise them, 64 codes a thread: eight warps for either half of the features, into two stages of the operands
+//   warp 0       copies the tokens by TMA, and both operands of the sub-branch's blocks
+//   warp 1       issues tcgen05.mma, 128 features x tokens x 16, for both halves
+//   warps 4-7    epilogue: of a tile that several CTAs share all but one store their fp32 sums; the one that holds its first block owns it, adds the
 //                others' in order of the contraction and writes the outputs
 //
 // A range ends with the tiles it owns and begins with the one it does not, so whoever waits for sums waits for what another CTA did
-// first.  CTA b takes the range of gridDim - 1 - b: ranges behind one's own belong to CTAs with lower numbers, which start earlier, and
+// first.  CTA b takes the last range but b: ranges behind one's own belong to CTAs with lower numbers, which start earlier, and
 // wait only for lower numbers still; any number of resident CTAs makes progress.  The sub-branch's blocks are the owner's, at the end of a tile.
 // Sums do not depend on timing.  Tags of finished sums carry the launch's number (as in fbq_dense.cu, with the same words): nothing is cleared.
 // All waits are bounded.
 //
-// Forward, features are rows of W and the operand is K-major: a pair of blocks is one group of 128 rows.  Grad, features are its columns,
-// 128 of them one group; a pair is 128 rows of it, and the operand is MN-major: rows are written as they lie.
+// Forward, features are rows of W and the operand is K-major: a pair of blocks is one group of each row.  Grad, features are its columns,
+// 128 of them one group; a pair of blocks is 128 rows of it, and the operand is MN-major: rows are written as they lie.
+//
+// (Pairs of CTAs with cta_group::2 and half the tokens each were built as well: the dequantising warps' fence towards the asynchronous proxy
+// then took 1500 cycles instead of 150, 77 tokens of 4096 -> 2 x 11008 41 us.)
 #include <algorithm>
 #include <type_traits>
 
@@ -37,12 +40,12 @@ namespace fbq {
 namespace {
 using namespace ptx;
 
-constexpr int kBK = 64, kFeat = 128;
-constexpr uint32_t kWBytes = kFeat * kBK * 2u, kBox = kWBytes / 2;
-constexpr int kMostTok = 512, kMostStages = 8;
+constexpr int kBK = 64, kHalf = 128, kFeat = 2 * kHalf;
+constexpr uint32_t kHalfBytes = kHalf * kBK * 2u, kWBytes = 2 * kHalfBytes, kBox = kHalfBytes / 2;
+constexpr int kMostTok = 192, kMostStages = 6;
 constexpr int kDqWarp = 8, kGroupWarps = 8, kThreads = (kDqWarp + 2 * kGroupWarps) * 32;
-constexpr int kRing = 4;                         // pairs of blocks whose codes and scales are there or on their way
-constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = kCodeBytes + 512u;      // codes (INT3: 48 of 64 bytes a row), scales and zero points
+constexpr int kRing = 2;                         // pairs of blocks whose codes and scales are there or on their way
+constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = 2 * (kCodeBytes + 512u);      // codes of both halves (INT3: 48 of 64 bytes a row), scales and zero points
 constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
 constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 256;     // ring, staging, largest |p|, barriers
@@ -52,8 +55,9 @@ constexpr int kTagEpoch = 0, kTagDone = 1, kTagFirst = 4;        // words of the
 enum Mode { kGated, kKept, kGrad };
 
 struct EvenParams {
+    int ranges;
     const __half *scales, *zeros;
-    float *part;              // [CTA][tok][kFeat] sums of the tile that a range begins with and does not own
+    float *part;              // [range][half][tok][kHalf] sums of the tile that a range begins with and does not own
     uint32_t *tags;           // see above; a word per range
     float *kept_scales;
     int *status;
@@ -69,7 +73,7 @@ struct EvenParams {
 struct Pieces {
     long long at, end;
     int nkp, tile, kp0, kp1;
-    __device__ __forceinline__ Pieces(const EvenParams &p, int range) : at(p.pairs * range / gridDim.x), end(p.pairs * (range + 1) / gridDim.x), nkp(p.nkp) {}
+    __device__ __forceinline__ Pieces(const EvenParams &p, int range) : at(p.pairs * range / p.ranges), end(p.pairs * (range + 1) / p.ranges), nkp(p.nkp) {}
     __device__ __forceinline__ bool next()
     {
         if (at >= end) return false;
@@ -136,9 +140,9 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMa
 {
     constexpr bool GRAD = MODE == kGrad;
     constexpr uint32_t kWords = BITS == 4 ? 16 : 12;
-    const int lane = threadIdx.x & 31, half = (int)(threadIdx.x >> 5) - 2, G = p.K / kGroupFast, rows = GRAD ? p.D : p.F;
+    const int lane = threadIdx.x & 31, half = (int)(threadIdx.x >> 5) - 2, G = p.K / kGroupFast;
     struct Scales {
-        uint32_t v[4];
+        uint32_t v[8];
         bool on;
     };
     Pieces ahead(p, range);
@@ -148,9 +152,9 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMa
     auto request = [&](Scales &c) {
         c.on = on;
         if (!on) return;
-        const int ft = ahead.tile / p.ntt, n0 = (GRAD ? kp : ft) * 128 + 64 * half + lane, g = GRAD ? ft : kp;
+        const int ft = 2 * (ahead.tile / p.ntt) + half, n0 = (GRAD ? kp : ft) * kHalf + lane, g = GRAD ? ft : kp, rows = g < G ? (GRAD ? p.D : p.F) : 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const size_t at = (size_t)(n0 + 32 * i) * G + g;
             c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros
             if (n0 + 32 * i < rows) {
@@ -176,16 +180,16 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMa
 #pragma unroll
         for (int i = 0; i < kScaleAhead; ++i) {
             if (!c[i].on) return true;
-            if (!__all_sync(0xffffffffu, first || umma::wait_cluster(rempty0 + 8u * slot, phase, quit))) return false;
+            if (!__all_sync(0xffffffffu, first || umma::wait(rempty0 + 8u * slot, phase, quit))) return false;
             const uint32_t dst = ring + slot * kSlotBytes, bar = rfull0 + 8u * slot;
             if (half == 0 && lane == 0) {
-                const int ft = cur.tile / p.ntt;
-                mbar_expect_tx(bar, 128u * kWords * 4u);
-                tma_load_2d(dst, qmap, (GRAD ? ft : ck) * (int)kWords, (GRAD ? ck : ft) * 128, bar);
+                const int ft = 2 * (cur.tile / p.ntt);
+                mbar_expect_tx(bar, 2u * 128u * kWords * 4u);
+                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kCodeBytes, qmap, (GRAD ? ft + h : ck) * (int)kWords, (GRAD ? ck : ft + h) * kHalf, bar);
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kCodeBytes + (uint32_t)(64 * half + lane + 32 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16)
+            for (int k = 0; k < 4; ++k)
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * kCodeBytes + (uint32_t)(128 * half + lane + 32 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16)
                              : "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
@@ -211,29 +215,27 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
     // 128-byte swizzle, as they load them from different banks (INT4: the 64-byte swizzle of the copy).
     const int row = 32 * (w & 3) + lane, part = w >> 2, blk = GRAD ? row >> 6 : part;
     const uint32_t r = GRAD ? row & 63 : row;
-    const uint32_t dst = sbase + (GRAD ? (uint32_t)part * kBox : 0u) + r * 128u + ((r & 7u) << 4);          // unit j: ^ (j << 4)
+    const uint32_t dst = sbase + (uint32_t)group * kHalfBytes + (GRAD ? (uint32_t)part * kBox : 0u) + r * 128u + ((r & 7u) << 4);          // unit j: ^ (j << 4)
     const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u + (uint32_t)part * 24u;
     Pieces pc(p, range);
     uint32_t s = 0, use = 0;                                     // stage of the next block, times it has been used
     uint32_t q = 0;                                              // pairs so far
     const uint32_t stages = (uint32_t)p.stages;
-    auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait_cluster(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
+    auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
     while (pc.next()) {
         const int n = pc.kp1 - pc.kp0;
 #pragma unroll 1
         for (int k = 0; k < n; ++k, ++q) {
-            // the stage of this thread's block, and its use before this one.  The other group's pairs and the sub-branch's blocks are waited
-            // for as well: a wait tells one phase of a barrier from the next, not from the one after that.
+            // the stage of this thread's block, and its use before this one (the sub-branch's blocks are waited for as well: a wait tells one
+            // phase of a barrier from the next, not from the one after that)
             uint32_t st = s + (uint32_t)blk, u = use;
             if (st >= stages) {
                 st -= stages;
                 ++u;
             }
-            if ((q & 1u) != (uint32_t)group) {
-                if (!free_again(st, u)) return false;
-            } else {
-                const uint32_t slot = q % kRing, at = ring + slot * kSlotBytes;
-                if (!__all_sync(0xffffffffu, umma::wait_cluster(rfull0 + 8u * slot, (q / kRing) & 1u, quit))) return false;
+            {
+                const uint32_t slot = q % kRing, at = ring + slot * kSlotBytes + (uint32_t)group * kCodeBytes;
+                if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, (q / kRing) & 1u, quit))) return false;
                 uint32_t c[2 * NW];
                 if constexpr (BITS == 4) {
                     const uint4 a = lds128(at + (src ^ (uint32_t)(part << 5))), b = lds128(at + (src ^ (uint32_t)(part << 5 | 16)));
@@ -248,7 +250,7 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                     }
                 }
                 uint32_t sz;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(at + kCodeBytes + (uint32_t)row * 4u) : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(ring + slot * kSlotBytes + 2 * kCodeBytes + (uint32_t)(128 * group + row) * 4u) : "memory");
                 const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
                 const uint32_t to = dst + st * stage_bytes;
 #pragma unroll
@@ -287,7 +289,7 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
     return true;
 }
 
-// xmap: x (Grad: dy) [M][D], boxes of 64 x tok rows (tok / 2 above 256); tmap: t (s) [M][rank_pad], the same boxes; bmap: B [F][rank], boxes 64 x 128 rows
+// xmap: x (Grad: dy) [M][D], boxes of 64 x tok rows; tmap: t (s) [M][rank_pad], the same boxes; bmap: B [F][rank], boxes 64 x 128 rows
 // (Grad: A [rank][F], 64 x 64, MN-major); all in the 128-byte swizzle.  ymap: h [M][F / 2], boxes of 16 rows x 64 columns (Grad: dx [M][F], x 128);
 // cmap, Kept: codes [M][F], 16 rows x 128.  qmap: packed codes [rows of W][words], boxes of 128 rows x one group (INT4: 64-byte swizzle).
 template <int BITS, typename T, int MODE>
@@ -305,19 +307,20 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + kRing * kSlotBytes);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = (int)(gridDim.x - 1 - blockIdx.x);
-    const int halves = p.tok > 256 ? 2 : 1, cols = p.tok / halves;     // an MMA has 256 columns at most
-    const int nbuf = halves == 1 ? 2 : 1;                               // accumulators in tensor memory
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = p.ranges - 1 - (int)blockIdx.x;
+    // accumulators in tensor memory: two of two halves where they fit
+    const uint32_t wide = p.tok > 128 ? 256u : 128u;
+    const int nbuf = p.tok > 128 ? 1 : 2;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) {
-            mbar_init(full0 + 8u * i, 1 + kGroupWarps / 2);      // the copies' lane, and the four warps that make a block
+            mbar_init(full0 + 8u * i, 1 + kGroupWarps);          // the copying lane, and four warps of either half
             mbar_init(empty0 + 8u * i, 1);
         }
         for (int i = 0; i < kRing; ++i) {
             mbar_init(rfull0 + 8u * i, 3);                       // the copy's lane and both loading warps
-            mbar_init(rempty0 + 8u * i, kGroupWarps);
+            mbar_init(rempty0 + 8u * i, 2 * kGroupWarps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(accf0 + 8u * i, 1);
@@ -353,19 +356,19 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, main = 2 * (pc.kp1 - pc.kp0), n = main + (pc.owner() ? p.slab : 0);
 #pragma unroll 1
                 for (int i = 0; i < n; ++i) {
-                    if (!first && !umma::wait_cluster(empty0 + 8u * s, phase, quit)) { ok = false; break; }
+                    if (!first && !umma::wait(empty0 + 8u * s, phase, quit)) { ok = false; break; }
                     const bool mine = i < main;
                     const int c0 = (mine ? 2 * pc.kp0 + i : i - main) * kBK;
                     const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes, xt = wt + kWBytes;
                     mbar_expect_tx(bar, mine ? xbytes : xbytes + kWBytes);
-                    for (int h = 0; h < halves; ++h) tma_load_2d(xt + (uint32_t)(h * cols) * (kBK * 2u), mine ? &xmap : &tmap, c0, m0 + h * cols, bar);
+                    tma_load_2d(xt, mine ? &xmap : &tmap, c0, m0, bar);
                     if (!mine) {
                         if (GRAD) {
-                            for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
+                            for (int h = 0; h < 4; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
                         } else {
-                            tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
+                            for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kHalfBytes, &bmap, c0, ft * kFeat + kHalf * h, bar);
                         }
-                        for (int k = 0; k < kGroupWarps / 2; ++k) mbar_arrive(bar);      // (for the warps that have nothing to make)
+                        for (int k = 0; k < kGroupWarps; ++k) mbar_arrive(bar);          // (for the warps that have nothing to make)
                     }
                     if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
                 }
@@ -374,32 +377,40 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         __syncwarp();
     } else if (warp == 1) {
         // =================================================== MMAs
-        // The whole warp walks the loop and one elected lane issues: the MMAs' operands stay in uniform registers.
-        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kFeat, (uint32_t)cols) | (GRAD ? umma::kIdescMnA : 0u);
-        const uint32_t wstep = GRAD ? 2048u >> 4 : 2u, xhalf = (uint32_t)cols * (kBK * 2u >> 4);
+        // The whole warp walks the loop and one elected lane issues: the MMAs' operands stay in uniform registers.  Two blocks at a time.
+        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kHalf, (uint32_t)p.tok) | (GRAD ? umma::kIdescMnA : 0u);
+        const uint32_t wstep = GRAD ? 2048u >> 4 : 2u;
         const uint64_t wd0 = GRAD ? umma::desc_mn128(sbase, kBox) : umma::desc_k128(sbase), xd0 = umma::desc_k128(sbase + kWBytes);
         uint32_t s = 0, phase = 0, it = 0;
 #pragma unroll 1
         for (Pieces pc(p, range); ok && pc.next(); ++it) {
             const uint32_t buf = nbuf == 2 ? it & 1u : 0u, use = nbuf == 2 ? it >> 1 : it, d = tmem + buf * 256u;
-            ok = __all_sync(0xffffffffu, use == 0 || umma::wait_cluster(acce0 + 8u * buf, (use - 1u) & 1u, quit));
-            umma::fence_after();
+            ok = __all_sync(0xffffffffu, use == 0 || umma::wait(acce0 + 8u * buf, (use - 1u) & 1u, quit));
             const int n = 2 * (pc.kp1 - pc.kp0) + (pc.owner() ? p.slab : 0);
 #pragma unroll 1
-            for (int i = 0; i < n && ok; ++i) {
-                ok = __all_sync(0xffffffffu, umma::wait_cluster(full0 + 8u * s, phase, quit));
+            for (int i = 0; i < n && ok; i += 2) {
+                const bool two = i + 1 < n;
+                const uint32_t s0 = s, s1 = s + 1 == (uint32_t)p.stages ? 0u : s + 1, ph0 = phase, ph1 = s1 ? phase : phase ^ 1u;
+                ok = umma::wait(full0 + 8u * s0, ph0, quit);
+                if (two) ok = umma::wait(full0 + 8u * s1, ph1, quit) && ok;
+                ok = __all_sync(0xffffffffu, ok);
                 umma::fence_after();
                 if (ok && umma::elect_one()) {
-                    const uint64_t wd = wd0 + s * (stage_bytes >> 4), xd = xd0 + s * (stage_bytes >> 4);
+                    auto block = [&](uint32_t stage, bool more) {
+                        const uint64_t wd = wd0 + stage * (stage_bytes >> 4), xd = xd0 + stage * (stage_bytes >> 4);
 #pragma unroll
-                    for (int j = 0; j < kBK / 16; ++j) {
-                        umma::mma(d, wd + wstep * j, xd + 2 * j, idesc, i > 0 || j > 0);
-                        if (halves == 2) umma::mma(d + (uint32_t)cols, wd + wstep * j, xd + 2 * j + xhalf, idesc, i > 0 || j > 0);
-                    }
-                    umma::commit(empty0 + 8u * s);
-                    if (i + 1 == n) umma::commit(accf0 + 8u * buf);
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int j = 0; j < kBK / 16; ++j) umma::mma(d + h * wide, wd + h * (kHalfBytes >> 4) + wstep * j, xd + 2 * j, idesc, more || j > 0);
+                        umma::commit(empty0 + 8u * stage);
+                    };
+                    block(s0, i > 0);
+                    if (two) block(s1, true);
+                    if (i + 2 >= n) umma::commit(accf0 + 8u * buf);
                 }
                 __syncwarp();
+                s = two ? s1 : s0;
+                phase = two ? ph1 : ph0;
                 if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; }
             }
         }
@@ -413,101 +424,99 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 #pragma unroll 1
         for (Pieces pc(p, range); ok && pc.next(); ++it) {
             const uint32_t buf = nbuf == 2 ? it & 1u : 0u, use = nbuf == 2 ? it >> 1 : it;
-            ok = named_barrier_and(1, 128, umma::wait_cluster(accf0 + 8u * buf, use & 1u, quit));      // (four warps go on, or none)
+            ok = named_barrier_and(1, 128, umma::wait(accf0 + 8u * buf, use & 1u, quit));      // (four warps go on, or none)
             if (!ok) break;
             umma::fence_after();
-            const uint32_t lanes = tmem + buf * 256u + ((uint32_t)(32 * wq) << 16);
-            const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, m_end = min(p.M, m0 + p.tok), n = ft * kFeat + 32 * wq + lane;
-            if (!pc.owner()) {
-                float *dst = p.part + (size_t)range * p.tok * kFeat + 32 * wq + lane;
+            const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, m_end = min(p.M, m0 + p.tok);
+            int others = 0;                                      // ranges behind this one that hold blocks of a tile of ours
+            if (pc.owner()) {
+                const long long tile_end = (long long)(pc.tile + 1) * p.nkp;
+                while (range + others + 1 < p.ranges && p.pairs * (range + others + 1) / p.ranges < tile_end) ++others;
+                for (int o = 1; o <= others && ok; ++o) ok = wait_tag(p, p.tags + kTagFirst + range + o, tag, quit);
+                if (others) ok = named_barrier_and(1, 128, ok);
+                if (!ok) break;
+            }
 #pragma unroll 1
-                for (int c = 0; c < m_end - m0; c += 32) {
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t lanes = tmem + buf * 256u + h * wide + ((uint32_t)(32 * wq) << 16);
+                const int n = ft * kFeat + h * kHalf + 32 * wq + lane;
+                const size_t part_at = (size_t)(2 * range + h) * p.tok * kHalf + 32 * wq + lane;
+#pragma unroll 1
+                for (int c = 0; c < p.tok; c += 32) {
                     uint32_t v[32];
                     umma::ld32(lanes + (uint32_t)c, v);
                     umma::wait_ld();
+                    if (h == 1 && c + 32 >= p.tok) {             // all of the accumulators is in registers
+                        umma::fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(acce0 + 8u * buf);
+                    }
+                    if (m0 + c >= p.M) continue;
+                    if (!pc.owner()) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (c + j < m_end - m0) __stcg(dst + (size_t)(c + j) * kFeat, __uint_as_float(v[j]));
+                        for (int j = 0; j < 32; ++j)
+                            if (c + j < m_end - m0) __stcg(p.part + part_at + (size_t)(c + j) * kHalf, __uint_as_float(v[j]));
+                        continue;
+                    }
+#pragma unroll 1
+                    for (int o = 1; o <= others; ++o) {
+                        const float *src = p.part + part_at + ((size_t)2 * o * p.tok + c) * kHalf;
+                        float e[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) e[j] = c + j < m_end - m0 ? __ldcg(src + (size_t)j * kHalf) : 0.f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + e[j]);
+                    }
+                    const uint32_t at = y_off + (staged & 1u) * kYBytes;
+                    if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    if constexpr (MODE == kKept) {               // the largest |p| of each token over this warp's rows, lane = token
+                        uint32_t mine = 0u;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const uint32_t top = __reduce_max_sync(0xffffffffu, v[j] & 0x7FFFFFFFu);
+                            if (lane == j) mine = top;
+                        }
+                        amax[32 * wq + lane] = __uint_as_float(mine);
+                    }
+                    named_barrier_sync(1, 128);                  // the buffer's last copy has been read
+                    if constexpr (GRAD) {
+                        unsigned short *row = reinterpret_cast<unsigned short *>(smem + at) + 32 * wq + lane;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) row[j * 128] = to_bits16<T>(__uint_as_float(v[j]));
+                    } else {
+                        gate_chunk<T>(p.gate, v, reinterpret_cast<T *>(smem + at) + 16 * wq);
+                    }
+                    if constexpr (MODE == kKept) {               // a half's 128 rows are the columns that share a scale
+                        uint32_t top = 0u;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) top = max(top, __float_as_uint(amax[32 * w + lane]));
+                        float scale, inverse;
+                        kept_scale(top, scale, inverse);
+                        if (wq == 0 && n - lane < p.F && lane < m_end - (m0 + c)) p.kept_scales[(size_t)(m0 + c + lane) * p.kept_pitch + 2 * ft + h] = scale;
+                        uint8_t *codes = smem + at + kYBytes / 2 + 32 * wq + lane;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) codes[j * 128] = (uint8_t)kept_code(__uint_as_float(v[j]), __shfl_sync(0xffffffffu, inverse, j));
+                    }
+                    fence_proxy_async();
+                    named_barrier_sync(1, 128);
+                    if (threadIdx.x == 4 * 32 && n < p.F) {
+                        const int out = GRAD ? n : n / 2;        // (lane 0's n is the half's first)
+                        const bool both = c + 16 < p.tok && m0 + c + 16 < m_end;
+                        tma_store_2d(&ymap, sbase + at, out, m0 + c);
+                        if (both) tma_store_2d(&ymap, sbase + at + kYBytes / (GRAD ? 2 : 4), out, m0 + c + 16);
+                        if (MODE == kKept) {
+                            tma_store_2d(&cmap, sbase + at + kYBytes / 2, n, m0 + c);
+                            if (both) tma_store_2d(&cmap, sbase + at + kYBytes / 2 + kYBytes / 4, n, m0 + c + 16);
+                        }
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                    ++staged;
                 }
-                umma::fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(acce0 + 8u * buf);
+            }
+            if (!pc.owner()) {
                 __threadfence();
                 named_barrier_sync(1, 128);
                 if (threadIdx.x == 4 * 32 && !p.test_skip_flag) store_release(p.tags + kTagFirst + range, tag);
-                continue;
-            }
-            // ranges behind this one that hold blocks of the tile
-            const long long tile_end = (long long)(pc.tile + 1) * p.nkp;
-            int others = 0;
-            while (range + others + 1 < (int)gridDim.x && p.pairs * (range + others + 1) / gridDim.x < tile_end) ++others;
-            for (int o = 1; o <= others && ok; ++o) ok = wait_tag(p, p.tags + kTagFirst + range + o, tag, quit);
-            if (others) ok = named_barrier_and(1, 128, ok);
-            if (!ok) break;
-#pragma unroll 1
-            for (int c = 0; c < p.tok; c += 32) {
-                uint32_t v[32];
-                umma::ld32(lanes + (uint32_t)c, v);
-                umma::wait_ld();
-                if (c + 32 >= p.tok) {                           // all of the accumulator is in registers
-                    umma::fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(acce0 + 8u * buf);
-                }
-                if (m0 + c >= p.M) continue;
-#pragma unroll 1
-                for (int o = 1; o <= others; ++o) {
-                    const float *src = p.part + ((size_t)(range + o) * p.tok + c) * kFeat + 32 * wq + lane;
-                    float e[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) e[j] = c + j < m_end - m0 ? __ldcg(src + (size_t)j * kFeat) : 0.f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + e[j]);
-                }
-                const uint32_t at = y_off + (staged & 1u) * kYBytes;
-                if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                if constexpr (MODE == kKept) {                   // the largest |p| of each token over this warp's rows, lane = token
-                    uint32_t mine = 0u;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const uint32_t top = __reduce_max_sync(0xffffffffu, v[j] & 0x7FFFFFFFu);
-                        if (lane == j) mine = top;
-                    }
-                    amax[32 * wq + lane] = __uint_as_float(mine);
-                }
-                named_barrier_sync(1, 128);                      // the buffer's last copy has been read
-                if constexpr (GRAD) {
-                    unsigned short *row = reinterpret_cast<unsigned short *>(smem + at) + 32 * wq + lane;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) row[j * 128] = to_bits16<T>(__uint_as_float(v[j]));
-                } else {
-                    gate_chunk<T>(p.gate, v, reinterpret_cast<T *>(smem + at) + 16 * wq);
-                }
-                if constexpr (MODE == kKept) {                   // a tile's 128 rows are the columns that share a scale
-                    uint32_t top = 0u;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) top = max(top, __float_as_uint(amax[32 * w + lane]));
-                    float scale, inverse;
-                    kept_scale(top, scale, inverse);
-                    if (wq == 0 && lane < m_end - (m0 + c)) p.kept_scales[(size_t)(m0 + c + lane) * p.kept_pitch + ft] = scale;
-                    uint8_t *codes = smem + at + kYBytes / 2 + 32 * wq + lane;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) codes[j * 128] = (uint8_t)kept_code(__uint_as_float(v[j]), __shfl_sync(0xffffffffu, inverse, j));
-                }
-                fence_proxy_async();
-                named_barrier_sync(1, 128);
-                if (threadIdx.x == 4 * 32) {
-                    const int n_first = n - lane, out = GRAD ? n_first : n_first / 2;
-                    const bool both = c + 16 < p.tok && m0 + c + 16 < m_end;
-                    tma_store_2d(&ymap, sbase + at, out, m0 + c);
-                    if (both) tma_store_2d(&ymap, sbase + at + kYBytes / (GRAD ? 2 : 4), out, m0 + c + 16);
-                    if (MODE == kKept) {
-                        tma_store_2d(&cmap, sbase + at + kYBytes / 2, n_first, m0 + c);
-                        if (both) tma_store_2d(&cmap, sbase + at + kYBytes / 2 + kYBytes / 4, n_first, m0 + c + 16);
-                    }
-                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                }
-                ++staged;
             }
         }
         if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -547,15 +556,14 @@ int sms_of_device()
     }
     return n;
 }
-// Tokens of a tile: all of them up to kMostTok, else equal parts.  Above 256 two MMAs share them, each a multiple of 16.
+// Tokens of a tile: all of them up to kMostTok, else equal parts, in sixteens.
 void token_tiles(int M, int *tok, int *ntt)
 {
     *ntt = (M + kMostTok - 1) / kMostTok;
-    const int m = (M + *ntt - 1) / *ntt;
-    *tok = m <= 256 ? (m + 15) / 16 * 16 : (m + 31) / 32 * 32;
+    *tok = ((M + *ntt - 1) / *ntt + 15) / 16 * 16;
 }
 long long all_pairs(int ntt, int F, int D) { return (long long)((F + kFeat - 1) / kFeat) * ntt * ((D + 2 * kBK - 1) / (2 * kBK)); }
-int ctas_for(long long pairs) { return (int)std::min<long long>(sms_of_device(), pairs); }
+int ranges_for(long long pairs) { return (int)std::min<long long>(sms_of_device(), pairs); }
 
 template <int BITS, typename T, int MODE>
 cudaError_t start(const CUtensorMap (&maps)[6], const EvenParams &p, bool pdl, cudaStream_t s)
@@ -567,7 +575,7 @@ cudaError_t start(const CUtensorMap (&maps)[6], const EvenParams &p, bool pdl, c
         attr_set = true;
     }
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)ctas_for(p.pairs));
+    cfg.gridDim = dim3((unsigned)p.ranges);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = (size_t)p.stages * (kWBytes + p.tok * (kBK * 2u)) + kFixed + 1024;
     cfg.stream = s;
@@ -585,7 +593,7 @@ size_t even_part_bytes(int M, int F, int D)
 {
     int tok, ntt;
     token_tiles(M, &tok, &ntt);
-    return (size_t)ctas_for(all_pairs(ntt, F, D)) * tok * kFeat * sizeof(float);
+    return (size_t)ranges_for(all_pairs(ntt, F, D)) * tok * kFeat * sizeof(float);
 }
 size_t even_tags() { return (size_t)kTagFirst + sms_of_device(); }
 
@@ -609,11 +617,12 @@ cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &t
     p.kept_scales = a.kept_scales;
     p.kept_pitch = (p.F + kKeptGroup - 1) / kKeptGroup;
     p.pairs = all_pairs(p.ntt, p.F, p.D);
+    p.ranges = ranges_for(p.pairs);
     p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
     p.test_skip_flag = tune.test_skip_flag;
     const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
-    const int box = p.tok > 256 ? p.tok / 2 : p.tok;
+    const int box = p.tok;
     CUtensorMap maps[6];
     cudaError_t e;
     const int words = a.bits == 4 ? 16 : 12;
@@ -624,7 +633,7 @@ cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &t
     maps[1] = maps[2] = maps[0];
     if (a.rank > 0) {
         if ((e = encode_map(&maps[1], matrix_map(a.thin, dt, 2, rank_pad, a.M, kBK, box, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&maps[2], grad ? matrix_map(a.factor, dt, 2, a.K, a.rank, kBK, kBK, sw) : matrix_map(a.factor, dt, 2, a.rank, a.N, kBK, kFeat, sw))) !=
+        if ((e = cached_map(&maps[2], grad ? matrix_map(a.factor, dt, 2, a.K, a.rank, kBK, kBK, sw) : matrix_map(a.factor, dt, 2, a.rank, a.N, kBK, kHalf, sw))) !=
             cudaSuccess)
             return e;
     }

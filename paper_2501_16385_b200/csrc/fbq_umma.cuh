@@ -145,6 +145,23 @@ __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, vola
     if (try_wait_cluster(bar, parity)) return true;
     return wait_cluster_slow(bar, parity, quit);
 }
+// The bounded wait within a CTA.
+static __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int *quit)
+{
+    const unsigned long long t0 = ptx::global_ns();
+#pragma unroll 1
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i)
+            if (ptx::mbar_try_wait(bar, parity)) return true;
+        if (*quit || ptx::global_ns() - t0 > ptx::kWaitNs) return false;
+    }
+}
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *quit)
+{
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    return wait_slow(bar, parity, quit);
+}
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t cluster_bar)
 {
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
