@@ -307,7 +307,6 @@ int run_gated_even(const LinearArgs &a, Workspace *ws, cudaStream_t s)
     ws->grad = scratch;
     if (e != cudaSuccess) return grow_status(e);
     size_t have_c = (size_t)ws->n_counters;
-    if ((e = grow(ws->tags, ws->n_tags, even_tags(), sizeof(uint32_t), s)) != cudaSuccess) return grow_status(e);
     if ((e = grow(ws->counters, have_c, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
     ws->n_counters = (int)have_c;
     int launches = 0;
@@ -321,7 +320,7 @@ int run_gated_even(const LinearArgs &a, Workspace *ws, cudaStream_t s)
     v.x = a.x; v.qw = a.qw; v.scales = a.scales; v.zeros = a.zeros; v.factor = a.B; v.thin = scratch; v.y = a.y;
     v.kept = a.kept; v.kept_scales = a.kept_scales; v.part = scratch + thin;
     v.M = a.M; v.N = a.N; v.K = a.K; v.bits = a.bits; v.rank = a.rank; v.gate = a.gate; v.bf16 = a.bf16;
-    if (launch_even(v, *ws, prefill_tuning(), s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (launch_even(v, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
     g_launches += launches;
     return FBQ_OK;
 }
@@ -482,8 +481,7 @@ int run_backward(Backward &b, cudaStream_t s)
     if (e != cudaSuccess) return grow_status(e);
     grad_workspace_need(g, &need_w, &need_tags);
     if (even) {
-        need_w = 0;
-        need_tags = even_tags();
+        need_w = need_tags = 0;
     }
     e = grow(w16, ws->w16_bytes, need_w, 1, s);
     ws->w16 = w16;
@@ -515,7 +513,7 @@ int run_backward(Backward &b, cudaStream_t s)
             EvenArgs v{};
             v.x = g.dy; v.qw = g.qw; v.scales = g.scales; v.zeros = g.zeros; v.factor = g.A; v.thin = g.s16; v.y = g.dx; v.part = scratch + even_at;
             v.M = g.M; v.N = g.N; v.K = g.K; v.bits = g.bits; v.rank = g.rank; v.gate = -1; v.bf16 = g.bf16;
-            if (launch_even(v, *ws, prefill_tuning(), s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+            if (launch_even(v, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
         }
     } else if (launch_grad(g, *ws, prefill_tuning(), s, &launches) != cudaSuccess) {
         return FBQ_ERR_CUDA;

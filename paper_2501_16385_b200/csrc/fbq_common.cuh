@@ -186,8 +186,7 @@ struct EvenArgs {
     bool bf16;
 };
 size_t even_part_bytes(int M, int features, int depth);
-size_t even_tags();
-cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);
+cudaError_t launch_even(const EvenArgs &a, int *status, bool pdl, cudaStream_t s, int *launches);
 size_t factor_grad_scratch_bytes(int M, int N, int K, int rank);
 cudaError_t launch_factor_grads(const void *dy, const void *x, const void *s16, const void *t16, void *dA, void *dB, int M, int N, int K, int rank, bool gated,
                                 bool bf16, void *scratch, int *status, bool pdl, cudaStream_t s, int *launches);

@@ -9,17 +9,16 @@
 // codes into the operand in shared memory, 256 features for up to 192 tokens (128 features would read x twice as often, 64 bytes a clock and SM:
 // more than L2 gives all of them), and the pairs of blocks of all tiles, in order, are cut into equal ranges, one per CTA:
 //
-//   warps 2, 3   bring the packed codes of a pair of blocks, 2 x 128 rows x one quantisation group, by TMA, and their scales and zero points
+//   warps 2, 3   bring the packed codes of a pair of blocks, 2 x 128 rows x one quantisation group, and their scales and zero points (pieces of 48 or
+//                64 bytes: the copy engine takes 9 cycles for each, 46 us of 53 for 4096 -> 2 x 11008; asynchronous copies of lanes far less)
 //   warps 8-23   dequantise them, 64 codes a thread: eight warps for either half of the features, into two stages of the operands
 //   warp 0       copies the tokens by TMA, and both operands of the sub-branch's blocks
 //   warp 1       issues tcgen05.mma, 128 features x tokens x 16, for both halves
-//   warps 4-7    epilogue: of a tile that several CTAs share all but one store their fp32 sums; the one that holds its first block owns it, adds the
-//                others' in order of the contraction and writes the outputs
+//   warps 4-7    epilogue: a tile that is the range's own is written; of one that several ranges share each stores its fp32 sums
 //
-// A range ends with the tiles it owns and begins with the one it does not, so whoever waits for sums waits for what another CTA did
-// first.  CTA b takes the last range but b: ranges behind one's own belong to CTAs with lower numbers, which start earlier, and
-// wait only for lower numbers still; any number of resident CTAs makes progress.  The sub-branch's blocks are the owner's, at the end of a tile.
-// Sums do not depend on timing.  Tags of finished sums carry the launch's number (as in fbq_dense.cu, with the same words): nothing is cleared.
+// and a second launch adds the shares of each such tile in order of the contraction, gates and writes it: nobody waits for another
+// CTA, and the results do not depend on timing.  (The CTA with a tile's first blocks adding the others' took 35 of 48 us at 61 tokens of 4096 x 4096,
+// where nine share a tile: one SM reads what nine have written.)  The sub-branch's blocks are done where the tile's first ones are.
 // All waits are bounded.
 //
 // Forward, features are rows of W and the operand is K-major: a pair of blocks is one group of each row.  Grad, features are its columns,
@@ -44,29 +43,27 @@ constexpr int kBK = 64, kHalf = 128, kFeat = 2 * kHalf;
 constexpr uint32_t kHalfBytes = kHalf * kBK * 2u, kWBytes = 2 * kHalfBytes, kBox = kHalfBytes / 2;
 constexpr int kMostTok = 192, kMostStages = 6;
 constexpr int kDqWarp = 8, kGroupWarps = 8, kThreads = (kDqWarp + 2 * kGroupWarps) * 32;
-constexpr int kRing = 2;                         // pairs of blocks whose codes and scales are there or on their way
+constexpr int kMostRing = 3;                     // pairs of blocks whose codes and scales are there or on their way
 constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = 2 * (kCodeBytes + 512u);      // codes of both halves (INT3: 48 of 64 bytes a row), scales and zero points
 constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
-constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 256;     // ring, staging, largest |p|, barriers
+constexpr uint32_t kFixed = 2 * kYBytes + 512 + 256;     // staging, largest |p|, barriers
 constexpr uint32_t kSmemMost = 227 * 1024 - 1024;        // (the base is moved up to 1024 bytes)
-constexpr int kTagEpoch = 0, kTagDone = 1, kTagFirst = 4;        // words of the tag scratch, shared with fbq_dense.cu
-
 enum Mode { kGated, kKept, kGrad };
 
 struct EvenParams {
     int ranges;
+    const uint8_t *qw;
     const __half *scales, *zeros;
-    float *part;              // [range][half][tok][kHalf] sums of the tile that a range begins with and does not own
-    uint32_t *tags;           // see above; a word per range
+    float *part;              // [2 range + whether it holds the tile's first block][half][tok][kHalf]: a range has at most two shares
     float *kept_scales;
     int *status;
     int M, F, D, K;           // tokens, features, contraction, columns of W
     int tok, ntt, nkp, slab;  // tokens of a tile, token tiles, pairs of blocks of the contraction, blocks of the sub-branch
-    int stages, gate, kept_pitch;
+    int stages, ring, gate, kept_pitch;
     long long pairs;          // of all tiles
-    uint32_t wait_looks;
-    int test_skip_flag;
+    void *y;                  // of the adding launch: h or dx, codes
+    int8_t *kept;
 };
 
 // The pieces of a CTA's range: pairs of blocks [kp0, kp1) of a tile, and whether the tile is its own.
@@ -84,15 +81,9 @@ struct Pieces {
         return true;
     }
     __device__ __forceinline__ bool owner() const { return kp0 == 0; }
+    __device__ __forceinline__ bool whole() const { return kp0 == 0 && kp1 == nkp; }
 };
 
-__device__ __forceinline__ void store_release(uint32_t *p, uint32_t v) { asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory"); }
-__device__ __forceinline__ uint32_t load_acquire(const uint32_t *p)
-{
-    uint32_t v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
 __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t *v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
@@ -101,19 +92,6 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c0), "r"(c1), "r"(src) : "memory");
 }
-// Whole warp; bounded.
-__device__ __forceinline__ bool wait_tag(const EvenParams &p, const uint32_t *word, uint32_t tag, volatile int *quit)
-{
-    const unsigned long long t0 = global_ns();
-#pragma unroll 1
-    for (uint32_t look = 1;; ++look) {
-        if (__all_sync(0xffffffffu, load_acquire(word) == tag)) return true;
-        const bool end = *quit || (p.wait_looks && look >= p.wait_looks) || ((look & 63u) == 0u && global_ns() - t0 > kWaitNs);
-        if (__any_sync(0xffffffffu, end)) return false;
-        __nanosleep(64);
-    }
-}
-
 __device__ __forceinline__ uint32_t ldg_u16(const __half *p)
 {
     uint32_t v;
@@ -133,14 +111,16 @@ __device__ __forceinline__ uint4 lds128(uint32_t a)
     return v;
 }
 
-// Warps 2 and 3: the ring.  Scales and zero points lie 2 bytes here and there (an instruction touches as many lines as it has lanes),
+// Warps 2 and 3: the ring.  A lane's copies of a pair are 16 bytes each, neighbouring lanes' along a row; they count on the slot's barrier when
+// they have arrived.  Scales and zero points lie 2 bytes here and there (an instruction touches as many lines as it has lanes),
 // so each is loaded once per row and pair, kScaleAhead pairs before it is stored.
 template <int BITS, int MODE>
-__device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMap *qmap, int range, uint32_t ring, uint32_t rfull0, uint32_t rempty0, volatile int *quit)
+__device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint32_t ring, uint32_t rfull0, uint32_t rempty0, volatile int *quit)
 {
     constexpr bool GRAD = MODE == kGrad;
-    constexpr uint32_t kWords = BITS == 4 ? 16 : 12;
-    const int lane = threadIdx.x & 31, half = (int)(threadIdx.x >> 5) - 2, G = p.K / kGroupFast;
+    constexpr int kChunks = BITS == 4 ? 4 : 3;                   // 16-byte pieces of a group of a row
+    const int lane = threadIdx.x & 31, half = (int)(threadIdx.x >> 5) - 2, tid = 32 * half + lane, G = p.K / kGroupFast, rows_all = GRAD ? p.D : p.F;
+    const size_t row_bytes = (size_t)G * kChunks * 16;
     struct Scales {
         uint32_t v[8];
         bool on;
@@ -152,11 +132,11 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMa
     auto request = [&](Scales &c) {
         c.on = on;
         if (!on) return;
-        const int ft = 2 * (ahead.tile / p.ntt) + half, n0 = (GRAD ? kp : ft) * kHalf + lane, g = GRAD ? ft : kp, rows = g < G ? (GRAD ? p.D : p.F) : 0;
+        const int ft = 2 * (ahead.tile / p.ntt) + half, n0 = (GRAD ? kp : ft) * kHalf + lane, g = GRAD ? ft : kp, rows = g < G ? rows_all : 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const size_t at = (size_t)(n0 + 32 * i) * G + g;
-            c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros
+            c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros, whatever its codes
             if (n0 + 32 * i < rows) {
                 c.v[2 * i] = ldg_u16(p.scales + at);
                 c.v[2 * i + 1] = ldg_u16(p.zeros + at);
@@ -182,11 +162,18 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMa
             if (!c[i].on) return true;
             if (!__all_sync(0xffffffffu, first || umma::wait(rempty0 + 8u * slot, phase, quit))) return false;
             const uint32_t dst = ring + slot * kSlotBytes, bar = rfull0 + 8u * slot;
-            if (half == 0 && lane == 0) {
-                const int ft = 2 * (cur.tile / p.ntt);
-                mbar_expect_tx(bar, 2u * 128u * kWords * 4u);
-                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kCodeBytes, qmap, (GRAD ? ft + h : ck) * (int)kWords, (GRAD ? ck : ft + h) * kHalf, bar);
+            const int ft = 2 * (cur.tile / p.ntt), n0 = (GRAD ? ck : ft) * kHalf;
+            // piece e of the pair: forward [half][row][piece], the tile's rows one after another; Grad [row][half][piece], both groups of a row
+#pragma unroll 2
+            for (int k = 0; k < 4 * kChunks; ++k) {
+                const int e = tid + 64 * k, u = e / kChunks, piece = e - u * kChunks;
+                const int h = GRAD ? u & 1 : u >> 7, row = GRAD ? u >> 1 : u & 127;
+                const int n = min(n0 + (GRAD ? row : u), rows_all - 1), g = GRAD ? min(ft + h, G - 1) : ck;
+                const uint32_t to = dst + (uint32_t)h * kCodeBytes +
+                                    (BITS == 4 ? (uint32_t)row * 64u + (uint32_t)((piece ^ ((row >> 1) & 3)) << 4) : (uint32_t)row * 48u + (uint32_t)piece * 16u);
+                cp_async16(to, p.qw + (size_t)n * row_bytes + (size_t)g * (kChunks * 16) + piece * 16);
             }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * kCodeBytes + (uint32_t)(128 * half + lane + 32 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16)
@@ -198,7 +185,7 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, const CUtensorMa
                 cur.next();
                 ck = cur.kp0;
             }
-            if (++slot == kRing) { slot = 0; phase ^= 1u; first = false; }
+            if (++slot == (uint32_t)p.ring) { slot = 0; phase ^= 1u; first = false; }
         }
     }
 }
@@ -219,13 +206,13 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
     const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u + (uint32_t)part * 24u;
     Pieces pc(p, range);
     uint32_t s = 0, use = 0;                                     // stage of the next block, times it has been used
-    uint32_t q = 0;                                              // pairs so far
+    uint32_t slot = 0, rphase = 0;
     const uint32_t stages = (uint32_t)p.stages;
     auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
     while (pc.next()) {
         const int n = pc.kp1 - pc.kp0;
 #pragma unroll 1
-        for (int k = 0; k < n; ++k, ++q) {
+        for (int k = 0; k < n; ++k) {
             // the stage of this thread's block, and its use before this one (the sub-branch's blocks are waited for as well: a wait tells one
             // phase of a barrier from the next, not from the one after that)
             uint32_t st = s + (uint32_t)blk, u = use;
@@ -234,8 +221,8 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                 ++u;
             }
             {
-                const uint32_t slot = q % kRing, at = ring + slot * kSlotBytes + (uint32_t)group * kCodeBytes;
-                if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, (q / kRing) & 1u, quit))) return false;
+                const uint32_t at = ring + slot * kSlotBytes + (uint32_t)group * kCodeBytes;
+                if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, rphase, quit))) return false;
                 uint32_t c[2 * NW];
                 if constexpr (BITS == 4) {
                     const uint4 a = lds128(at + (src ^ (uint32_t)(part << 5))), b = lds128(at + (src ^ (uint32_t)(part << 5 | 16)));
@@ -275,6 +262,7 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                 s -= stages;
                 ++use;
             }
+            if (++slot == (uint32_t)p.ring) { slot = 0; rphase ^= 1u; }
         }
         if (pc.owner()) {                                        // the sub-branch's stages are made by copies
             for (int k = 0; k < p.slab; ++k) {
@@ -291,23 +279,23 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
 
 // xmap: x (Grad: dy) [M][D], boxes of 64 x tok rows; tmap: t (s) [M][rank_pad], the same boxes; bmap: B [F][rank], boxes 64 x 128 rows
 // (Grad: A [rank][F], 64 x 64, MN-major); all in the 128-byte swizzle.  ymap: h [M][F / 2], boxes of 16 rows x 64 columns (Grad: dx [M][F], x 128);
-// cmap, Kept: codes [M][F], 16 rows x 128.  qmap: packed codes [rows of W][words], boxes of 128 rows x one group (INT4: 64-byte swizzle).
+// cmap, Kept: codes [M][F], 16 rows x 128.
 template <int BITS, typename T, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
 even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap bmap,
-            const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap qmap, const EvenParams p)
+            const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap cmap, const EvenParams p)
 {
     constexpr bool GRAD = MODE == kGrad;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t sbase = smem_u32(smem), stage_bytes = kWBytes + (uint32_t)p.tok * (kBK * 2u), y_off = (uint32_t)p.stages * stage_bytes;
-    const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = kRing * kSlotBytes + 512u;
+    const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = (uint32_t)p.ring * kSlotBytes + 512u;
     const uint32_t full0 = ring + bars, empty0 = full0 + 8u * kMostStages, accf0 = empty0 + 8u * kMostStages, acce0 = accf0 + 16u, rfull0 = acce0 + 16u,
-                   rempty0 = rfull0 + 8u * kRing;
-    float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + kRing * kSlotBytes);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing);
+                   rempty0 = rfull0 + 8u * kMostRing;
+    float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + (uint32_t)p.ring * kSlotBytes);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kMostRing);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = p.ranges - 1 - (int)blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = (int)blockIdx.x;
     // accumulators in tensor memory: two of two halves where they fit
     const uint32_t wide = p.tok > 128 ? 256u : 128u;
     const int nbuf = p.tok > 128 ? 1 : 2;
@@ -318,8 +306,8 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             mbar_init(full0 + 8u * i, 1 + kGroupWarps);          // the copying lane, and four warps of either half
             mbar_init(empty0 + 8u * i, 1);
         }
-        for (int i = 0; i < kRing; ++i) {
-            mbar_init(rfull0 + 8u * i, 3);                       // the copy's lane and both loading warps
+        for (int i = 0; i < p.ring; ++i) {
+            mbar_init(rfull0 + 8u * i, 64 + 2);                  // every loading lane's copies, and both warps' scales
             mbar_init(rempty0 + 8u * i, 2 * kGroupWarps);
         }
         for (int i = 0; i < 2; ++i) {
@@ -334,7 +322,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             prefetch_tensormap(&tmap);
             prefetch_tensormap(&bmap);
         }
-        prefetch_tensormap(&qmap);
+
     }
     if (warp == 1) umma::tmem_alloc<1>(smem_u32(tmem_slot), 512u);
     umma::fence_before();
@@ -342,7 +330,6 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     umma::fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    uint32_t tag = 0;
 
     if (warp == 0) {
         // =================================================== copies
@@ -418,7 +405,6 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     } else if (warp >= 4 && warp < kDqWarp) {
         // =================================================== epilogue: lane = feature, column = token
         pdl_wait();
-        tag = load_acquire(p.tags + kTagEpoch) + 1u;
         const int wq = warp & 3;
         uint32_t it = 0, staged = 0;
 #pragma unroll 1
@@ -428,19 +414,11 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             if (!ok) break;
             umma::fence_after();
             const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, m_end = min(p.M, m0 + p.tok);
-            int others = 0;                                      // ranges behind this one that hold blocks of a tile of ours
-            if (pc.owner()) {
-                const long long tile_end = (long long)(pc.tile + 1) * p.nkp;
-                while (range + others + 1 < p.ranges && p.pairs * (range + others + 1) / p.ranges < tile_end) ++others;
-                for (int o = 1; o <= others && ok; ++o) ok = wait_tag(p, p.tags + kTagFirst + range + o, tag, quit);
-                if (others) ok = named_barrier_and(1, 128, ok);
-                if (!ok) break;
-            }
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
                 const uint32_t lanes = tmem + buf * 256u + h * wide + ((uint32_t)(32 * wq) << 16);
                 const int n = ft * kFeat + h * kHalf + 32 * wq + lane;
-                const size_t part_at = (size_t)(2 * range + h) * p.tok * kHalf + 32 * wq + lane;
+                const size_t part_at = ((size_t)(2 * range + pc.owner()) * 2 + h) * p.tok * kHalf + 32 * wq + lane;
 #pragma unroll 1
                 for (int c = 0; c < p.tok; c += 32) {
                     uint32_t v[32];
@@ -452,20 +430,11 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                         if (lane == 0) mbar_arrive(acce0 + 8u * buf);
                     }
                     if (m0 + c >= p.M) continue;
-                    if (!pc.owner()) {
+                    if (!pc.whole()) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
                             if (c + j < m_end - m0) __stcg(p.part + part_at + (size_t)(c + j) * kHalf, __uint_as_float(v[j]));
                         continue;
-                    }
-#pragma unroll 1
-                    for (int o = 1; o <= others; ++o) {
-                        const float *src = p.part + part_at + ((size_t)2 * o * p.tok + c) * kHalf;
-                        float e[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) e[j] = c + j < m_end - m0 ? __ldcg(src + (size_t)j * kHalf) : 0.f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + e[j]);
                     }
                     const uint32_t at = y_off + (staged & 1u) * kYBytes;
                     if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
@@ -513,17 +482,12 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     ++staged;
                 }
             }
-            if (!pc.owner()) {
-                __threadfence();
-                named_barrier_sync(1, 128);
-                if (threadIdx.x == 4 * 32 && !p.test_skip_flag) store_release(p.tags + kTagFirst + range, tag);
-            }
         }
         if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp >= kDqWarp) {
         ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, ring, full0, empty0, rfull0, rempty0, quit);
     } else {
-        ok = load_codes<BITS, MODE>(p, &qmap, range, ring, rfull0, rempty0, quit);
+        ok = load_codes<BITS, MODE>(p, range, ring, rfull0, rempty0, quit);
     }
     if (!ok) {
         *quit = 1;
@@ -536,12 +500,67 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         umma::fence_after();
         umma::tmem_free<1>(tmem, 512u);
     }
-    if (threadIdx.x == 4 * 32) {                                 // (this thread has waited for the launch before)
-        __threadfence();
-        if (atomicAdd(p.tags + kTagDone, 1u) == gridDim.x - 1) { // the last CTA: the next launch's tags are other ones
-            p.tags[kTagDone] = 0;
-            __threadfence();
-            p.tags[kTagEpoch] = tag;
+}
+
+// The tiles that several ranges share: a block adds eight tokens of one, a thread per feature, in order of the ranges.
+constexpr int kAddTok = 8;
+template <typename T, int MODE> __global__ void __launch_bounds__(kFeat) add_kernel(const EvenParams p)
+{
+    __shared__ uint32_t tops[kFeat / 32][kAddTok];
+    pdl_launch_dependents();
+    pdl_wait();                                                  // (all blocks, so that this launch is not through before the one before it)
+    const int tile = (int)blockIdx.x, c0 = (int)blockIdx.y * kAddTok, ft = tile / p.ntt, m0 = (tile - ft * p.ntt) * p.tok + c0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int count = min(min(kAddTok, p.tok - c0), p.M - m0);
+    // the ranges that hold the tile's first and last pair
+    const long long first = (long long)tile * p.nkp, last = first + p.nkp - 1;
+    const int r0 = (int)(((first + 1) * p.ranges - 1) / p.pairs), r1 = (int)(((last + 1) * p.ranges - 1) / p.pairs);
+    if (r0 == r1 || count <= 0) return;
+    const int half = threadIdx.x / kHalf, n = ft * kFeat + (int)threadIdx.x;
+    const float *src = p.part + ((size_t)half * p.tok + c0) * kHalf + threadIdx.x % kHalf;
+    const size_t slot = (size_t)2 * p.tok * kHalf;
+    float v[kAddTok];
+#pragma unroll
+    for (int j = 0; j < kAddTok; ++j) v[j] = j < count ? __ldcg(src + (2 * (size_t)r0 + 1) * slot + j * kHalf) : 0.f;
+#pragma unroll 2
+    for (int r = r0 + 1; r <= r1; ++r) {
+        float e[kAddTok];
+#pragma unroll
+        for (int j = 0; j < kAddTok; ++j) e[j] = j < count ? __ldcg(src + 2 * (size_t)r * slot + j * kHalf) : 0.f;
+#pragma unroll
+        for (int j = 0; j < kAddTok; ++j) v[j] += e[j];
+    }
+    if constexpr (MODE == kKept) {
+#pragma unroll
+        for (int j = 0; j < kAddTok; ++j) {
+            const uint32_t top = __reduce_max_sync(0xffffffffu, n < p.F ? __float_as_uint(v[j]) & 0x7FFFFFFFu : 0u);
+            if (lane == 0) tops[warp][j] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kAddTok; ++j) {
+            const uint32_t *t = &tops[warp & 4][j];
+            float scale, inverse;
+            kept_scale(max(max(t[0], t[kAddTok]), max(t[2 * kAddTok], t[3 * kAddTok])), scale, inverse);
+            if (j < count && n < p.F) {
+                p.kept[(size_t)(m0 + j) * p.F + n] = (int8_t)kept_code(v[j], inverse);
+                if (threadIdx.x % kHalf == 0) p.kept_scales[(size_t)(m0 + j) * p.kept_pitch + n / kKeptGroup] = scale;
+            }
+        }
+    }
+    T *y = static_cast<T *>(p.y);
+    if constexpr (MODE == kGrad) {
+#pragma unroll
+        for (int j = 0; j < kAddTok; ++j)
+            if (j < count && n < p.F) y[(size_t)(m0 + j) * p.F + n] = ActTraits<T>::from_float(v[j]);
+    } else {
+        // lanes eight apart swap halves of their tokens, so that each gates four
+        const bool up = (lane & kGateUp) != 0;
+        const int col = ft * (kFeat / 2) + warp * 16 + (lane >> 4) * kGateUp + (lane & (kGateUp - 1));
+#pragma unroll
+        for (int j = 0; j < kAddTok / 2; ++j) {
+            const float got = __shfl_xor_sync(0xffffffffu, up ? v[j] : v[j + kAddTok / 2], kGateUp), mine = up ? v[j + kAddTok / 2] : v[j];
+            const int t = up ? j + kAddTok / 2 : j;
+            if (t < count && n < p.F) y[(size_t)(m0 + t) * (p.F / 2) + col] = ActTraits<T>::from_float(gate_value(p.gate, up ? got : mine) * (up ? mine : got));
         }
     }
 }
@@ -566,7 +585,7 @@ long long all_pairs(int ntt, int F, int D) { return (long long)((F + kFeat - 1) 
 int ranges_for(long long pairs) { return (int)std::min<long long>(sms_of_device(), pairs); }
 
 template <int BITS, typename T, int MODE>
-cudaError_t start(const CUtensorMap (&maps)[6], const EvenParams &p, bool pdl, cudaStream_t s)
+cudaError_t start(const CUtensorMap (&maps)[5], const EvenParams &p, bool pdl, cudaStream_t s, int *launches)
 {
     auto kern = even_kernel<BITS, T, MODE>;
     static bool attr_set = false;
@@ -577,14 +596,22 @@ cudaError_t start(const CUtensorMap (&maps)[6], const EvenParams &p, bool pdl, c
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.ranges);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)p.stages * (kWBytes + p.tok * (kBK * 2u)) + kFixed + 1024;
+    cfg.dynamicSmemBytes = (size_t)p.stages * (kWBytes + p.tok * (kBK * 2u)) + p.ring * kSlotBytes + kFixed + 1024;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], p);
+    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, maps[0], maps[1], maps[2], maps[3], maps[4], p); e != cudaSuccess) return e;
+    ++*launches;
+    if (p.nkp == 1 || (p.pairs % p.ranges == 0 && p.pairs / p.ranges % p.nkp == 0)) return cudaSuccess;      // (every range is whole tiles)
+    cfg.gridDim = dim3((unsigned)(p.pairs / p.nkp), (unsigned)((p.tok + kAddTok - 1) / kAddTok));
+    cfg.blockDim = dim3(kFeat);
+    cfg.dynamicSmemBytes = 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, add_kernel<T, MODE>, p);
+    if (e == cudaSuccess) ++*launches;
+    return e;
 }
 
 }  // namespace
@@ -593,18 +620,17 @@ size_t even_part_bytes(int M, int F, int D)
 {
     int tok, ntt;
     token_tiles(M, &tok, &ntt);
-    return (size_t)ranges_for(all_pairs(ntt, F, D)) * tok * kFeat * sizeof(float);
+    return (size_t)2 * ranges_for(all_pairs(ntt, F, D)) * tok * kFeat * sizeof(float);
 }
-size_t even_tags() { return (size_t)kTagFirst + sms_of_device(); }
 
-cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches)
+cudaError_t launch_even(const EvenArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
 {
     const bool grad = a.gate < 0;
     EvenParams p{};
+    p.qw = reinterpret_cast<const uint8_t *>(a.qw);
     p.scales = a.scales; p.zeros = a.zeros;
     p.part = static_cast<float *>(a.part);
-    p.tags = ws.tags;
-    p.status = ws.counters + kCtrStatus;
+    p.status = status;
     p.M = a.M; p.K = a.K;
     p.F = grad ? a.K : a.N;
     p.D = grad ? a.N : a.K;
@@ -612,23 +638,24 @@ cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &t
     p.nkp = (p.D + 2 * kBK - 1) / (2 * kBK);
     const int rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.slab = rank_pad / kBK;
-    p.stages = (int)std::min<uint32_t>(kMostStages, (kSmemMost - kFixed) / (kWBytes + p.tok * (kBK * 2u)));
+    // three stages before the third slot of the ring
+    const uint32_t stage = kWBytes + p.tok * (kBK * 2u);
+    for (p.ring = kMostRing;; --p.ring) {
+        p.stages = (int)std::min<uint32_t>(kMostStages, (kSmemMost - kFixed - p.ring * kSlotBytes) / stage);
+        if (p.stages >= 3 || p.ring == 2) break;
+    }
     p.gate = a.gate;
     p.kept_scales = a.kept_scales;
     p.kept_pitch = (p.F + kKeptGroup - 1) / kKeptGroup;
     p.pairs = all_pairs(p.ntt, p.F, p.D);
     p.ranges = ranges_for(p.pairs);
-    p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
-    p.test_skip_flag = tune.test_skip_flag;
+    p.y = a.y;
+    p.kept = a.kept;
     const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B, none = CU_TENSOR_MAP_SWIZZLE_NONE;
     const int box = p.tok;
-    CUtensorMap maps[6];
+    CUtensorMap maps[5];
     cudaError_t e;
-    const int words = a.bits == 4 ? 16 : 12;
-    if ((e = cached_map(&maps[5], matrix_map(a.qw, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, (size_t)(a.K / kGroupFast) * words, a.N, words, 128,
-                                             a.bits == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : none))) != cudaSuccess)
-        return e;
     if ((e = encode_map(&maps[0], matrix_map(a.x, dt, 2, p.D, a.M, kBK, box, sw))) != cudaSuccess) return e;
     maps[1] = maps[2] = maps[0];
     if (a.rank > 0) {
@@ -642,12 +669,10 @@ cudaError_t launch_even(const EvenArgs &a, Workspace &ws, const PrefillTuning &t
     if (a.kept && (e = encode_map(&maps[4], matrix_map(a.kept, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.N, a.M, 128, 16, none))) != cudaSuccess) return e;
     auto go = [&](auto mode) {
         constexpr int MODE = decltype(mode)::value;
-        const bool pdl = tune.pdl != 0;
-        return a.bits == 4 ? (a.bf16 ? start<4, __nv_bfloat16, MODE>(maps, p, pdl, s) : start<4, __half, MODE>(maps, p, pdl, s))
-                           : (a.bf16 ? start<3, __nv_bfloat16, MODE>(maps, p, pdl, s) : start<3, __half, MODE>(maps, p, pdl, s));
+        return a.bits == 4 ? (a.bf16 ? start<4, __nv_bfloat16, MODE>(maps, p, pdl, s, launches) : start<4, __half, MODE>(maps, p, pdl, s, launches))
+                           : (a.bf16 ? start<3, __nv_bfloat16, MODE>(maps, p, pdl, s, launches) : start<3, __half, MODE>(maps, p, pdl, s, launches));
     };
     e = grad ? go(std::integral_constant<int, kGrad>{}) : a.kept ? go(std::integral_constant<int, kKept>{}) : go(std::integral_constant<int, kGated>{});
-    if (e == cudaSuccess) ++*launches;
     return e;
 }
 
