@@ -6,14 +6,13 @@
 //
 // Up to a few hundred tokens a weight is used too seldom to be dequantised in a pass of its own (the dense kernel's 16-bit copy costs 4
 // bytes a weight through L2 beside the half byte of its code), and tiles are fewer than SMs or fill a second wave badly.  So a CTA turns
-// codes into the operand in shared memory, 256 features for up to 192 tokens (128 features would read x twice as often, 64 bytes a clock and SM:
-// more than L2 gives all of them), and the pairs of blocks of all tiles, in order, are cut into equal ranges, one per CTA:
+// codes into the operand in shared memory, 128 features for up to 192 tokens, and the pairs of blocks of all tiles, in order, are cut into equal
+// ranges, one per CTA:
 //
-//   warps 2, 3   bring the packed codes of a pair of blocks, 2 x 128 rows x one quantisation group, and their scales and zero points (pieces of 48 or
-//                64 bytes: the copy engine takes 9 cycles for each, 46 us of 53 for 4096 -> 2 x 11008; asynchronous copies of lanes far less)
-//   warps 8-23   dequantise them, 64 codes a thread: eight warps for either half of the features, into two stages of the operands
+//   warps 2, 3   bring the packed codes of a pair of blocks, 128 rows x one quantisation group, and their scales and zero points
+//   warps 8-23   two groups of eight dequantise every other pair, 64 codes a thread, into two stages of the operands
 //   warp 0       copies the tokens by TMA, and both operands of the sub-branch's blocks
-//   warp 1       issues tcgen05.mma, 128 features x tokens x 16, for both halves
+//   warp 1       issues tcgen05.mma 128 features x tokens x 16
 //   warps 4-7    epilogue: a tile that is the range's own is written; of one that several ranges share each stores its fp32 sums
 //
 // and a second launch adds the shares of each such tile in order of the contraction, gates and writes it: nobody waits for another
@@ -24,8 +23,9 @@
 // Forward, features are rows of W and the operand is K-major: a pair of blocks is one group of each row.  Grad, features are its columns,
 // 128 of them one group; a pair of blocks is 128 rows of it, and the operand is MN-major: rows are written as they lie.
 //
-// (Pairs of CTAs with cta_group::2 and half the tokens each were built as well: the dequantising warps' fence towards the asynchronous proxy
-// then took 1500 cycles instead of 150, 77 tokens of 4096 -> 2 x 11008 41 us.)
+// What a pair of blocks passes through (codes, operand, MMAs, free again) takes some 2500 cycles and the warps are through with one in 600, so
+// what counts is how many are on their way.  256 features a CTA, which reads x half as often, leaves room for one and a half pairs: 77 tokens of
+// 4096 -> 2 x 11008 38 us.  Pairs of CTAs with cta_group::2 were slower still (the dequantising warps' fence towards the asynchronous proxy).
 #include <algorithm>
 #include <type_traits>
 
@@ -39,15 +39,15 @@ namespace fbq {
 namespace {
 using namespace ptx;
 
-constexpr int kBK = 64, kHalf = 128, kFeat = 2 * kHalf;
-constexpr uint32_t kHalfBytes = kHalf * kBK * 2u, kWBytes = 2 * kHalfBytes, kBox = kHalfBytes / 2;
-constexpr int kMostTok = 192, kMostStages = 6;
+constexpr int kBK = 64, kFeat = 128;
+constexpr uint32_t kWBytes = kFeat * kBK * 2u, kBox = kWBytes / 2;
+constexpr int kMostTok = 192, kMostStages = 8;
 constexpr int kDqWarp = 8, kGroupWarps = 8, kThreads = (kDqWarp + 2 * kGroupWarps) * 32;
-constexpr int kMostRing = 3;                     // pairs of blocks whose codes and scales are there or on their way
-constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = 2 * (kCodeBytes + 512u);      // codes of both halves (INT3: 48 of 64 bytes a row), scales and zero points
+constexpr int kRing = 3;                         // pairs of blocks whose codes and scales are there or on their way
+constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = kCodeBytes + 512u;      // codes (INT3: 48 of 64 bytes a row), scales and zero points
 constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
-constexpr uint32_t kFixed = 2 * kYBytes + 512 + 256;     // staging, largest |p|, barriers
+constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 256;     // ring, staging, largest |p|, barriers
 constexpr uint32_t kSmemMost = 227 * 1024 - 1024;        // (the base is moved up to 1024 bytes)
 enum Mode { kGated, kKept, kGrad };
 
@@ -55,12 +55,12 @@ struct EvenParams {
     int ranges;
     const uint8_t *qw;
     const __half *scales, *zeros;
-    float *part;              // [2 range + whether it holds the tile's first block][half][tok][kHalf]: a range has at most two shares
+    float *part;              // [2 range + whether it holds the tile's first block][tok][kFeat]: a range has at most two shares
     float *kept_scales;
     int *status;
     int M, F, D, K;           // tokens, features, contraction, columns of W
     int tok, ntt, nkp, slab;  // tokens of a tile, token tiles, pairs of blocks of the contraction, blocks of the sub-branch
-    int stages, ring, gate, kept_pitch;
+    int stages, gate, kept_pitch;
     long long pairs;          // of all tiles
     void *y;                  // of the adding launch: h or dx, codes
     int8_t *kept;
@@ -119,10 +119,10 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint3
 {
     constexpr bool GRAD = MODE == kGrad;
     constexpr int kChunks = BITS == 4 ? 4 : 3;                   // 16-byte pieces of a group of a row
-    const int lane = threadIdx.x & 31, half = (int)(threadIdx.x >> 5) - 2, tid = 32 * half + lane, G = p.K / kGroupFast, rows_all = GRAD ? p.D : p.F;
+    const int lane = threadIdx.x & 31, tid = (int)threadIdx.x - 64, G = p.K / kGroupFast, rows_all = GRAD ? p.D : p.F;
     const size_t row_bytes = (size_t)G * kChunks * 16;
     struct Scales {
-        uint32_t v[8];
+        uint32_t v[4];
         bool on;
     };
     Pieces ahead(p, range);
@@ -132,12 +132,12 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint3
     auto request = [&](Scales &c) {
         c.on = on;
         if (!on) return;
-        const int ft = 2 * (ahead.tile / p.ntt) + half, n0 = (GRAD ? kp : ft) * kHalf + lane, g = GRAD ? ft : kp, rows = g < G ? rows_all : 0;
+        const int ft = ahead.tile / p.ntt, n0 = (GRAD ? kp : ft) * 128 + tid, g = GRAD ? ft : kp;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const size_t at = (size_t)(n0 + 32 * i) * G + g;
+        for (int i = 0; i < 2; ++i) {
+            const size_t at = (size_t)(n0 + 64 * i) * G + g;
             c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros, whatever its codes
-            if (n0 + 32 * i < rows) {
+            if (n0 + 64 * i < rows_all) {
                 c.v[2 * i] = ldg_u16(p.scales + at);
                 c.v[2 * i + 1] = ldg_u16(p.zeros + at);
             }
@@ -162,22 +162,18 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint3
             if (!c[i].on) return true;
             if (!__all_sync(0xffffffffu, first || umma::wait(rempty0 + 8u * slot, phase, quit))) return false;
             const uint32_t dst = ring + slot * kSlotBytes, bar = rfull0 + 8u * slot;
-            const int ft = 2 * (cur.tile / p.ntt), n0 = (GRAD ? ck : ft) * kHalf;
-            // piece e of the pair: forward [half][row][piece], the tile's rows one after another; Grad [row][half][piece], both groups of a row
+            const int ft = cur.tile / p.ntt, n0 = (GRAD ? ck : ft) * 128;
+            const uint8_t *src = p.qw + (size_t)(GRAD ? ft : ck) * (kChunks * 16);
 #pragma unroll 2
-            for (int k = 0; k < 4 * kChunks; ++k) {
-                const int e = tid + 64 * k, u = e / kChunks, piece = e - u * kChunks;
-                const int h = GRAD ? u & 1 : u >> 7, row = GRAD ? u >> 1 : u & 127;
-                const int n = min(n0 + (GRAD ? row : u), rows_all - 1), g = GRAD ? min(ft + h, G - 1) : ck;
-                const uint32_t to = dst + (uint32_t)h * kCodeBytes +
-                                    (BITS == 4 ? (uint32_t)row * 64u + (uint32_t)((piece ^ ((row >> 1) & 3)) << 4) : (uint32_t)row * 48u + (uint32_t)piece * 16u);
-                cp_async16(to, p.qw + (size_t)n * row_bytes + (size_t)g * (kChunks * 16) + piece * 16);
+            for (int k = 0; k < 2 * kChunks; ++k) {              // pieces [row][piece]
+                const int e = tid + 64 * k, row = e / kChunks, piece = e - row * kChunks;
+                const uint32_t to = dst + (BITS == 4 ? (uint32_t)row * 64u + (uint32_t)((piece ^ ((row >> 1) & 3)) << 4) : (uint32_t)row * 48u + (uint32_t)piece * 16u);
+                cp_async16(to, src + (size_t)min(n0 + row, rows_all - 1) * row_bytes + piece * 16);
             }
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + 2 * kCodeBytes + (uint32_t)(128 * half + lane + 32 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16)
-                             : "memory");
+            for (int k = 0; k < 2; ++k)
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kCodeBytes + (uint32_t)(tid + 64 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16) : "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
             request(c[i]);
@@ -185,7 +181,7 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint3
                 cur.next();
                 ck = cur.kp0;
             }
-            if (++slot == (uint32_t)p.ring) { slot = 0; phase ^= 1u; first = false; }
+            if (++slot == kRing) { slot = 0; phase ^= 1u; first = false; }
         }
     }
 }
@@ -202,26 +198,29 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
     // 128-byte swizzle, as they load them from different banks (INT4: the 64-byte swizzle of the copy).
     const int row = 32 * (w & 3) + lane, part = w >> 2, blk = GRAD ? row >> 6 : part;
     const uint32_t r = GRAD ? row & 63 : row;
-    const uint32_t dst = sbase + (uint32_t)group * kHalfBytes + (GRAD ? (uint32_t)part * kBox : 0u) + r * 128u + ((r & 7u) << 4);          // unit j: ^ (j << 4)
+    const uint32_t dst = sbase + (GRAD ? (uint32_t)part * kBox : 0u) + r * 128u + ((r & 7u) << 4);          // unit j: ^ (j << 4)
     const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u + (uint32_t)part * 24u;
     Pieces pc(p, range);
     uint32_t s = 0, use = 0;                                     // stage of the next block, times it has been used
-    uint32_t slot = 0, rphase = 0;
+    uint32_t slot = 0, rphase = 0;                               // of the ring
+    int turn = 0;                                                // whose pair it is
     const uint32_t stages = (uint32_t)p.stages;
     auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
     while (pc.next()) {
         const int n = pc.kp1 - pc.kp0;
 #pragma unroll 1
         for (int k = 0; k < n; ++k) {
-            // the stage of this thread's block, and its use before this one (the sub-branch's blocks are waited for as well: a wait tells one
-            // phase of a barrier from the next, not from the one after that)
+            // the stage of this thread's block, and its use before this one.  The other group's pairs and the sub-branch's blocks are waited
+            // for as well: a wait tells one phase of a barrier from the next, not from the one after that.
             uint32_t st = s + (uint32_t)blk, u = use;
             if (st >= stages) {
                 st -= stages;
                 ++u;
             }
-            {
-                const uint32_t at = ring + slot * kSlotBytes + (uint32_t)group * kCodeBytes;
+            if (turn != group) {
+                if (!free_again(st, u)) return false;
+            } else {
+                const uint32_t at = ring + slot * kSlotBytes;
                 if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, rphase, quit))) return false;
                 uint32_t c[2 * NW];
                 if constexpr (BITS == 4) {
@@ -237,7 +236,7 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                     }
                 }
                 uint32_t sz;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(ring + slot * kSlotBytes + 2 * kCodeBytes + (uint32_t)(128 * group + row) * 4u) : "memory");
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(at + kCodeBytes + (uint32_t)row * 4u) : "memory");
                 const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
                 const uint32_t to = dst + st * stage_bytes;
 #pragma unroll
@@ -262,7 +261,8 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                 s -= stages;
                 ++use;
             }
-            if (++slot == (uint32_t)p.ring) { slot = 0; rphase ^= 1u; }
+            turn ^= 1;
+            if (++slot == kRing) { slot = 0; rphase ^= 1u; }
         }
         if (pc.owner()) {                                        // the sub-branch's stages are made by copies
             for (int k = 0; k < p.slab; ++k) {
@@ -289,26 +289,23 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t sbase = smem_u32(smem), stage_bytes = kWBytes + (uint32_t)p.tok * (kBK * 2u), y_off = (uint32_t)p.stages * stage_bytes;
-    const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = (uint32_t)p.ring * kSlotBytes + 512u;
+    const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = kRing * kSlotBytes + 512u;
     const uint32_t full0 = ring + bars, empty0 = full0 + 8u * kMostStages, accf0 = empty0 + 8u * kMostStages, acce0 = accf0 + 16u, rfull0 = acce0 + 16u,
-                   rempty0 = rfull0 + 8u * kMostRing;
-    float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + (uint32_t)p.ring * kSlotBytes);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kMostRing);
+                   rempty0 = rfull0 + 8u * kRing;
+    float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + kRing * kSlotBytes);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = (int)blockIdx.x;
-    // accumulators in tensor memory: two of two halves where they fit
-    const uint32_t wide = p.tok > 128 ? 256u : 128u;
-    const int nbuf = p.tok > 128 ? 1 : 2;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) {
-            mbar_init(full0 + 8u * i, 1 + kGroupWarps);          // the copying lane, and four warps of either half
+            mbar_init(full0 + 8u * i, 1 + kGroupWarps / 2);      // the copying lane, and the four warps that make a block
             mbar_init(empty0 + 8u * i, 1);
         }
-        for (int i = 0; i < p.ring; ++i) {
+        for (int i = 0; i < kRing; ++i) {
             mbar_init(rfull0 + 8u * i, 64 + 2);                  // every loading lane's copies, and both warps' scales
-            mbar_init(rempty0 + 8u * i, 2 * kGroupWarps);
+            mbar_init(rempty0 + 8u * i, kGroupWarps);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(accf0 + 8u * i, 1);
@@ -351,11 +348,11 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     tma_load_2d(xt, mine ? &xmap : &tmap, c0, m0, bar);
                     if (!mine) {
                         if (GRAD) {
-                            for (int h = 0; h < 4; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
+                            for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
                         } else {
-                            for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kHalfBytes, &bmap, c0, ft * kFeat + kHalf * h, bar);
+                            tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
                         }
-                        for (int k = 0; k < kGroupWarps; ++k) mbar_arrive(bar);          // (for the warps that have nothing to make)
+                        for (int k = 0; k < kGroupWarps / 2; ++k) mbar_arrive(bar);      // (for the warps that have nothing to make)
                     }
                     if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
                 }
@@ -365,13 +362,13 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     } else if (warp == 1) {
         // =================================================== MMAs
         // The whole warp walks the loop and one elected lane issues: the MMAs' operands stay in uniform registers.  Two blocks at a time.
-        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kHalf, (uint32_t)p.tok) | (GRAD ? umma::kIdescMnA : 0u);
+        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kFeat, (uint32_t)p.tok) | (GRAD ? umma::kIdescMnA : 0u);
         const uint32_t wstep = GRAD ? 2048u >> 4 : 2u;
         const uint64_t wd0 = GRAD ? umma::desc_mn128(sbase, kBox) : umma::desc_k128(sbase), xd0 = umma::desc_k128(sbase + kWBytes);
         uint32_t s = 0, phase = 0, it = 0;
 #pragma unroll 1
         for (Pieces pc(p, range); ok && pc.next(); ++it) {
-            const uint32_t buf = nbuf == 2 ? it & 1u : 0u, use = nbuf == 2 ? it >> 1 : it, d = tmem + buf * 256u;
+            const uint32_t buf = it & 1u, use = it >> 1, d = tmem + buf * 256u;
             ok = __all_sync(0xffffffffu, use == 0 || umma::wait(acce0 + 8u * buf, (use - 1u) & 1u, quit));
             const int n = 2 * (pc.kp1 - pc.kp0) + (pc.owner() ? p.slab : 0);
 #pragma unroll 1
@@ -386,9 +383,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     auto block = [&](uint32_t stage, bool more) {
                         const uint64_t wd = wd0 + stage * (stage_bytes >> 4), xd = xd0 + stage * (stage_bytes >> 4);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int j = 0; j < kBK / 16; ++j) umma::mma(d + h * wide, wd + h * (kHalfBytes >> 4) + wstep * j, xd + 2 * j, idesc, more || j > 0);
+                        for (int j = 0; j < kBK / 16; ++j) umma::mma(d, wd + wstep * j, xd + 2 * j, idesc, more || j > 0);
                         umma::commit(empty0 + 8u * stage);
                     };
                     block(s0, i > 0);
@@ -409,22 +404,21 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         uint32_t it = 0, staged = 0;
 #pragma unroll 1
         for (Pieces pc(p, range); ok && pc.next(); ++it) {
-            const uint32_t buf = nbuf == 2 ? it & 1u : 0u, use = nbuf == 2 ? it >> 1 : it;
+            const uint32_t buf = it & 1u, use = it >> 1;
             ok = named_barrier_and(1, 128, umma::wait(accf0 + 8u * buf, use & 1u, quit));      // (four warps go on, or none)
             if (!ok) break;
             umma::fence_after();
             const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, m_end = min(p.M, m0 + p.tok);
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const uint32_t lanes = tmem + buf * 256u + h * wide + ((uint32_t)(32 * wq) << 16);
-                const int n = ft * kFeat + h * kHalf + 32 * wq + lane;
-                const size_t part_at = ((size_t)(2 * range + pc.owner()) * 2 + h) * p.tok * kHalf + 32 * wq + lane;
+            {
+                const uint32_t lanes = tmem + buf * 256u + ((uint32_t)(32 * wq) << 16);
+                const int n = ft * kFeat + 32 * wq + lane;
+                const size_t part_at = (size_t)(2 * range + pc.owner()) * p.tok * kFeat + 32 * wq + lane;
 #pragma unroll 1
                 for (int c = 0; c < p.tok; c += 32) {
                     uint32_t v[32];
                     umma::ld32(lanes + (uint32_t)c, v);
                     umma::wait_ld();
-                    if (h == 1 && c + 32 >= p.tok) {             // all of the accumulators is in registers
+                    if (c + 32 >= p.tok) {                       // all of the accumulator is in registers
                         umma::fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(acce0 + 8u * buf);
@@ -433,7 +427,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     if (!pc.whole()) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (c + j < m_end - m0) __stcg(p.part + part_at + (size_t)(c + j) * kHalf, __uint_as_float(v[j]));
+                            if (c + j < m_end - m0) __stcg(p.part + part_at + (size_t)(c + j) * kFeat, __uint_as_float(v[j]));
                         continue;
                     }
                     const uint32_t at = y_off + (staged & 1u) * kYBytes;
@@ -455,13 +449,13 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     } else {
                         gate_chunk<T>(p.gate, v, reinterpret_cast<T *>(smem + at) + 16 * wq);
                     }
-                    if constexpr (MODE == kKept) {               // a half's 128 rows are the columns that share a scale
+                    if constexpr (MODE == kKept) {               // a tile's 128 rows are the columns that share a scale
                         uint32_t top = 0u;
 #pragma unroll
                         for (int w = 0; w < 4; ++w) top = max(top, __float_as_uint(amax[32 * w + lane]));
                         float scale, inverse;
                         kept_scale(top, scale, inverse);
-                        if (wq == 0 && n - lane < p.F && lane < m_end - (m0 + c)) p.kept_scales[(size_t)(m0 + c + lane) * p.kept_pitch + 2 * ft + h] = scale;
+                        if (wq == 0 && n - lane < p.F && lane < m_end - (m0 + c)) p.kept_scales[(size_t)(m0 + c + lane) * p.kept_pitch + ft] = scale;
                         uint8_t *codes = smem + at + kYBytes / 2 + 32 * wq + lane;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) codes[j * 128] = (uint8_t)kept_code(__uint_as_float(v[j]), __shfl_sync(0xffffffffu, inverse, j));
@@ -469,7 +463,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     fence_proxy_async();
                     named_barrier_sync(1, 128);
                     if (threadIdx.x == 4 * 32 && n < p.F) {
-                        const int out = GRAD ? n : n / 2;        // (lane 0's n is the half's first)
+                        const int out = GRAD ? n : n / 2;        // (lane 0's n is the tile's first)
                         const bool both = c + 16 < p.tok && m0 + c + 16 < m_end;
                         tma_store_2d(&ymap, sbase + at, out, m0 + c);
                         if (both) tma_store_2d(&ymap, sbase + at + kYBytes / (GRAD ? 2 : 4), out, m0 + c + 16);
@@ -515,17 +509,17 @@ template <typename T, int MODE> __global__ void __launch_bounds__(kFeat) add_ker
     const long long first = (long long)tile * p.nkp, last = first + p.nkp - 1;
     const int r0 = (int)(((first + 1) * p.ranges - 1) / p.pairs), r1 = (int)(((last + 1) * p.ranges - 1) / p.pairs);
     if (r0 == r1 || count <= 0) return;
-    const int half = threadIdx.x / kHalf, n = ft * kFeat + (int)threadIdx.x;
-    const float *src = p.part + ((size_t)half * p.tok + c0) * kHalf + threadIdx.x % kHalf;
-    const size_t slot = (size_t)2 * p.tok * kHalf;
+    const int n = ft * kFeat + (int)threadIdx.x;
+    const float *src = p.part + (size_t)c0 * kFeat + threadIdx.x;
+    const size_t slot = (size_t)p.tok * kFeat;
     float v[kAddTok];
 #pragma unroll
-    for (int j = 0; j < kAddTok; ++j) v[j] = j < count ? __ldcg(src + (2 * (size_t)r0 + 1) * slot + j * kHalf) : 0.f;
+    for (int j = 0; j < kAddTok; ++j) v[j] = j < count ? __ldcg(src + (2 * (size_t)r0 + 1) * slot + j * kFeat) : 0.f;
 #pragma unroll 2
     for (int r = r0 + 1; r <= r1; ++r) {
         float e[kAddTok];
 #pragma unroll
-        for (int j = 0; j < kAddTok; ++j) e[j] = j < count ? __ldcg(src + 2 * (size_t)r * slot + j * kHalf) : 0.f;
+        for (int j = 0; j < kAddTok; ++j) e[j] = j < count ? __ldcg(src + 2 * (size_t)r * slot + j * kFeat) : 0.f;
 #pragma unroll
         for (int j = 0; j < kAddTok; ++j) v[j] += e[j];
     }
@@ -538,12 +532,12 @@ template <typename T, int MODE> __global__ void __launch_bounds__(kFeat) add_ker
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kAddTok; ++j) {
-            const uint32_t *t = &tops[warp & 4][j];
+            const uint32_t *t = &tops[0][j];
             float scale, inverse;
             kept_scale(max(max(t[0], t[kAddTok]), max(t[2 * kAddTok], t[3 * kAddTok])), scale, inverse);
             if (j < count && n < p.F) {
                 p.kept[(size_t)(m0 + j) * p.F + n] = (int8_t)kept_code(v[j], inverse);
-                if (threadIdx.x % kHalf == 0) p.kept_scales[(size_t)(m0 + j) * p.kept_pitch + n / kKeptGroup] = scale;
+                if (threadIdx.x == 0) p.kept_scales[(size_t)(m0 + j) * p.kept_pitch + n / kKeptGroup] = scale;
             }
         }
     }
@@ -596,7 +590,7 @@ cudaError_t start(const CUtensorMap (&maps)[5], const EvenParams &p, bool pdl, c
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.ranges);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)p.stages * (kWBytes + p.tok * (kBK * 2u)) + p.ring * kSlotBytes + kFixed + 1024;
+    cfg.dynamicSmemBytes = (size_t)p.stages * (kWBytes + p.tok * (kBK * 2u)) + kFixed + 1024;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -638,12 +632,7 @@ cudaError_t launch_even(const EvenArgs &a, int *status, bool pdl, cudaStream_t s
     p.nkp = (p.D + 2 * kBK - 1) / (2 * kBK);
     const int rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.slab = rank_pad / kBK;
-    // three stages before the third slot of the ring
-    const uint32_t stage = kWBytes + p.tok * (kBK * 2u);
-    for (p.ring = kMostRing;; --p.ring) {
-        p.stages = (int)std::min<uint32_t>(kMostStages, (kSmemMost - kFixed - p.ring * kSlotBytes) / stage);
-        if (p.stages >= 3 || p.ring == 2) break;
-    }
+    p.stages = (int)std::min<uint32_t>(kMostStages, (kSmemMost - kFixed) / (kWBytes + p.tok * (kBK * 2u)));
     p.gate = a.gate;
     p.kept_scales = a.kept_scales;
     p.kept_pitch = (p.F + kKeptGroup - 1) / kKeptGroup;
@@ -660,7 +649,7 @@ cudaError_t launch_even(const EvenArgs &a, int *status, bool pdl, cudaStream_t s
     maps[1] = maps[2] = maps[0];
     if (a.rank > 0) {
         if ((e = encode_map(&maps[1], matrix_map(a.thin, dt, 2, rank_pad, a.M, kBK, box, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&maps[2], grad ? matrix_map(a.factor, dt, 2, a.K, a.rank, kBK, kBK, sw) : matrix_map(a.factor, dt, 2, a.rank, a.N, kBK, kHalf, sw))) !=
+        if ((e = cached_map(&maps[2], grad ? matrix_map(a.factor, dt, 2, a.K, a.rank, kBK, kBK, sw) : matrix_map(a.factor, dt, 2, a.rank, a.N, kBK, kFeat, sw))) !=
             cudaSuccess)
             return e;
     }
