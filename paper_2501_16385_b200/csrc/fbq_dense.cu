@@ -453,14 +453,15 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
         }
     } else if (warp == 1) {
         // =================================================== MMAs
-        if (cr == 0 && lane == 0) {
+        // The leader's whole warp walks the loop and one elected lane issues: the MMAs' operands stay in uniform registers.
+        if (cr == 0) {
             uint32_t s = 0, phase = 0, it = 0;
             const uint64_t desc0 = umma::desc_k128(sbase);
 #pragma unroll 1
             for (; ok; ++it) {
                 const int q = tile_at(it, tfull0, tiles, quit);
                 if (q < 0) ok = false;
-                if (q < 0 || q >= n_all) break;
+                if (!__all_sync(0xffffffffu, q >= 0 && q < n_all)) break;
                 const bool t2_role = GRAD && q >= n_main, t_role = q < p.n_t || t2_role, mn = GRAD && !t2_role;
                 const int nkb = t2_role ? p.K_all / kBK : t_role ? kbx : kbx + slab;
                 const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, 2 * 128, (uint32_t)(t_role ? kTTok : p.tok)) | (mn ? umma::kIdescMnA : 0u);
@@ -468,28 +469,34 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                 const uint32_t wstep = mn ? 2048u >> 4 : 2u;
                 const uint64_t wdesc0 = mn ? umma::desc_mn128(sbase, kBoxBytes) : desc0;
                 const uint32_t buf = it & 1u, d = tmem + buf * 256u;
-                if (it >= 2 && !umma::wait_cluster(acce0 + 8u * buf, ((it >> 1) - 1u) & 1u, quit)) { ok = false; break; }
+                ok = __all_sync(0xffffffffu, it < 2 || umma::wait_cluster(acce0 + 8u * buf, ((it >> 1) - 1u) & 1u, quit));
+                if (!ok) break;
                 umma::fence_after();
                 bool there = mbar_try_wait(full0 + 8u * s, phase) != 0;
 #pragma unroll 1
                 for (int kb = 0; kb < nkb; kb += kPer) {
-                    if (!there && !umma::wait_cluster(full0 + 8u * s, phase, quit)) { ok = false; break; }
+                    ok = __all_sync(0xffffffffu, there || umma::wait_cluster(full0 + 8u * s, phase, quit));
+                    if (!ok) break;
                     umma::fence_after();
                     const uint64_t wd = wdesc0 + s * (kStageBytes >> 4), xd = desc0 + s * (kStageBytes >> 4) + (kHalfBytes >> 4);
                     const uint32_t freed = empty0 + 8u * s;
                     if (++s == kStages) { s = 0; phase ^= 1u; }
-                    umma::mma_pair(d, wd, xd, idesc, kb ? 1u : 0u);
+                    if (umma::elect_one()) {
+                        umma::mma_pair(d, wd, xd, idesc, kb ? 1u : 0u);
 #pragma unroll
-                    for (int j = 1; j < kBK / 16; ++j) umma::mma_pair(d, wd + wstep * j, xd + 2 * j, idesc, 1u);
-                    if (kb + 1 < nkb) {
-                        const uint64_t w2 = wd + (kBlockBytes >> 4), x2 = xd + (kBlockBytes >> 4);
+                        for (int j = 1; j < kBK / 16; ++j) umma::mma_pair(d, wd + wstep * j, xd + 2 * j, idesc, 1u);
+                        if (kb + 1 < nkb) {
+                            const uint64_t w2 = wd + (kBlockBytes >> 4), x2 = xd + (kBlockBytes >> 4);
 #pragma unroll
-                        for (int j = 0; j < kBK / 16; ++j) umma::mma_pair(d, w2 + wstep * j, x2 + 2 * j, idesc, 1u);
+                            for (int j = 0; j < kBK / 16; ++j) umma::mma_pair(d, w2 + wstep * j, x2 + 2 * j, idesc, 1u);
+                        }
+                        umma::commit_pair(freed);
+                        if (kb + kPer >= nkb) umma::commit_pair(accf0 + 8u * buf);
                     }
-                    umma::commit_pair(freed);
+                    __syncwarp();
                     there = mbar_try_wait(full0 + 8u * s, phase) != 0;
                 }
-                if (ok) umma::commit_pair(accf0 + 8u * buf);
+                if (!ok) break;
             }
         }
     } else if (warp == 2) {

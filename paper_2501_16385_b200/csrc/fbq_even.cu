@@ -9,8 +9,9 @@
 // codes into the operand in shared memory, 128 features for up to 192 tokens, and the pairs of blocks of all tiles, in order, are cut into equal
 // ranges, one per CTA:
 //
-//   warps 2, 3   bring the packed codes of a pair of blocks, 128 rows x one quantisation group, and their scales and zero points
-//   warps 8-23   two groups of eight dequantise every other pair, 64 codes a thread, into two stages of the operands
+//   warp 2       copies the packed codes of a pair of blocks, 128 rows x one quantisation group, warp 3 their scales and zero points
+//   warps 8-23   four groups of four dequantise a pair in turn, a row's 128 codes a thread, into two stages of the operands (of some 2500 cycles that
+//                a group then takes, half go into waits, fences and loops; two groups of eight with 64 codes a thread: 34 us for 77 tokens, 27 so)
 //   warp 0       copies the tokens by TMA, and both operands of the sub-branch's blocks
 //   warp 1       issues tcgen05.mma 128 features x tokens x 16
 //   warps 4-7    epilogue: a tile that is the range's own is written; of one that several ranges share each stores its fp32 sums
@@ -42,8 +43,8 @@ using namespace ptx;
 constexpr int kBK = 64, kFeat = 128;
 constexpr uint32_t kWBytes = kFeat * kBK * 2u, kBox = kWBytes / 2;
 constexpr int kMostTok = 192, kMostStages = 8;
-constexpr int kDqWarp = 8, kGroupWarps = 8, kThreads = (kDqWarp + 2 * kGroupWarps) * 32;
-constexpr int kRing = 3;                         // pairs of blocks whose codes and scales are there or on their way
+constexpr int kDqWarp = 8, kGroups = 4, kGroupWarps = 4, kThreads = (kDqWarp + kGroups * kGroupWarps) * 32;
+constexpr int kRing = 4;                         // pairs of blocks whose codes and scales are there or on their way
 constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = kCodeBytes + 512u;      // codes (INT3: 48 of 64 bytes a row), scales and zero points
 constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
@@ -98,12 +99,6 @@ __device__ __forceinline__ uint32_t ldg_u16(const __half *p)
     asm volatile("ld.global.nc.u16 %0, [%1];" : "=r"(v) : "l"(p));
     return v;
 }
-__device__ __forceinline__ uint2 lds_v2(uint32_t a)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint4 lds128(uint32_t a)
 {
     uint4 v;
@@ -111,48 +106,118 @@ __device__ __forceinline__ uint4 lds128(uint32_t a)
     return v;
 }
 
-// Warps 2 and 3: the ring.  A lane's copies of a pair are 16 bytes each, neighbouring lanes' along a row; they count on the slot's barrier when
-// they have arrived.  Scales and zero points lie 2 bytes here and there (an instruction touches as many lines as it has lanes),
-// so each is loaded once per row and pair, kScaleAhead pairs before it is stored.
+// Where a ring's pair begins: row n0 of W, group g.  A warp alone runs on its instructions' latencies, some 500 cycles for a hundred of them, and a
+// pair has that long: what changes from pair to pair is a step, the rest is worked out once per piece.
+template <int MODE> struct Walk {
+    Pieces pc;
+    int kp, n0, g;
+    bool on, opened;
+    __device__ __forceinline__ Walk(const EvenParams &p, int range) : pc(p, range) { open(p); }
+    __device__ __forceinline__ void open(const EvenParams &p)
+    {
+        on = pc.next();
+        opened = true;
+        const int ft = pc.tile / p.ntt;
+        kp = pc.kp0;
+        n0 = (MODE == kGrad ? kp : ft) * 128;
+        g = MODE == kGrad ? ft : kp;
+    }
+    __device__ __forceinline__ void step(const EvenParams &p)
+    {
+        opened = false;
+        if (MODE == kGrad) n0 += 128;
+        else ++g;
+        if (++kp == pc.kp1) open(p);
+    }
+};
+
+// Warp 2: codes, 16 bytes a lane and copy, neighbouring lanes' along a row; they count on the slot's barrier when they have arrived.
 template <int BITS, int MODE>
 __device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint32_t ring, uint32_t rfull0, uint32_t rempty0, volatile int *quit)
 {
-    constexpr bool GRAD = MODE == kGrad;
-    constexpr int kChunks = BITS == 4 ? 4 : 3;                   // 16-byte pieces of a group of a row
-    const int lane = threadIdx.x & 31, tid = (int)threadIdx.x - 64, G = p.K / kGroupFast, rows_all = GRAD ? p.D : p.F;
-    const size_t row_bytes = (size_t)G * kChunks * 16;
-    struct Scales {
-        uint32_t v[4];
-        bool on;
-    };
-    Pieces ahead(p, range);
-    int kp = 0;
-    bool on = ahead.next();
-    kp = ahead.kp0;
-    auto request = [&](Scales &c) {
-        c.on = on;
-        if (!on) return;
-        const int ft = ahead.tile / p.ntt, n0 = (GRAD ? kp : ft) * 128 + tid, g = GRAD ? ft : kp;
+    constexpr int kChunks = BITS == 4 ? 4 : 3, kCopies = 4 * kChunks;        // 16-byte pieces of a row's group, copies of a lane
+    constexpr int kTurn = BITS == 4 ? 1 : 3, kTurnRows = 32 * kTurn / kChunks;          // copies after which the lane's piece is the same one, rows on
+    const int lane = threadIdx.x & 31, G = p.K / kGroupFast, rows_all = MODE == kGrad ? p.D : p.F;
+    const size_t row_bytes = (size_t)G * kChunks * 16, turn_bytes = (size_t)kTurnRows * row_bytes;
+    const ptrdiff_t step = MODE == kGrad ? (ptrdiff_t)(128 * row_bytes) : kChunks * 16;
+    int row[kTurn], piece[kTurn];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const size_t at = (size_t)(n0 + 64 * i) * G + g;
-            c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros, whatever its codes
-            if (n0 + 64 * i < rows_all) {
-                c.v[2 * i] = ldg_u16(p.scales + at);
-                c.v[2 * i + 1] = ldg_u16(p.zeros + at);
+    for (int i = 0; i < kTurn; ++i) {
+        row[i] = (lane + 32 * i) / kChunks;
+        piece[i] = (lane + 32 * i) % kChunks;
+    }
+    // INT4: the 64-byte swizzle (rows are loaded by eight lanes at a time); the rows of further copies are multiples of eight on
+    const uint32_t to0 = ring + (BITS == 4 ? (uint32_t)row[0] * 64u + (uint32_t)((piece[0] ^ ((row[0] >> 1) & 3)) << 4) : (uint32_t)lane * 16u);
+    Walk<MODE> at(p, range);
+    const uint8_t *src[kTurn];
+    uint32_t slot = 0, phase = 1u;
+    bool first = true;
+#pragma unroll 1
+    while (at.on) {
+        if (at.opened) {
+#pragma unroll
+            for (int i = 0; i < kTurn; ++i) src[i] = p.qw + (size_t)at.n0 * row_bytes + (size_t)at.g * (kChunks * 16) + (size_t)row[i] * row_bytes + piece[i] * 16;
+        }
+        if (!__all_sync(0xffffffffu, first || umma::wait(rempty0 + 8u * slot, phase, quit))) return false;
+        const uint32_t to = to0 + slot * kSlotBytes;
+        const int last = rows_all - 1 - at.n0;                   // rows past it repeat it: their scales are 0
+        if (last >= 127) {
+            size_t more = 0;
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+                cp_async16(to + 512u * k, src[k % kTurn] + more);
+                if (k % kTurn == kTurn - 1) more += turn_bytes;
+            }
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < kCopies; ++k) {
+                const int e = lane + 32 * k, n = e / kChunks;
+                cp_async16(to + 512u * k, p.qw + (size_t)(at.n0 + min(n, last)) * row_bytes + (size_t)at.g * (kChunks * 16) + e % kChunks * 16);
             }
         }
-        if (++kp == ahead.kp1) {
-            on = ahead.next();
-            kp = ahead.kp0;
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(rfull0 + 8u * slot) : "memory");
+        at.step(p);
+#pragma unroll
+        for (int i = 0; i < kTurn; ++i) src[i] += step;
+        if (++slot == kRing) { slot = 0; phase ^= 1u; first = false; }
+    }
+    return true;
+}
+
+// Warp 3: scales and zero points.  They lie 2 bytes here and there (an instruction touches as many lines as it has lanes), so each is loaded
+// once per row and pair, kScaleAhead pairs before it is stored.
+template <int MODE>
+__device__ __forceinline__ bool load_scales(const EvenParams &p, int range, uint32_t ring, uint32_t rfull0, uint32_t rempty0, volatile int *quit)
+{
+    const int lane = threadIdx.x & 31, G = p.K / kGroupFast, rows_all = MODE == kGrad ? p.D : p.F;
+    const ptrdiff_t zero = p.zeros - p.scales, step = MODE == kGrad ? (ptrdiff_t)128 * G : 1, next = (ptrdiff_t)32 * G;
+    struct Scales {
+        uint32_t v[8];
+        bool on;
+    };
+    Walk<MODE> at(p, range);
+    const __half *src = p.scales;
+    auto request = [&](Scales &c) {
+        c.on = at.on;
+        if (!at.on) return;
+        if (at.opened) src = p.scales + (size_t)(at.n0 + lane) * G + at.g;
+        const int left = rows_all - at.n0 - lane;
+        const __half *q = src;
+#pragma unroll
+        for (int i = 0; i < 4; ++i, q += next) {
+            c.v[2 * i] = c.v[2 * i + 1] = 0u;                    // what lies outside is a row of zeros, whatever its codes
+            if (left > 32 * i) {
+                c.v[2 * i] = ldg_u16(q);
+                c.v[2 * i + 1] = ldg_u16(q + zero);
+            }
         }
+        at.step(p);
+        src += step;
     };
     Scales c[kScaleAhead];
 #pragma unroll
     for (int i = 0; i < kScaleAhead; ++i) request(c[i]);
-    Pieces cur(p, range);
-    cur.next();
-    int ck = cur.kp0;
+    const uint32_t to0 = ring + kCodeBytes + (uint32_t)lane * 4u;
     uint32_t slot = 0, phase = 1u;
     bool first = true;
 #pragma unroll 1
@@ -161,26 +226,13 @@ __device__ __forceinline__ bool load_codes(const EvenParams &p, int range, uint3
         for (int i = 0; i < kScaleAhead; ++i) {
             if (!c[i].on) return true;
             if (!__all_sync(0xffffffffu, first || umma::wait(rempty0 + 8u * slot, phase, quit))) return false;
-            const uint32_t dst = ring + slot * kSlotBytes, bar = rfull0 + 8u * slot;
-            const int ft = cur.tile / p.ntt, n0 = (GRAD ? ck : ft) * 128;
-            const uint8_t *src = p.qw + (size_t)(GRAD ? ft : ck) * (kChunks * 16);
-#pragma unroll 2
-            for (int k = 0; k < 2 * kChunks; ++k) {              // pieces [row][piece]
-                const int e = tid + 64 * k, row = e / kChunks, piece = e - row * kChunks;
-                const uint32_t to = dst + (BITS == 4 ? (uint32_t)row * 64u + (uint32_t)((piece ^ ((row >> 1) & 3)) << 4) : (uint32_t)row * 48u + (uint32_t)piece * 16u);
-                cp_async16(to, src + (size_t)min(n0 + row, rows_all - 1) * row_bytes + piece * 16);
-            }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+            const uint32_t to = to0 + slot * kSlotBytes;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kCodeBytes + (uint32_t)(tid + 64 * k) * 4u), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16) : "memory");
+            for (int k = 0; k < 4; ++k)
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + 128u * k), "r"(c[i].v[2 * k] | c[i].v[2 * k + 1] << 16) : "memory");
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar);
+            if (lane == 0) mbar_arrive(rfull0 + 8u * slot);
             request(c[i]);
-            if (++ck == cur.kp1) {
-                cur.next();
-                ck = cur.kp0;
-            }
             if (++slot == kRing) { slot = 0; phase ^= 1u; first = false; }
         }
     }
@@ -193,75 +245,78 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
     constexpr bool GRAD = MODE == kGrad;
     constexpr int NW = BITS == 4 ? 4 : 3;
     const int warp = (threadIdx.x >> 5) - kDqWarp, group = warp / kGroupWarps, w = warp % kGroupWarps, lane = threadIdx.x & 31;
-    // A thread's row of the pair and its 64 of the row's 128 codes.  Forward those are the pair's block and the row the operand's; Grad the
-    // row's half chooses the block and the codes a box of the operand.  Eight neighbouring lanes store to eight rows: different banks in the
-    // 128-byte swizzle, as they load them from different banks (INT4: the 64-byte swizzle of the copy).
-    const int row = 32 * (w & 3) + lane, part = w >> 2, blk = GRAD ? row >> 6 : part;
+    // A thread's row of the pair.  Forward the pair's blocks are the row's halves; Grad the row's half chooses the block and the codes' halves are the
+    // operand's boxes.  Eight neighbouring lanes store to eight rows: different banks in the 128-byte swizzle, as they load them from different
+    // banks (INT4: the 64-byte swizzle of the copy).
+    const int row = 32 * w + lane;
     const uint32_t r = GRAD ? row & 63 : row;
-    const uint32_t dst = sbase + (GRAD ? (uint32_t)part * kBox : 0u) + r * 128u + ((r & 7u) << 4);          // unit j: ^ (j << 4)
-    const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u + (uint32_t)part * 24u;
+    const uint32_t dst = sbase + r * 128u + ((r & 7u) << 4);                 // unit j: ^ (j << 4)
+    const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u;
     Pieces pc(p, range);
     uint32_t s = 0, use = 0;                                     // stage of the next block, times it has been used
     uint32_t slot = 0, rphase = 0;                               // of the ring
     int turn = 0;                                                // whose pair it is
     const uint32_t stages = (uint32_t)p.stages;
     auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
+    auto announce = [&](uint32_t stage) {
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full0 + 8u * stage);
+    };
     while (pc.next()) {
         const int n = pc.kp1 - pc.kp0;
 #pragma unroll 1
         for (int k = 0; k < n; ++k) {
-            // the stage of this thread's block, and its use before this one.  The other group's pairs and the sub-branch's blocks are waited
-            // for as well: a wait tells one phase of a barrier from the next, not from the one after that.
-            uint32_t st = s + (uint32_t)blk, u = use;
-            if (st >= stages) {
-                st -= stages;
-                ++u;
-            }
+            // the pair's second stage, and its use before this one.  Other groups' pairs and the sub-branch's blocks are waited for as well: a
+            // wait tells one phase of a barrier from the next, not from the one after that.
+            const bool wrap = s + 1 == stages;
+            const uint32_t s1 = wrap ? 0u : s + 1, u1 = wrap ? use + 1 : use;
             if (turn != group) {
-                if (!free_again(st, u)) return false;
+                if (!free_again(s1, u1)) return false;
             } else {
                 const uint32_t at = ring + slot * kSlotBytes;
                 if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, rphase, quit))) return false;
-                uint32_t c[2 * NW];
+                uint32_t c[4 * NW];
                 if constexpr (BITS == 4) {
-                    const uint4 a = lds128(at + (src ^ (uint32_t)(part << 5))), b = lds128(at + (src ^ (uint32_t)(part << 5 | 16)));
-                    c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w;
-                    c[4] = b.x; c[5] = b.y; c[6] = b.z; c[7] = b.w;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 a = lds128(at + (src ^ (uint32_t)(i << 4)));
+                        c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
+                    }
                 } else {
 #pragma unroll
                     for (int i = 0; i < 3; ++i) {
-                        const uint2 a = lds_v2(at + src + 8u * i);
-                        c[2 * i] = a.x;
-                        c[2 * i + 1] = a.y;
+                        const uint4 a = lds128(at + src + 16u * i);
+                        c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
                     }
                 }
                 uint32_t sz;
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(at + kCodeBytes + (uint32_t)row * 4u) : "memory");
                 const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
-                const uint32_t to = dst + st * stage_bytes;
+                const uint32_t mine = GRAD ? (row < 64 ? s : s1) : s, used = GRAD ? (row < 64 ? use : u1) : use;
+                const uint32_t to0 = dst + mine * stage_bytes, to1 = GRAD ? to0 + kBox : dst + s1 * stage_bytes;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     uint32_t d[16], out[16];
                     Dequant<BITS, T>::run(c + NW * i, fs, fz, d);
                     natural_pairs<BITS>(d, out);
                     if (i == 0) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(rempty0 + 8u * slot);         // (this warp has its codes in registers)
-                        if (!free_again(st, u)) return false;
+                        if (!free_again(mine, used)) return false;
                     }
+                    if (i == 2 && !GRAD && !free_again(s1, u1)) return false;
+                    const uint32_t to = i < 2 ? to0 : to1;
 #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) sts128(to ^ ((4u * i + j) << 4), out + 4 * j);
+                    for (uint32_t j = 0; j < 4; ++j) sts128(to ^ ((4u * (i & 1) + j) << 4), out + 4 * j);
+                    if (i == 1 && !GRAD) announce(s);
                 }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full0 + 8u * st);
+                announce(GRAD ? mine : s1);
+                if (GRAD && row < 64 && !free_again(s1, u1)) return false;
             }
-            s += 2;
-            if (s >= stages) {
-                s -= stages;
-                ++use;
-            }
-            turn ^= 1;
+            s = s1 + 1 == stages ? 0u : s1 + 1;
+            use = s1 + 1 == stages ? u1 + 1 : u1;
+            if (++turn == kGroups) turn = 0;
             if (++slot == kRing) { slot = 0; rphase ^= 1u; }
         }
         if (pc.owner()) {                                        // the sub-branch's stages are made by copies
@@ -286,6 +341,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap cmap, const EvenParams p)
 {
     constexpr bool GRAD = MODE == kGrad;
+    constexpr int kMakers = GRAD ? kGroupWarps / 2 : kGroupWarps;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t sbase = smem_u32(smem), stage_bytes = kWBytes + (uint32_t)p.tok * (kBK * 2u), y_off = (uint32_t)p.stages * stage_bytes;
@@ -300,11 +356,11 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int i = 0; i < p.stages; ++i) {
-            mbar_init(full0 + 8u * i, 1 + kGroupWarps / 2);      // the copying lane, and the four warps that make a block
+            mbar_init(full0 + 8u * i, 1 + kMakers);               // the copying lane, and the warps that make a block
             mbar_init(empty0 + 8u * i, 1);
         }
         for (int i = 0; i < kRing; ++i) {
-            mbar_init(rfull0 + 8u * i, 64 + 2);                  // every loading lane's copies, and both warps' scales
+            mbar_init(rfull0 + 8u * i, 32 + 1);                  // every copying lane's codes, and the scales
             mbar_init(rempty0 + 8u * i, kGroupWarps);
         }
         for (int i = 0; i < 2; ++i) {
@@ -334,27 +390,34 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             pdl_wait();                                          // (codes, scales and zero points are weights: the others do not wait)
             uint32_t s = 0, phase = 1u;
             bool first = true;
-            const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u);
+            const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), x0 = sbase + kWBytes;
+            auto free_stage = [&]() { return first || umma::wait(empty0 + 8u * s, phase, quit); };
+            auto next_stage = [&]() {
+                if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
+            };
 #pragma unroll 1
             for (Pieces pc(p, range); ok && pc.next();) {
-                const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, main = 2 * (pc.kp1 - pc.kp0), n = main + (pc.owner() ? p.slab : 0);
+                const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, end = 2 * pc.kp1 * kBK;
 #pragma unroll 1
-                for (int i = 0; i < n; ++i) {
-                    if (!first && !umma::wait(empty0 + 8u * s, phase, quit)) { ok = false; break; }
-                    const bool mine = i < main;
-                    const int c0 = (mine ? 2 * pc.kp0 + i : i - main) * kBK;
-                    const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes, xt = wt + kWBytes;
-                    mbar_expect_tx(bar, mine ? xbytes : xbytes + kWBytes);
-                    tma_load_2d(xt, mine ? &xmap : &tmap, c0, m0, bar);
-                    if (!mine) {
-                        if (GRAD) {
-                            for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
-                        } else {
-                            tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
-                        }
-                        for (int k = 0; k < kGroupWarps / 2; ++k) mbar_arrive(bar);      // (for the warps that have nothing to make)
+                for (int c0 = 2 * pc.kp0 * kBK; c0 < end; c0 += kBK) {
+                    if (!free_stage()) { ok = false; break; }
+                    mbar_expect_tx(full0 + 8u * s, xbytes);
+                    tma_load_2d(x0 + s * stage_bytes, &xmap, c0, m0, full0 + 8u * s);
+                    next_stage();
+                }
+#pragma unroll 1
+                for (int c0 = 0; ok && pc.owner() && c0 < p.slab * kBK; c0 += kBK) {
+                    if (!free_stage()) { ok = false; break; }
+                    const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes;
+                    mbar_expect_tx(bar, xbytes + kWBytes);
+                    tma_load_2d(wt + kWBytes, &tmap, c0, m0, bar);
+                    if (GRAD) {
+                        for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
+                    } else {
+                        tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
                     }
-                    if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
+                    for (int k = 0; k < kMakers; ++k) mbar_arrive(bar);              // (for the warps that have nothing to make)
+                    next_stage();
                 }
             }
         }
@@ -480,8 +543,10 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp >= kDqWarp) {
         ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, ring, full0, empty0, rfull0, rempty0, quit);
-    } else {
+    } else if (warp == 2) {
         ok = load_codes<BITS, MODE>(p, range, ring, rfull0, rempty0, quit);
+    } else {
+        ok = load_scales<MODE>(p, range, ring, rfull0, rempty0, quit);
     }
     if (!ok) {
         *quit = 1;

@@ -109,20 +109,23 @@ factor_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ 
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kCols, (uint32_t)p.rank_pad) | umma::kIdescMnA | umma::kIdescMnB;
-            uint32_t s = 0, phase = 0;
+        // (the whole warp walks the loop, one elected lane issues: operands stay in uniform registers)
+        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kCols, (uint32_t)p.rank_pad) | umma::kIdescMnA | umma::kIdescMnB;
+        const uint64_t qd0 = umma::desc_mn128(sbase, kBox), pd0 = umma::desc_mn128(sbase + 2 * kBox, kBox);
+        uint32_t s = 0, phase = 0;
 #pragma unroll 1
-            for (int b = b0; b < b1; ++b) {
-                if (!mbar_wait(full0 + 8u * s, phase)) { ok = false; break; }
-                umma::fence_after();
-                const uint64_t qd = umma::desc_mn128(sbase + s * stage_bytes, kBox), pd = umma::desc_mn128(sbase + s * stage_bytes + 2 * kBox, kBox);
+        for (int b = b0; b < b1 && ok; ++b) {
+            ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8u * s, phase));
+            umma::fence_after();
+            if (ok && umma::elect_one()) {
+                const uint64_t qd = qd0 + s * (stage_bytes >> 4), pd = pd0 + s * (stage_bytes >> 4);
 #pragma unroll
                 for (int j = 0; j < kTok / 16; ++j) umma::mma(tmem, qd + j * (2048u >> 4), pd + j * (2048u >> 4), idesc, b > b0 || j > 0);
                 umma::commit(empty0 + 8u * s);
-                if (++s == (uint32_t)stages) { s = 0; phase ^= 1u; }
+                if (b + 1 == b1) umma::commit(done);
             }
-            if (ok) umma::commit(done);
+            __syncwarp();
+            if (++s == (uint32_t)stages) { s = 0; phase ^= 1u; }
         }
     } else {
         // lane = column of Q, column of tensor memory = entry of the rank

@@ -17,11 +17,12 @@ namespace {
 using namespace ptx;
 
 constexpr int kBK = 64, kRows = 128;
-constexpr int kMostTok = 128, kStages = 4, kMostCluster = 8;
+constexpr int kMostTok = 128, kStages = 3, kMostCluster = 8;
+constexpr int kPer = 2;                          // blocks of a stage
 constexpr uint32_t kABytes = kRows * kBK * 2u, kBox = kABytes / 2;
 constexpr int kThreads = 192;
-constexpr uint32_t kSmem = kStages * (kABytes + kMostTok * kBK * 2u) + 1024;
-static_assert(kMostTok * kRows * 4u <= kStages * (kABytes + kMostTok * kBK * 2u), "the sums take the stages' place");
+constexpr uint32_t kSmem = kStages * kPer * (kABytes + kMostTok * kBK * 2u) + 1024;
+static_assert(kMostTok * kRows * 4u <= kSmem - 1024, "the sums take the stages' place");
 
 struct ThinParams {
     void *t, *s;              // [M][rank_pad]
@@ -61,7 +62,7 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const int rt = cluster % p.nrt, m0 = cluster / p.nrt * p.tok, row0 = rt * kRows;
     const int all = of_s ? p.blocks_s : p.blocks_t, b0 = (int)((long long)all * crank / cs), b1 = (int)((long long)all * (crank + 1) / cs);
     const int boxes = min(2, (p.rank_pad - row0) / 64);
-    const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), stage_bytes = kABytes + xbytes, abytes = of_s ? (uint32_t)boxes * kBox : (uint32_t)p.a_rows * (kBK * 2u);
+    const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), block_bytes = kABytes + xbytes, stage_bytes = kPer * block_bytes, abytes = of_s ? (uint32_t)boxes * kBox : (uint32_t)p.a_rows * (kBK * 2u);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -86,40 +87,52 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         if (lane == 0) {
             uint32_t s = 0, phase = 1u;
 #pragma unroll 1
-            for (int b = b0; b < b1; ++b) {
-                if (b - b0 >= kStages && !mbar_wait(empty0 + 8u * s, phase)) { ok = false; break; }
-                const uint32_t bar = full0 + 8u * s, dst = sbase + s * stage_bytes;
-                mbar_expect_tx(bar, abytes + xbytes);
-                if (of_s)
-                    for (int i = 0; i < boxes; ++i) tma_load_2d(dst + i * kBox, &bmap, row0 + 64 * i, b * kBK, bar);
-                else
-                    tma_load_2d(dst, &amap, b * kBK, row0, bar);
-                tma_load_2d(dst + kABytes, of_s ? &dymap : &xmap, b * kBK, m0, bar);
+            for (int b = b0; b < b1; b += kPer) {
+                if (b - b0 >= kPer * kStages && !mbar_wait(empty0 + 8u * s, phase)) { ok = false; break; }
+                const uint32_t bar = full0 + 8u * s;
+                const int n = min(kPer, b1 - b);
+                mbar_expect_tx(bar, n * (abytes + xbytes));
+                for (int k = 0; k < n; ++k) {
+                    const uint32_t dst = sbase + s * stage_bytes + k * block_bytes;
+                    if (of_s)
+                        for (int i = 0; i < boxes; ++i) tma_load_2d(dst + i * kBox, &bmap, row0 + 64 * i, (b + k) * kBK, bar);
+                    else
+                        tma_load_2d(dst, &amap, (b + k) * kBK, row0, bar);
+                    tma_load_2d(dst + kABytes, of_s ? &dymap : &xmap, (b + k) * kBK, m0, bar);
+                }
                 if (++s == kStages) { s = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kRows, (uint32_t)p.tok) | (of_s ? umma::kIdescMnA : 0u), astep = of_s ? 2048u >> 4 : 2u;
-            uint32_t s = 0, phase = 0;
+        // (the whole warp walks the loop, one elected lane issues: operands stay in uniform registers)
+        const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kRows, (uint32_t)p.tok) | (of_s ? umma::kIdescMnA : 0u), astep = of_s ? 2048u >> 4 : 2u;
+        const uint64_t ad0 = of_s ? umma::desc_mn128(sbase, kBox) : umma::desc_k128(sbase), xd0 = umma::desc_k128(sbase + kABytes);
+        uint32_t s = 0, phase = 0;
 #pragma unroll 1
-            for (int b = b0; b < b1; ++b) {
-                if (!mbar_wait(full0 + 8u * s, phase)) { ok = false; break; }
-                umma::fence_after();
-                const uint32_t at = sbase + s * stage_bytes;
-                const uint64_t ad = of_s ? umma::desc_mn128(at, kBox) : umma::desc_k128(at), xd = umma::desc_k128(at + kABytes);
+        for (int b = b0; b < b1 && ok; b += kPer) {
+            ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8u * s, phase));
+            umma::fence_after();
+            if (ok && umma::elect_one()) {
+                uint64_t ad = ad0 + s * (stage_bytes >> 4), xd = xd0 + s * (stage_bytes >> 4);
 #pragma unroll
                 for (int j = 0; j < kBK / 16; ++j) umma::mma(tmem, ad + astep * j, xd + 2 * j, idesc, b > b0 || j > 0);
+                if (b + 1 < b1) {
+                    ad += block_bytes >> 4;
+                    xd += block_bytes >> 4;
+#pragma unroll
+                    for (int j = 0; j < kBK / 16; ++j) umma::mma(tmem, ad + astep * j, xd + 2 * j, idesc, 1u);
+                }
                 umma::commit(empty0 + 8u * s);
-                if (++s == kStages) { s = 0; phase ^= 1u; }
+                if (b + kPer >= b1) umma::commit(done);
             }
-            if (ok) umma::commit(done);
+            __syncwarp();
+            if (++s == kStages) { s = 0; phase ^= 1u; }
         }
     } else {
         // sums [token][rank entry] into shared memory, where the operands were
         const int q = warp & 3, j = 32 * q + lane;
         float *sums = reinterpret_cast<float *>(smem) + j;
-        ok = __all_sync(0xffffffffu, mbar_wait(done, 0u));       // (of no blocks the commit arrives at once)
+        ok = b0 == b1 || __all_sync(0xffffffffu, mbar_wait(done, 0u));
         if (ok) {
             umma::fence_after();
 #pragma unroll 1
