@@ -301,9 +301,14 @@ PrefillTuning prefill_tuning()
 
 int run_gated_even(const LinearArgs &a, Workspace *ws, cudaStream_t s)
 {
-    const size_t thin = thin_bytes(a.M, a.rank);
+    ThinArgs t{};
+    t.x = a.x; t.A = a.A;
+    t.M = a.M; t.N = a.N; t.K = a.K; t.rank = a.rank; t.bf16 = a.bf16;
     char *scratch = static_cast<char *>(ws->grad);
-    cudaError_t e = grow(scratch, ws->grad_bytes, thin + even_part_bytes(a.M, a.N, a.K), 1, s);
+    t.t = scratch;                                               // (any address: where it will be is not known yet)
+    if (!t.t) t.t = ws;
+    const size_t thin = thin_bytes(a.M, a.rank), thin_part = a.rank > 0 ? padded256(thin_part_bytes(t)) : 0;
+    cudaError_t e = grow(scratch, ws->grad_bytes, thin + thin_part + even_part_bytes(a.M, a.N, a.K), 1, s);
     ws->grad = scratch;
     if (e != cudaSuccess) return grow_status(e);
     size_t have_c = (size_t)ws->n_counters;
@@ -311,14 +316,13 @@ int run_gated_even(const LinearArgs &a, Workspace *ws, cudaStream_t s)
     ws->n_counters = (int)have_c;
     int launches = 0;
     if (a.rank > 0) {
-        ThinArgs t{};
-        t.x = a.x; t.A = a.A; t.t = scratch;
-        t.M = a.M; t.N = a.N; t.K = a.K; t.rank = a.rank; t.bf16 = a.bf16;
+        t.t = scratch;
+        t.part = scratch + thin;
         if (launch_thin(t, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
     }
     EvenArgs v{};
     v.x = a.x; v.qw = a.qw; v.scales = a.scales; v.zeros = a.zeros; v.factor = a.B; v.thin = scratch; v.y = a.y;
-    v.kept = a.kept; v.kept_scales = a.kept_scales; v.part = scratch + thin;
+    v.kept = a.kept; v.kept_scales = a.kept_scales; v.part = scratch + thin + thin_part;
     v.M = a.M; v.N = a.N; v.K = a.K; v.bits = a.bits; v.rank = a.rank; v.gate = a.gate; v.bf16 = a.bf16;
     if (launch_even(v, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
     g_launches += launches;
@@ -470,9 +474,13 @@ int run_backward(Backward &b, cudaStream_t s)
         return at;
     };
     const bool even = even_takes(g.M);
+    ThinArgs t{};
+    t.M = g.M; t.N = g.N; t.K = g.K; t.rank = g.rank; t.bf16 = g.bf16;
+    t.s = ws;                                                    // (any address: where it will be is not known yet)
+    t.t = factors ? ws : nullptr;
     const size_t M = g.M, thin = thin_bytes(g.M, g.rank);
     const size_t x_at = place(unpack ? M * g.K * 2 : 0), dy_at = place(b.kept ? M * g.N * 2 : 0), s_at = place(thin), t_at = place(factors ? thin : 0),
-                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
+                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), thin_at = place(even && g.rank > 0 ? thin_part_bytes(t) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
     cudaError_t e;
     size_t have_c = (size_t)ws->n_counters, need_w = 0, need_tags = 0;
     char *scratch = static_cast<char *>(ws->grad), *w16 = static_cast<char *>(ws->w16);
@@ -504,9 +512,7 @@ int run_backward(Backward &b, cudaStream_t s)
     g.t16 = factors ? scratch + t_at : nullptr;
     if (even) {
         if (g.rank > 0) {
-            ThinArgs t{};
-            t.x = g.x; t.dy = g.dy; t.A = g.A; t.B = g.B; t.t = g.t16; t.s = g.s16;
-            t.M = g.M; t.N = g.N; t.K = g.K; t.rank = g.rank; t.bf16 = g.bf16;
+            t.x = g.x; t.dy = g.dy; t.A = g.A; t.B = g.B; t.t = g.t16; t.s = g.s16; t.part = scratch + thin_at;
             if (launch_thin(t, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
         }
         if (g.dx) {

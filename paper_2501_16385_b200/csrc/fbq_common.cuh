@@ -169,9 +169,11 @@ cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &t
 struct ThinArgs {
     const void *x, *dy, *A, *B;
     void *t, *s;                  // [M][rank rounded up to 64] or none
+    void *part;                   // thin_part_bytes of scratch
     int M, N, K, rank;
     bool bf16;
 };
+size_t thin_part_bytes(const ThinArgs &a);
 cudaError_t launch_thin(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches);
 struct EvenArgs {
     const void *x;                // x [M][K], or dy [M][N]

@@ -295,21 +295,21 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                 const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
                 const uint32_t mine = GRAD ? (row < 64 ? s : s1) : s, used = GRAD ? (row < 64 ? use : u1) : use;
                 const uint32_t to0 = dst + mine * stage_bytes, to1 = GRAD ? to0 + kBox : dst + s1 * stage_bytes;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(rempty0 + 8u * slot);                 // (this warp has its codes in registers)
+                // half a row at a time, in registers before its stage is waited for
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t d[16], out[16];
-                    Dequant<BITS, T>::run(c + NW * i, fs, fz, d);
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t d[16], out[32];
+                    Dequant<BITS, T>::run(c + 2 * NW * i, fs, fz, d);
                     natural_pairs<BITS>(d, out);
-                    if (i == 0) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(rempty0 + 8u * slot);         // (this warp has its codes in registers)
-                        if (!free_again(mine, used)) return false;
-                    }
-                    if (i == 2 && !GRAD && !free_again(s1, u1)) return false;
-                    const uint32_t to = i < 2 ? to0 : to1;
+                    Dequant<BITS, T>::run(c + 2 * NW * i + NW, fs, fz, d);
+                    natural_pairs<BITS>(d, out + 16);
+                    if (GRAD ? i == 0 && !free_again(mine, used) : !free_again(i ? s1 : s, i ? u1 : use)) return false;
+                    const uint32_t to = i ? to1 : to0;
 #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) sts128(to ^ ((4u * (i & 1) + j) << 4), out + 4 * j);
-                    if (i == 1 && !GRAD) announce(s);
+                    for (uint32_t j = 0; j < 8; ++j) sts128(to ^ (j << 4), out + 4 * j);
+                    if (i == 0 && !GRAD) announce(s);
                 }
                 announce(GRAD ? mine : s1);
                 if (GRAD && row < 64 && !free_again(s1, u1)) return false;

@@ -4,7 +4,8 @@
 // Little arithmetic over long contractions, so what counts is how many SMs read: a cluster of CTAs takes a tile of tokens and up to 128
 // entries of the rank and cuts the contraction (tcgen05.mma, the rank's entries are the rows, tokens the columns; A is K-major, B as
 // it lies MN-major).  Each CTA puts its fp32 sums into its shared memory, and after one cluster barrier every CTA adds an equal share of the
-// tokens from all of them, in order, through distributed shared memory.
+// tokens from all of them, in order, through distributed shared memory.  Long contractions (22016 rows of B at 333 tokens: 22 us with one cluster a
+// tile) are cut over several clusters as well, each with its fp32 sums, which a second launch adds in order and rounds.
 #include <algorithm>
 
 #include "fbq_common.cuh"
@@ -29,14 +30,16 @@ struct ThinParams {
     int *status;
     int M, rank_pad, a_rows;
     int tok, ntt, nrt;        // tokens of a tile, tiles, tiles of the rank
+    int cuts_s, cuts_t;       // clusters that share a tile's contraction
     int n_s;                  // clusters of s, before those of t
+    float *part;              // [cut][M][rank_pad] of s, then of t, or none: no contraction is cut
     int blocks_t, blocks_s;   // of the contractions
 };
 
 __device__ __forceinline__ float ld_cluster(uint32_t addr)
 {
     float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
     return v;
 }
 
@@ -59,8 +62,11 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     int cluster = (int)(blockIdx.x / cs);
     const bool of_s = cluster < p.n_s;
     if (!of_s) cluster -= p.n_s;
+    const int cuts = of_s ? p.cuts_s : p.cuts_t, cut = cluster % cuts;
+    cluster /= cuts;
     const int rt = cluster % p.nrt, m0 = cluster / p.nrt * p.tok, row0 = rt * kRows;
-    const int all = of_s ? p.blocks_s : p.blocks_t, b0 = (int)((long long)all * crank / cs), b1 = (int)((long long)all * (crank + 1) / cs);
+    const long long all = of_s ? p.blocks_s : p.blocks_t;
+    const int shares = cuts * (int)cs, share = cut * (int)cs + (int)crank, b0 = (int)(all * share / shares), b1 = (int)(all * (share + 1) / shares);
     const int boxes = min(2, (p.rank_pad - row0) / 64);
     const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), block_bytes = kABytes + xbytes, stage_bytes = kPer * block_bytes, abytes = of_s ? (uint32_t)boxes * kBox : (uint32_t)p.a_rows * (kBK * 2u);
 
@@ -155,12 +161,19 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     cluster_wait();
     const int width = min(kRows, p.rank_pad - row0);
     unsigned short *out = static_cast<unsigned short *>(of_s ? p.s : p.t);
-    for (int e = threadIdx.x; e < p.tok * kRows; e += kThreads) {
-        const int c = e / kRows, j = e % kRows;
-        if (c % (int)cs != (int)crank || m0 + c >= p.M || j >= width) continue;
-        float v = 0.f;
-        for (uint32_t k = 0; k < cs; ++k) v += ld_cluster(mapa_shared(sbase + (uint32_t)e * 4u, k));
-        out[(size_t)(m0 + c) * p.rank_pad + row0 + j] = to_bits16<T>(v);
+    float *part = p.part + (size_t)((of_s ? 0 : p.cuts_s) + cut) * p.M * p.rank_pad;
+    // this CTA's tokens are crank, crank + cs, ...; a thread has the loads of a sum on their way at once
+    for (int e = threadIdx.x; e < (p.tok + (int)cs - 1) / (int)cs * kRows; e += kThreads) {
+        const int c = e / kRows * (int)cs + (int)crank, j = e % kRows;
+        if (c >= p.tok || m0 + c >= p.M || j >= width) continue;
+        float w[kMostCluster], v = 0.f;
+#pragma unroll
+        for (uint32_t k = 0; k < kMostCluster; ++k) w[k] = k < cs ? ld_cluster(mapa_shared(sbase + (uint32_t)(c * kRows + j) * 4u, k)) : 0.f;
+#pragma unroll
+        for (int k = 0; k < kMostCluster; ++k) v += w[k];
+        const size_t to = (size_t)(m0 + c) * p.rank_pad + row0 + j;
+        if (p.part) part[to] = v;
+        else out[to] = to_bits16<T>(v);
     }
     cluster_arrive();
     cluster_wait();                                              // nobody reads this CTA's sums any more
@@ -170,12 +183,27 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     }
 }
 
-template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
+// s and t from the sums of their cuts, in order.
+template <typename T> __global__ void __launch_bounds__(256) thin_add_kernel(const ThinParams p)
 {
-    const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
-    const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-    ThinParams p{};
-    p.t = a.t; p.s = a.s; p.status = status;
+    pdl_launch_dependents();
+    pdl_wait();
+    const bool of_s = blockIdx.y == 0 && p.s;
+    const size_t n = (size_t)p.M * p.rank_pad, at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= n) return;
+    const float *src = p.part + (of_s ? 0 : p.cuts_s * n) + at;
+    float v = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < (of_s ? p.cuts_s : p.cuts_t); ++c) v += __ldcg(src + c * n);
+    static_cast<unsigned short *>(of_s ? p.s : p.t)[at] = to_bits16<T>(v);
+}
+
+// The plan: clusters as many as are resident at once (15 of eight CTAs).  Either their number goes to tiles of tokens, of 16 at least; or, where
+// a CTA then has a long contraction to go through (more than kLong blocks), tiles are wide and the contractions cut, each into shares of
+// about the same length.  One CTA reads some 60 bytes a nanosecond, and narrow tiles read A or B once each.
+constexpr int kLong = 16, kResident = 15;
+void plan(const ThinArgs &a, ThinParams &p, int *cluster)
+{
     p.M = a.M;
     p.rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.a_rows = std::min(kRows, p.rank_pad);
@@ -185,12 +213,33 @@ template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, 
     const int kinds = (a.t ? 1 : 0) + (a.s ? 1 : 0), deep = std::max(p.blocks_t, p.blocks_s);
     int cs = 1;
     while (2 * cs <= std::min(kMostCluster, deep / 2)) cs *= 2;
-    // tiles of tokens: as many as clusters are resident at once (15 of eight CTAs), of 16 tokens at least
-    const int room = std::max(1, 120 / (cs * p.nrt * kinds));
-    p.tok = std::min(kMostTok, ((a.M + room - 1) / room + 15) / 16 * 16);
-    p.ntt = (a.M + p.tok - 1) / p.tok;
-    p.n_s = a.s ? p.ntt * p.nrt : 0;
-    const int clusters = p.n_s + (a.t ? p.ntt * p.nrt : 0);
+    *cluster = cs;
+    auto tiles = [&](int room) {
+        p.tok = std::min(kMostTok, ((a.M + room - 1) / room + 15) / 16 * 16);
+        p.ntt = (a.M + p.tok - 1) / p.tok;
+    };
+    tiles(std::max(1, kResident * kMostCluster / (cs * p.nrt * kinds)));
+    p.cuts_s = a.s ? 1 : 0;
+    p.cuts_t = a.t ? 1 : 0;
+    if (deep <= kLong * cs) return;
+    tiles((a.M + kMostTok - 1) / kMostTok);
+    const int sets = p.ntt * p.nrt, all = sets * (p.blocks_s + p.blocks_t);
+    auto cuts = [&](int blocks) { return blocks ? std::max(1, (int)((long long)blocks * kResident / all)) : 0; };
+    p.cuts_s = cuts(p.blocks_s);
+    p.cuts_t = cuts(p.blocks_t);
+}
+
+template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
+{
+    const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+    ThinParams p{};
+    int cs = 1;
+    plan(a, p, &cs);
+    p.t = a.t; p.s = a.s; p.status = status;
+    p.part = p.cuts_s > 1 || p.cuts_t > 1 ? static_cast<float *>(a.part) : nullptr;
+    p.n_s = p.ntt * p.nrt * p.cuts_s;
+    const int clusters = p.n_s + p.ntt * p.nrt * p.cuts_t;
     CUtensorMap xmap, dymap, amap, bmap;
     cudaError_t e;
     if (a.t) {
@@ -224,11 +273,27 @@ template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, 
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = pdl ? 2 : 1;
-    if ((e = cudaLaunchKernelEx(&cfg, kern, xmap, dymap, amap, bmap, p)) == cudaSuccess) ++*launches;
+    if ((e = cudaLaunchKernelEx(&cfg, kern, xmap, dymap, amap, bmap, p)) != cudaSuccess) return e;
+    ++*launches;
+    if (!p.part) return e;
+    cfg.gridDim = dim3((unsigned)(((size_t)p.M * p.rank_pad + 255) / 256), (unsigned)((a.s ? 1 : 0) + (a.t ? 1 : 0)));
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = 0;
+    cfg.attrs = at + 1;
+    cfg.numAttrs = pdl ? 1 : 0;
+    if ((e = cudaLaunchKernelEx(&cfg, thin_add_kernel<T>, p)) == cudaSuccess) ++*launches;
     return e;
 }
 
 }  // namespace
+
+size_t thin_part_bytes(const ThinArgs &a)
+{
+    ThinParams p{};
+    int cs;
+    plan(a, p, &cs);
+    return p.cuts_s > 1 || p.cuts_t > 1 ? (size_t)(p.cuts_s + p.cuts_t) * p.M * p.rank_pad * sizeof(float) : 0;
+}
 
 cudaError_t launch_thin(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
 {
