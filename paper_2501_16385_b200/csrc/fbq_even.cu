@@ -46,9 +46,11 @@ constexpr int kMostTok = 192, kMostStages = 8;
 constexpr int kDqWarp = 8, kGroups = 4, kGroupWarps = 4, kThreads = (kDqWarp + kGroups * kGroupWarps) * 32;
 constexpr int kRing = 4;                         // pairs of blocks whose codes and scales are there or on their way
 constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = kCodeBytes + 512u;      // codes (INT3: 48 of 64 bytes a row), scales and zero points
+static_assert(kMostStages <= 8, "");
+constexpr int kGo = 8;                           // pairs whose stages can be free and not yet written: less than half of these (see `dequantise`)
 constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
-constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 256;     // ring, staging, largest |p|, barriers
+constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 512;     // ring, staging, largest |p|, barriers
 constexpr uint32_t kSmemMost = 227 * 1024 - 1024;        // (the base is moved up to 1024 bytes)
 enum Mode { kGated, kKept, kGrad };
 
@@ -239,7 +241,7 @@ __device__ __forceinline__ bool load_scales(const EvenParams &p, int range, uint
 }
 
 template <int BITS, typename T, int MODE>
-__device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint32_t sbase, uint32_t stage_bytes, uint32_t ring, uint32_t full0, uint32_t empty0,
+__device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint32_t sbase, uint32_t stage_bytes, uint32_t ring, uint32_t full0, uint32_t go0,
                                            uint32_t rfull0, uint32_t rempty0, volatile int *quit)
 {
     constexpr bool GRAD = MODE == kGrad;
@@ -253,11 +255,11 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
     const uint32_t dst = sbase + r * 128u + ((r & 7u) << 4);                 // unit j: ^ (j << 4)
     const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u;
     Pieces pc(p, range);
-    uint32_t s = 0, use = 0;                                     // stage of the next block, times it has been used
+    uint32_t s = 0;                                              // stage of the next block
+    uint32_t q = 0;                                              // pairs so far
     uint32_t slot = 0, rphase = 0;                               // of the ring
     int turn = 0;                                                // whose pair it is
     const uint32_t stages = (uint32_t)p.stages;
-    auto free_again = [&](uint32_t stage, uint32_t n) { return __all_sync(0xffffffffu, n == 0 || umma::wait(empty0 + 8u * stage, (n - 1u) & 1u, quit)) != 0; };
     auto announce = [&](uint32_t stage) {
         fence_proxy_async();
         __syncwarp();
@@ -267,13 +269,8 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
         const int n = pc.kp1 - pc.kp0;
 #pragma unroll 1
         for (int k = 0; k < n; ++k) {
-            // the pair's second stage, and its use before this one.  Other groups' pairs and the sub-branch's blocks are waited for as well: a
-            // wait tells one phase of a barrier from the next, not from the one after that.
-            const bool wrap = s + 1 == stages;
-            const uint32_t s1 = wrap ? 0u : s + 1, u1 = wrap ? use + 1 : use;
-            if (turn != group) {
-                if (!free_again(s1, u1)) return false;
-            } else {
+            const uint32_t s1 = s + 1 == stages ? 0u : s + 1;    // the pair's second stage
+            if (turn == group) {
                 const uint32_t at = ring + slot * kSlotBytes;
                 if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, rphase, quit))) return false;
                 uint32_t c[4 * NW];
@@ -293,7 +290,7 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                 uint32_t sz;
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(at + kCodeBytes + (uint32_t)row * 4u) : "memory");
                 const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
-                const uint32_t mine = GRAD ? (row < 64 ? s : s1) : s, used = GRAD ? (row < 64 ? use : u1) : use;
+                const uint32_t mine = GRAD && row >= 64 ? s1 : s;
                 const uint32_t to0 = dst + mine * stage_bytes, to1 = GRAD ? to0 + kBox : dst + s1 * stage_bytes;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(rempty0 + 8u * slot);                 // (this warp has its codes in registers)
@@ -305,29 +302,24 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint3
                     natural_pairs<BITS>(d, out);
                     Dequant<BITS, T>::run(c + 2 * NW * i + NW, fs, fz, d);
                     natural_pairs<BITS>(d, out + 16);
-                    if (GRAD ? i == 0 && !free_again(mine, used) : !free_again(i ? s1 : s, i ? u1 : use)) return false;
+                    // The pair's stages are free: the copying warp, which waits for every block's, tells by a barrier per pair.  (A group that waited for
+                    // a stage's own barrier would have to look at every phase of it: one that passes two between looks it misses, or takes an old one
+                    // for the next.)  Eight of them are told apart although a wait knows a phase only from its neighbours: kMostStages / 2 pairs at most
+                    // are free before this group's is written, and the last eight before it have been.
+                    if (i == 0 && !__all_sync(0xffffffffu, umma::wait(go0 + 8u * (q % kGo), (q / kGo) & 1u, quit))) return false;
                     const uint32_t to = i ? to1 : to0;
 #pragma unroll
                     for (uint32_t j = 0; j < 8; ++j) sts128(to ^ (j << 4), out + 4 * j);
                     if (i == 0 && !GRAD) announce(s);
                 }
                 announce(GRAD ? mine : s1);
-                if (GRAD && row < 64 && !free_again(s1, u1)) return false;
             }
+            ++q;
             s = s1 + 1 == stages ? 0u : s1 + 1;
-            use = s1 + 1 == stages ? u1 + 1 : u1;
             if (++turn == kGroups) turn = 0;
             if (++slot == kRing) { slot = 0; rphase ^= 1u; }
         }
-        if (pc.owner()) {                                        // the sub-branch's stages are made by copies
-            for (int k = 0; k < p.slab; ++k) {
-                if (!free_again(s, use)) return false;
-                if (++s == stages) {
-                    s = 0;
-                    ++use;
-                }
-            }
-        }
+        if (pc.owner()) s = (s + (uint32_t)p.slab) % stages;     // the sub-branch's stages are made by copies
     }
     return true;
 }
@@ -347,9 +339,9 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const uint32_t sbase = smem_u32(smem), stage_bytes = kWBytes + (uint32_t)p.tok * (kBK * 2u), y_off = (uint32_t)p.stages * stage_bytes;
     const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = kRing * kSlotBytes + 512u;
     const uint32_t full0 = ring + bars, empty0 = full0 + 8u * kMostStages, accf0 = empty0 + 8u * kMostStages, acce0 = accf0 + 16u, rfull0 = acce0 + 16u,
-                   rempty0 = rfull0 + 8u * kRing;
+                   rempty0 = rfull0 + 8u * kRing, go0 = rempty0 + 8u * kRing;
     float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + kRing * kSlotBytes);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing + 8u * kGo);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = (int)blockIdx.x;
 
@@ -363,6 +355,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             mbar_init(rfull0 + 8u * i, 32 + 1);                  // every copying lane's codes, and the scales
             mbar_init(rempty0 + 8u * i, kGroupWarps);
         }
+        for (int i = 0; i < kGo; ++i) mbar_init(go0 + 8u * i, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(accf0 + 8u * i, 1);
             mbar_init(acce0 + 8u * i, 4);
@@ -388,7 +381,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         // =================================================== copies
         if (lane == 0) {
             pdl_wait();                                          // (codes, scales and zero points are weights: the others do not wait)
-            uint32_t s = 0, phase = 1u;
+            uint32_t s = 0, phase = 1u, q = 0;
             bool first = true;
             const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), x0 = sbase + kWBytes;
             auto free_stage = [&]() { return first || umma::wait(empty0 + 8u * s, phase, quit); };
@@ -401,6 +394,10 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 #pragma unroll 1
                 for (int c0 = 2 * pc.kp0 * kBK; c0 < end; c0 += kBK) {
                     if (!free_stage()) { ok = false; break; }
+                    if (c0 & kBK) {                              // both stages of the pair are free
+                        mbar_arrive(go0 + 8u * (q % kGo));
+                        ++q;
+                    }
                     mbar_expect_tx(full0 + 8u * s, xbytes);
                     tma_load_2d(x0 + s * stage_bytes, &xmap, c0, m0, full0 + 8u * s);
                     next_stage();
@@ -542,7 +539,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp >= kDqWarp) {
-        ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, ring, full0, empty0, rfull0, rempty0, quit);
+        ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, ring, full0, go0, rfull0, rempty0, quit);
     } else if (warp == 2) {
         ok = load_codes<BITS, MODE>(p, range, ring, rfull0, rempty0, quit);
     } else {
