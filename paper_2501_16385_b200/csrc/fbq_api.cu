@@ -285,9 +285,27 @@ int gated_kernel(const LinearArgs &a)
     return g_opt.use_gemv && !a.kept && a.M <= kGemvMaxM && g_opt.force_kernel < 0 && gemv_supported(a) ? FBQ_KERNEL_DECODE : FBQ_KERNEL_PREFILL;
 }
 
-// Calls of few hundred tokens: weights dequantised where they are multiplied (fbq_even.cu), the sub-branch's thin products in a launch before.
-constexpr int kEvenMost = 512;
+// Which calls dequantise weights where they are multiplied, with the blocks shared out evenly (fbq_even.cu), the sub-branch's thin products in a
+// launch before.  Backward passes, us, this / the dense kernel (INT4, rank 64; the first is the gated block's, 4096 -> 2 x 11008):
+//                    77 tokens    512       768       1024      1536      2048
+//   4096 <- 22016    57 / 248  144 / 192  191 / 199 261 / 218 371 / 372 511 / 421
+//   2048 <- 11008    39 / 131   72 / 109   85 / 111  97 / 116 127 / 142 185 / 165
+//   11008 <- 4096    36 /  72   83 / 103  105 / 125 146 / 135 190 / 186 295 / 228
+//   4096 <- 4096     25 /  62   43 /  55   52 /  57  72 /  59  88 /  99 129 / 109
+// so up to 768 tokens; in thousands of them more where the dense kernel's tiles (256 x 256 on 74 pairs) leave most of a wave empty, which
+// is not followed up here.
+constexpr int kEvenMost = 768, kEvenMostGated = 640;
 bool even_takes(int M) { return M <= kEvenMost; }
+// Gated blocks: where the tiles of the kernel that dequantises per tile (128 rows x up to 256 tokens, K cut where they are few) fit the SMs at once
+// that one is ahead, this / it: 2048 -> 2 x 5504 at 77 tokens 23 / 18 us, 256 33 / 24; 4096 -> 2 x 11008 42 / 60 and 76 / 74, at 512 (dense) 120 / 127,
+// 768 162 / 153.
+bool gated_even_takes(const LinearArgs &a)
+{
+    if (a.M > kEvenMostGated) return false;
+    if (a.kept) return true;
+    const long long tiles = (long long)((a.N + 127) / 128) * ((a.M + 255) / 256);
+    return tiles > 148;
+}
 size_t padded256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t thin_bytes(int M, int rank) { return padded256((size_t)M * ((rank + 63) / 64 * 64) * 2); }
 PrefillTuning prefill_tuning()
@@ -404,7 +422,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
             return FBQ_ERR_CUDA;
         }
     }
-    if (a.gate >= 0 && kernel == FBQ_KERNEL_PREFILL && even_takes(a.M)) return run_gated_even(a, ws, s);
+    if (a.gate >= 0 && kernel == FBQ_KERNEL_PREFILL && gated_even_takes(a)) return run_gated_even(a, ws, s);
     if (kernel == FBQ_KERNEL_PREFILL) {
         size_t have_c = (size_t)ws->n_counters, need_t = 0, need_p = 0;
         int need_c = 0;
@@ -473,14 +491,14 @@ int run_backward(Backward &b, cudaStream_t s)
         need += padded256(bytes);
         return at;
     };
-    const bool even = even_takes(g.M);
+    const bool even = even_takes(g.M), thin_first = g.rank > 0 && (even || grad_thin_first(g));
     ThinArgs t{};
     t.M = g.M; t.N = g.N; t.K = g.K; t.rank = g.rank; t.bf16 = g.bf16;
     t.s = ws;                                                    // (any address: where it will be is not known yet)
     t.t = factors ? ws : nullptr;
     const size_t M = g.M, thin = thin_bytes(g.M, g.rank);
     const size_t x_at = place(unpack ? M * g.K * 2 : 0), dy_at = place(b.kept ? M * g.N * 2 : 0), s_at = place(thin), t_at = place(factors ? thin : 0),
-                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), thin_at = place(even && g.rank > 0 ? thin_part_bytes(t) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
+                 part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), thin_at = place(thin_first ? thin_part_bytes(t) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
     cudaError_t e;
     size_t have_c = (size_t)ws->n_counters, need_w = 0, need_tags = 0;
     char *scratch = static_cast<char *>(ws->grad), *w16 = static_cast<char *>(ws->w16);
@@ -488,7 +506,7 @@ int run_backward(Backward &b, cudaStream_t s)
     ws->grad = scratch;
     if (e != cudaSuccess) return grow_status(e);
     grad_workspace_need(g, &need_w, &need_tags);
-    if (even) {
+    if (even || !g.dx) {
         need_w = need_tags = 0;
     }
     e = grow(w16, ws->w16_bytes, need_w, 1, s);
@@ -510,19 +528,18 @@ int run_backward(Backward &b, cudaStream_t s)
     }
     g.s16 = scratch + s_at;
     g.t16 = factors ? scratch + t_at : nullptr;
-    if (even) {
-        if (g.rank > 0) {
-            t.x = g.x; t.dy = g.dy; t.A = g.A; t.B = g.B; t.t = g.t16; t.s = g.s16; t.part = scratch + thin_at;
-            if (launch_thin(t, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
-        }
-        if (g.dx) {
-            EvenArgs v{};
-            v.x = g.dy; v.qw = g.qw; v.scales = g.scales; v.zeros = g.zeros; v.factor = g.A; v.thin = g.s16; v.y = g.dx; v.part = scratch + even_at;
-            v.M = g.M; v.N = g.N; v.K = g.K; v.bits = g.bits; v.rank = g.rank; v.gate = -1; v.bf16 = g.bf16;
-            if (launch_even(v, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
-        }
-    } else if (launch_grad(g, *ws, prefill_tuning(), s, &launches) != cudaSuccess) {
-        return FBQ_ERR_CUDA;
+    if (thin_first) {
+        t.x = g.x; t.dy = g.dy; t.A = g.A; t.B = g.B; t.t = g.t16; t.s = g.s16; t.part = scratch + thin_at;
+        if (launch_thin(t, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+        g.made = true;
+    }
+    if (g.dx && even) {
+        EvenArgs v{};
+        v.x = g.dy; v.qw = g.qw; v.scales = g.scales; v.zeros = g.zeros; v.factor = g.A; v.thin = g.s16; v.y = g.dx; v.part = scratch + even_at;
+        v.M = g.M; v.N = g.N; v.K = g.K; v.bits = g.bits; v.rank = g.rank; v.gate = -1; v.bf16 = g.bf16;
+        if (launch_even(v, ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
+    } else if (g.dx) {
+        if (launch_grad(g, *ws, prefill_tuning(), s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
     }
     if (factors && launch_factor_grads(g.dy, g.x, g.s16, g.t16, b.dA, b.dB, g.M, g.N, g.K, g.rank, b.kept != nullptr, g.bf16, scratch + part_at,
                                        ws->counters + kCtrStatus, g_opt.decode.pdl != 0, s, &launches) != cudaSuccess)

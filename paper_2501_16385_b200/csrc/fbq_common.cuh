@@ -158,9 +158,11 @@ struct GradArgs {
     const void *A, *B;
     void *dx;                     // [M][K] or none
     void *s16, *t16;              // scratch [M][rank rounded up to 64]: s and t in the activation type
+    bool made;                    // they are there
     int M, N, K, bits, rank;
     bool bf16;
 };
+bool grad_thin_first(const GradArgs &a);        // s and t are better made by launch_thin
 bool grad_supported(int M, int N, int K, int group, int rank);
 void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags);
 cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);

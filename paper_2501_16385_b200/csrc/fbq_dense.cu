@@ -414,7 +414,7 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
                     ready += n;
                     if (lane == 0) asm volatile("fence.proxy.async;" ::: "memory");
                 }
-                if (kb == kb_slab) {                             // t of this tile's tokens, from both CTAs of each t tile
+                if (kb == kb_slab && p.n_t > 0) {                // t of this tile's tokens, from both CTAs of each t tile
                     const int t0 = tt * p.tok / kTTok, t1 = (min(p.M, (tt + 1) * p.tok) + kTTok - 1) / kTTok;
                     for (int i = 2 * t0; i < 2 * t1;) {
                         const int n = wait_tags(p, [&] { return i + lane < 2 * t1 && load_acquire(t_tags + i + lane) == tag; }, 1, quit);
@@ -778,10 +778,11 @@ cudaError_t run_grad(const GradArgs &a, int k_first, int cols, bool first, Works
     p.nft = a.dx ? (cols + kFeat - 1) / kFeat : 0;
     p.tok = token_tile(a.M, p.nft, (a.N + kBK - 1) / kBK);
     p.ntt = (a.M + p.tok - 1) / p.tok;
-    p.n_t = a.rank > 0 ? (a.M + kTTok - 1) / kTTok : 0;
+    p.n_t = a.rank > 0 && !a.made ? (a.M + kTTok - 1) / kTTok : 0;
     p.n_t2 = a.rank > 0 && a.t16 && first ? p.n_t : 0;
     p.nkc = (a.N + kItemK - 1) / kItemK;
-    const int n_pairs = std::max(1, std::min(pairs_of_device(), p.n_t + p.nft * p.ntt + p.n_t2));
+    // (where there are fewer tiles than pairs the others dequantise)
+    const int n_pairs = p.nft > 0 ? pairs_of_device() : std::max(1, std::min(pairs_of_device(), p.n_t + p.n_t2));
     p.wave_ft = std::max(1, std::min(p.nft, (n_pairs + p.ntt - 1) / p.ntt));
     p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
     p.test_skip_flag = tune.test_skip_flag;
@@ -852,6 +853,24 @@ cudaError_t launch_dense(const LinearArgs &a, Workspace &ws, const PrefillTuning
         if (e == cudaSuccess) ++*launches;
     }
     return e;
+}
+
+// Tiles of s and t among those of dx cost a wave of pairs where they do not fit into the last one, and from some thousand tokens on more than a
+// launch of their own before this one.  Measured (us, in this launch / before it; INT4, rank 64, 4096 x 4096 INT3, rank 16):
+//                   768 tokens    1024       1536       2048       4096
+//   4096 <- 22016   200 / 218  220 / 239  448 / 387  481 / 430  881 / 815
+//   2048 <- 11008   112 / 130  116 / 128  171 / 144  181 / 175  311 / 326
+//   11008 <- 4096   150 / 125  164 / 135  199 / 201  249 / 233  502 / 449
+//   4096 <- 4096     57 /  68   59 /  73   99 / 101  108 / 108  185 / 181
+// A tile of s has as many blocks as one of dx, one of t K / N as many.
+bool grad_thin_first(const GradArgs &a)
+{
+    if (a.rank == 0) return false;
+    const int cols = launch_columns(a.N, a.K);
+    if (!a.dx || a.M > 1024 || cols < a.K) return true;
+    const int nft = (cols + kFeat - 1) / kFeat, tok = token_tile(a.M, nft, (a.N + kBK - 1) / kBK);
+    const int tiles = nft * ((a.M + tok - 1) / tok), pairs = pairs_of_device(), thin = (a.M + kTTok - 1) / kTTok;
+    return tiles + thin * std::max(1.0, (double)a.K / a.N) > (tiles + pairs - 1) / pairs * pairs;
 }
 
 bool grad_supported(int M, int N, int K, int group, int rank)

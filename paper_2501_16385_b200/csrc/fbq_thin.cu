@@ -198,10 +198,10 @@ template <typename T> __global__ void __launch_bounds__(256) thin_add_kernel(con
     static_cast<unsigned short *>(of_s ? p.s : p.t)[at] = to_bits16<T>(v);
 }
 
-// The plan: clusters as many as are resident at once (15 of eight CTAs).  Either their number goes to tiles of tokens, of 16 at least; or, where
-// a CTA then has a long contraction to go through (more than kLong blocks), tiles are wide and the contractions cut, each into shares of
-// about the same length.  One CTA reads some 60 bytes a nanosecond, and narrow tiles read A or B once each.
-constexpr int kLong = 16, kResident = 15;
+// The plan: CTAs of a cluster, tokens of a tile, and clusters that share a tile's contraction, such that what a CTA has to go through takes
+// least.  It reads some 60 bytes a nanosecond (A or B once per tile of tokens) and spends 4 us besides; clusters wait for one another where
+// more are wanted than the GPU holds at a time (one CTA per SM, and a cluster stays within one of the processing clusters).  Cuts cost
+// a launch and their sums' way through L2.  22016 rows of B at 333 tokens, rank 128: 22 us with eight CTAs a tile of 48 tokens and no cuts, 12 + 3 now.
 void plan(const ThinArgs &a, ThinParams &p, int *cluster)
 {
     p.M = a.M;
@@ -210,23 +210,39 @@ void plan(const ThinArgs &a, ThinParams &p, int *cluster)
     p.nrt = (p.rank_pad + kRows - 1) / kRows;
     p.blocks_t = a.t ? (a.K + kBK - 1) / kBK : 0;
     p.blocks_s = a.s ? (a.N + kBK - 1) / kBK : 0;
-    const int kinds = (a.t ? 1 : 0) + (a.s ? 1 : 0), deep = std::max(p.blocks_t, p.blocks_s);
-    int cs = 1;
-    while (2 * cs <= std::min(kMostCluster, deep / 2)) cs *= 2;
-    *cluster = cs;
-    auto tiles = [&](int room) {
-        p.tok = std::min(kMostTok, ((a.M + room - 1) / room + 15) / 16 * 16);
-        p.ntt = (a.M + p.tok - 1) / p.tok;
-    };
-    tiles(std::max(1, kResident * kMostCluster / (cs * p.nrt * kinds)));
-    p.cuts_s = a.s ? 1 : 0;
-    p.cuts_t = a.t ? 1 : 0;
-    if (deep <= kLong * cs) return;
-    tiles((a.M + kMostTok - 1) / kMostTok);
-    const int sets = p.ntt * p.nrt, all = sets * (p.blocks_s + p.blocks_t);
-    auto cuts = [&](int blocks) { return blocks ? std::max(1, (int)((long long)blocks * kResident / all)) : 0; };
-    p.cuts_s = cuts(p.blocks_s);
-    p.cuts_t = cuts(p.blocks_t);
+    static const int resident[4] = {148, 74, 33, 15};
+    double least = 1e30;
+    const int most = std::max(p.blocks_t, p.blocks_s);
+    for (int c = 0; (1 << c) <= kMostCluster; ++c) {
+        const int cs = 1 << c;
+        if (c > 0 && 2 * cs > most) break;
+        for (int tok = 16; tok <= kMostTok; tok += 16) {
+            const int ntt = (a.M + tok - 1) / tok, sets = ntt * p.nrt;
+            if (tok > 16 && (a.M + tok - 17) / (tok - 16) == ntt) continue;          // (fewer tokens make as many tiles)
+            auto piece = [&](int blocks, int cuts) { return (double)((blocks + cs * cuts - 1) / (cs * cuts)) * (kABytes + tok * kBK * 2) / 60e3 + 4.0; };
+            for (int cut = 1; cut <= 8; cut *= 2) {
+                // of s and t the longer contraction is cut more often
+                const int cuts_s = p.blocks_s ? std::max(1, std::min(cut, cut * p.blocks_s / most)) : 0, cuts_t = p.blocks_t ? std::max(1, std::min(cut, cut * p.blocks_t / most)) : 0;
+                double longest = 0, all = 0;
+                if (cuts_s) {
+                    longest = piece(p.blocks_s, cuts_s);
+                    all = sets * cuts_s * longest;
+                }
+                if (cuts_t) {
+                    longest = std::max(longest, piece(p.blocks_t, cuts_t));
+                    all += sets * cuts_t * piece(p.blocks_t, cuts_t);
+                }
+                const double cost = std::max(longest, all / resident[c]) + (cut > 1 ? 8.0 : 0.0);
+                if (cost >= least) continue;
+                least = cost;
+                *cluster = cs;
+                p.tok = tok;
+                p.ntt = ntt;
+                p.cuts_s = cuts_s;
+                p.cuts_t = cuts_t;
+            }
+        }
+    }
 }
 
 template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)

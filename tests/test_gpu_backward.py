@@ -281,7 +281,7 @@ def test_results_end_where_they_should():
 
 def test_a_wait_that_runs_out():
     """s that its tiles do not announce: the main tiles' bounded wait gives up and the status tells; the next call is fine."""
-    N, K, bits, rank, dt, M = 264, 384, 4, 64, torch.float16, 1500
+    N, K, bits, rank, dt, M = 264, 384, 4, 64, torch.float16, 900
     layer = Layer(fbq, N, K, bits, rank, dt, seed=1)
     dy, x = normal(M, N, dt, seed=2, scale=0.1), normal(M, K, dt, seed=3)
     want = fbq.linear_backward(dy, x, *layer.tensors, 128, bits)
