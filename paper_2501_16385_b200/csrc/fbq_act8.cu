@@ -1,5 +1,6 @@
 // Activations in 8 bits: the form in which a training step keeps them between its passes, and what the gated block's backward
-// pass makes of it.  All three kernels are bound by memory: one pass, 16 bytes a lane and access where rows allow.
+// pass makes of it.  All three kernels are bound by memory: one pass, 16 bytes a lane and access where rows allow, the lanes of a kernel with
+// two accesses each on their way, places in 32 bits where they fit (a division of 64 bits takes as long as the rest of a lane's work).
 #include "fbq_common.cuh"
 #include "fbq_dequant.cuh"
 #include "fbq_gate.cuh"
@@ -8,6 +9,7 @@ namespace fbq {
 namespace {
 
 constexpr int kThr = 256;
+constexpr int kTwice = 2;                                    // groups, or units, of a lane, a block's width apart
 constexpr int kLanes = 16, kEach = kKeptGroup / kLanes;       // lanes of a group, values of a lane
 
 template <typename T> __device__ __forceinline__ float2 unpair(uint32_t v);
@@ -17,23 +19,14 @@ template <> __device__ __forceinline__ float2 unpair<__nv_bfloat16>(uint32_t v)
     return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
 }
 
-// Sixteen lanes take a group: the largest |v| crosses lanes once, codes and values do not.  WIDE: rows of whole units of eight.
+// One group, sixteen lanes: this lane's n values (WIDE: in `raw`, zeros where there are none).
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kThr) pack_kernel(const T *__restrict__ x, int8_t *__restrict__ codes, float *__restrict__ scales, long long groups, int K, int G)
+__device__ __forceinline__ void pack_group(const T *src, const uint4 &raw, int8_t *dst, float *scale_at, int n, bool first)
 {
-    const long long at = (long long)blockIdx.x * (kThr / kLanes) + threadIdx.x / kLanes;
-    const int l = threadIdx.x % kLanes;
-    const bool on = at < groups;
-    const long long m = on ? at / G : 0;
-    const int g = on ? (int)(at - m * G) : 0, k = g * kKeptGroup + l * kEach, n = on ? min(kEach, K - k) : 0;     // n <= 0: nothing
-    const T *src = x + m * K + k;
     float v[kEach] = {};
     if (WIDE) {
-        if (n > 0) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(src));
-            const float2 a = unpair<T>(w.x), b = unpair<T>(w.y), c = unpair<T>(w.z), d = unpair<T>(w.w);
-            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
-        }
+        const float2 a = unpair<T>(raw.x), b = unpair<T>(raw.y), c = unpair<T>(raw.z), d = unpair<T>(raw.w);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
@@ -46,12 +39,11 @@ __global__ void __launch_bounds__(kThr) pack_kernel(const T *__restrict__ x, int
     for (int o = 1; o < kLanes; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     float scale, inverse;
     kept_scale(top, scale, inverse);
-    if (on && l == 0) scales[at] = scale;
-    int8_t *dst = codes + m * K + k;
+    if (first) *scale_at = scale;
     if (WIDE) {
         uint32_t w[2] = {0u, 0u};
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) w[i / 4] |= ((uint32_t)kept_code(v[i], inverse) & 0xFFu) << (8 * (i % 4));
+        for (int i = 0; i < kEach; ++i) w[i / 4] |= kept_code(v[i], inverse) << (8 * (i % 4));
         if (n > 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
@@ -60,62 +52,108 @@ __global__ void __launch_bounds__(kThr) pack_kernel(const T *__restrict__ x, int
     }
 }
 
+// Sixteen lanes take a group: the largest |v| crosses lanes once, codes and values do not.  WIDE: rows of whole units of eight.
+template <typename T, bool WIDE, typename I>
+__global__ void __launch_bounds__(kThr) pack_kernel(const T *__restrict__ x, int8_t *__restrict__ codes, float *__restrict__ scales, I groups, int K, int G)
+{
+    const int l = threadIdx.x % kLanes;
+    I at[kTwice];
+    int n[kTwice];                                               // <= 0: nothing
+    size_t to[kTwice];
+    uint4 raw[kTwice];
+#pragma unroll
+    for (int j = 0; j < kTwice; ++j) {
+        at[j] = ((I)blockIdx.x * kTwice + j) * (kThr / kLanes) + threadIdx.x / kLanes;
+        const I m = at[j] < groups ? at[j] / G : 0;
+        const int k = (int)(at[j] < groups ? at[j] - m * G : 0) * kKeptGroup + l * kEach;
+        n[j] = at[j] < groups ? min(kEach, K - k) : 0;
+        to[j] = (size_t)m * K + k;
+        if (WIDE) raw[j] = n[j] > 0 ? __ldg(reinterpret_cast<const uint4 *>(x + to[j])) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int j = 0; j < kTwice; ++j) pack_group<T, WIDE>(x + to[j], raw[j], codes + to[j], scales + at[j], n[j], at[j] < groups && l == 0);
+}
+
 __device__ __forceinline__ float byte_to_float(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
 // A lane turns EACH codes of a row (16, 8 or 1; K a multiple of it): code * scale, rounded once.
-template <typename T, int EACH>
-__global__ void __launch_bounds__(kThr) unpack_kernel(const int8_t *__restrict__ codes, const float *__restrict__ scales, T *__restrict__ x, long long units, int K, int G)
+template <typename T, int EACH, typename I>
+__global__ void __launch_bounds__(kThr) unpack_kernel(const int8_t *__restrict__ codes, const float *__restrict__ scales, T *__restrict__ x, I units, int K, int G)
 {
-    const long long at = (long long)blockIdx.x * kThr + threadIdx.x;
-    if (at >= units) return;
-    const int per = K / EACH;
-    const long long m = at / per;
-    const int k = (int)(at - m * per) * EACH;
-    const float s = __ldg(scales + m * G + k / kKeptGroup);
-    if constexpr (EACH == 1) {
-        x[at] = ActTraits<T>::from_float((float)codes[at] * s);
-    } else {
-        uint32_t w[EACH / 4], o[EACH / 2];
+    const I per = K / EACH;
+    I at[kTwice];
+    float s[kTwice];
+    uint32_t w[kTwice][EACH / 4 + 1];
+#pragma unroll
+    for (int j = 0; j < kTwice; ++j) {
+        at[j] = ((I)blockIdx.x * kTwice + j) * kThr + threadIdx.x;
+        if (at[j] >= units) continue;
+        const I m = at[j] / per;
+        s[j] = __ldg(scales + (size_t)m * G + (int)(at[j] - m * per) * EACH / kKeptGroup);
+        const int8_t *src = codes + (size_t)at[j] * EACH;
         if constexpr (EACH == 16) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(codes + at * EACH));
-            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(src));
+            w[j][0] = q.x; w[j][1] = q.y; w[j][2] = q.z; w[j][3] = q.w;
+        } else if constexpr (EACH == 8) {
+            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(src));
+            w[j][0] = q.x; w[j][1] = q.y;
         } else {
-            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(codes + at * EACH));
-            w[0] = q.x; w[1] = q.y;
+            w[j][0] = (uint8_t)*src;
         }
+    }
 #pragma unroll
-        for (int i = 0; i < EACH / 2; ++i) o[i] = P2<T>::pack(byte_to_float(w[i / 2], 2 * i % 4) * s, byte_to_float(w[i / 2], 2 * i % 4 + 1) * s);
+    for (int j = 0; j < kTwice; ++j) {
+        if (at[j] >= units) continue;
+        T *dst = x + (size_t)at[j] * EACH;
+        if constexpr (EACH == 1) {
+            *dst = ActTraits<T>::from_float(byte_to_float(w[j][0], 0) * s[j]);
+        } else {
+            uint32_t o[EACH / 2];
 #pragma unroll
-        for (int i = 0; i < EACH / 8; ++i) reinterpret_cast<uint4 *>(x + at * EACH)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            for (int i = 0; i < EACH / 2; ++i) o[i] = P2<T>::pack(byte_to_float(w[j][i / 2], 2 * i % 4) * s[j], byte_to_float(w[j][i / 2], 2 * i % 4 + 1) * s[j]);
+#pragma unroll
+            for (int i = 0; i < EACH / 8; ++i) reinterpret_cast<uint4 *>(dst)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        }
     }
 }
 
 // dp of the gated block: p[16i + j] the gate's, p[16i + 8 + j] the up projection's value that met in h[8i + j], both as they were kept:
 // dp_gate = dh p_up f'(p_gate), dp_up = dh f(p_gate), rounded once (they are operands of tensor-core products next).  A lane
 // takes eight columns of h.
-template <typename T>
+template <typename T, typename I>
 __global__ void __launch_bounds__(kThr) gate_grad_kernel(const T *__restrict__ dh, const int8_t *__restrict__ codes, const float *__restrict__ scales, T *__restrict__ dp,
-                                                         long long units, int per, int G, int fn)
+                                                         I units, I per, int G, int fn)
 {
-    const long long at = (long long)blockIdx.x * kThr + threadIdx.x;
-    if (at >= units) return;
-    const long long m = at / per;
-    const float s = __ldg(scales + m * G + (int)(at - m * per) / (kKeptGroup / 16));
-    const uint4 q = __ldg(reinterpret_cast<const uint4 *>(codes) + at), d = __ldg(reinterpret_cast<const uint4 *>(dh) + at);
-    const uint32_t gate[2] = {q.x, q.y}, up[2] = {q.z, q.w}, dd[4] = {d.x, d.y, d.z, d.w};
-    uint32_t og[4], ou[4];
+    I at[kTwice];
+    float s[kTwice];
+    uint4 q[kTwice], d[kTwice];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 e = unpair<T>(dd[i]);
-        float f0, f1, df0, df1;
-        gate_both(fn, byte_to_float(gate[i / 2], 2 * i % 4) * s, f0, df0);
-        gate_both(fn, byte_to_float(gate[i / 2], 2 * i % 4 + 1) * s, f1, df1);
-        og[i] = P2<T>::pack(e.x * (byte_to_float(up[i / 2], 2 * i % 4) * s) * df0, e.y * (byte_to_float(up[i / 2], 2 * i % 4 + 1) * s) * df1);
-        ou[i] = P2<T>::pack(e.x * f0, e.y * f1);
+    for (int j = 0; j < kTwice; ++j) {
+        at[j] = ((I)blockIdx.x * kTwice + j) * kThr + threadIdx.x;
+        if (at[j] >= units) continue;
+        const I m = at[j] / per;
+        s[j] = __ldg(scales + (size_t)m * G + (int)(at[j] - m * per) / (kKeptGroup / 16));
+        q[j] = __ldg(reinterpret_cast<const uint4 *>(codes) + at[j]);
+        d[j] = __ldg(reinterpret_cast<const uint4 *>(dh) + at[j]);
     }
-    uint4 *dst = reinterpret_cast<uint4 *>(dp) + 2 * at;
-    dst[0] = make_uint4(og[0], og[1], og[2], og[3]);
-    dst[1] = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+#pragma unroll
+    for (int j = 0; j < kTwice; ++j) {
+        if (at[j] >= units) continue;
+        const uint32_t gate[2] = {q[j].x, q[j].y}, up[2] = {q[j].z, q[j].w}, dd[4] = {d[j].x, d[j].y, d[j].z, d[j].w};
+        uint32_t og[4], ou[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 e = unpair<T>(dd[i]);
+            float f0, f1, df0, df1;
+            gate_both(fn, byte_to_float(gate[i / 2], 2 * i % 4) * s[j], f0, df0);
+            gate_both(fn, byte_to_float(gate[i / 2], 2 * i % 4 + 1) * s[j], f1, df1);
+            og[i] = P2<T>::pack(e.x * (byte_to_float(up[i / 2], 2 * i % 4) * s[j]) * df0, e.y * (byte_to_float(up[i / 2], 2 * i % 4 + 1) * s[j]) * df1);
+            ou[i] = P2<T>::pack(e.x * f0, e.y * f1);
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(dp) + 2 * (size_t)at[j];
+        dst[0] = make_uint4(og[0], og[1], og[2], og[3]);
+        dst[1] = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+    }
 }
 
 // Rows of `units` pieces of P: eight of the gate, eight of the up projection, and so on.  `half` > 0: a row of the result has twice the
@@ -143,22 +181,29 @@ unsigned blocks_for(long long n, int per) { return (unsigned)((n + per - 1) / pe
 // Grids have 31 bits.
 bool fits(long long n, int per) { return n <= (long long)per * 0x7FFFFFFF; }
 
+// `go` with the number of units in 32 bits where they and what a block may count beyond them fit, else in 64.
+template <typename F> cudaError_t by_size(long long units, int per_block, F go)
+{
+    if (!fits(units, per_block)) return cudaErrorInvalidConfiguration;
+    const unsigned grid = blocks_for(units, per_block);
+    if (units < (1ll << 31)) go((unsigned)units, grid);
+    else go(units, grid);
+    return cudaGetLastError();
+}
 template <typename T> cudaError_t pack(const void *x, int8_t *codes, float *scales, int M, int K, cudaStream_t s)
 {
     const int G = (K + kKeptGroup - 1) / kKeptGroup;
-    const long long groups = (long long)M * G;
-    if (!fits(groups, kThr / kLanes)) return cudaErrorInvalidConfiguration;
-    const unsigned grid = blocks_for(groups, kThr / kLanes);
-    if (K % kEach == 0) pack_kernel<T, true><<<grid, kThr, 0, s>>>(static_cast<const T *>(x), codes, scales, groups, K, G);
-    else pack_kernel<T, false><<<grid, kThr, 0, s>>>(static_cast<const T *>(x), codes, scales, groups, K, G);
-    return cudaGetLastError();
+    return by_size((long long)M * G, kTwice * (kThr / kLanes), [&](auto groups, unsigned grid) {
+        using I = decltype(groups);
+        if (K % kEach == 0) pack_kernel<T, true, I><<<grid, kThr, 0, s>>>(static_cast<const T *>(x), codes, scales, groups, K, G);
+        else pack_kernel<T, false, I><<<grid, kThr, 0, s>>>(static_cast<const T *>(x), codes, scales, groups, K, G);
+    });
 }
 template <typename T, int EACH> cudaError_t unpack_by(const int8_t *codes, const float *scales, void *x, int M, int K, cudaStream_t s)
 {
-    const long long units = (long long)M * (K / EACH);
-    if (!fits(units, kThr)) return cudaErrorInvalidConfiguration;
-    unpack_kernel<T, EACH><<<blocks_for(units, kThr), kThr, 0, s>>>(codes, scales, static_cast<T *>(x), units, K, (K + kKeptGroup - 1) / kKeptGroup);
-    return cudaGetLastError();
+    return by_size((long long)M * (K / EACH), kTwice * kThr, [&](auto units, unsigned grid) {
+        unpack_kernel<T, EACH, decltype(units)><<<grid, kThr, 0, s>>>(codes, scales, static_cast<T *>(x), units, K, (K + kKeptGroup - 1) / kKeptGroup);
+    });
 }
 template <typename T> cudaError_t unpack(const int8_t *codes, const float *scales, void *x, int M, int K, cudaStream_t s)
 {
@@ -181,14 +226,13 @@ cudaError_t launch_act8_unpack(const int8_t *codes, const float *scales, void *x
 cudaError_t launch_gate_grad(const void *dh, const int8_t *codes, const float *scales, void *dp, int M, int N, int fn, bool bf16, cudaStream_t s)
 {
     const int per = N / 16, G = (N + kKeptGroup - 1) / kKeptGroup;
-    const long long units = (long long)M * per;
-    if (!fits(units, kThr)) return cudaErrorInvalidConfiguration;
-    if (bf16)
-        gate_grad_kernel<__nv_bfloat16><<<blocks_for(units, kThr), kThr, 0, s>>>(static_cast<const __nv_bfloat16 *>(dh), codes, scales, static_cast<__nv_bfloat16 *>(dp),
-                                                                                 units, per, G, fn);
-    else
-        gate_grad_kernel<__half><<<blocks_for(units, kThr), kThr, 0, s>>>(static_cast<const __half *>(dh), codes, scales, static_cast<__half *>(dp), units, per, G, fn);
-    return cudaGetLastError();
+    return by_size((long long)M * per, kTwice * kThr, [&](auto units, unsigned grid) {
+        using I = decltype(units);
+        if (bf16)
+            gate_grad_kernel<__nv_bfloat16, I><<<grid, kThr, 0, s>>>(static_cast<const __nv_bfloat16 *>(dh), codes, scales, static_cast<__nv_bfloat16 *>(dp), units, (I)per, G, fn);
+        else
+            gate_grad_kernel<__half, I><<<grid, kThr, 0, s>>>(static_cast<const __half *>(dh), codes, scales, static_cast<__half *>(dp), units, (I)per, G, fn);
+    });
 }
 
 // Rows of `bytes` bytes each, F of either branch, in pieces of 16, 4 or 2 bytes.

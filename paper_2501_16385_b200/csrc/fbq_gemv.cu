@@ -1175,9 +1175,11 @@ Plan make_plan_on(const LinearArgs &a, const GemvTuning &tune, int per_sm)
     p.t_kb = 0;
     const int nblk = (a.K + kTKB - 1) / kTKB;
     if (a.rank > 0) {
-        const int per = std::min(kCW, std::max(1, (int)((128 * 1024) / ((size_t)a.rank * 128))));     // one block per warp
+        // (a gated layer of rank 128 on two CTAs per SM: chunks that leave its share of shared memory to them)
+        const size_t chunk = a.gate >= 0 && per_sm == 2 && a.rank > 64 ? 96 * 1024 : 128 * 1024;
+        const int per = std::min(kCW, std::max(1, (int)(chunk / ((size_t)a.rank * 128))));     // one block per warp
         p.n_t = std::min(64, std::max((nblk + per - 1) / per, std::min(nblk, 8)));
-        if (tune.main_ctas == 0) p.n_t = balanced_t_ctas(p.n_t, nblk, a.rank, p.NT, want);
+        if (tune.main_ctas == 0 && chunk == 128 * 1024) p.n_t = balanced_t_ctas(p.n_t, nblk, a.rank, p.NT, want);
         p.t_kb = (nblk + p.n_t - 1) / p.n_t;
         p.n_t = (nblk + p.t_kb - 1) / p.t_kb;
     }
@@ -1267,7 +1269,7 @@ Plan make_plan_on(const LinearArgs &a, const GemvTuning &tune, int per_sm)
 // the batch, which is faster than either (37.9); a mix by size was worse in a row (53.6).
 Plan make_plan(const LinearArgs &a, const GemvTuning &tune)
 {
-    if (tune.max_ctas == 0 && tune.main_ctas == 0 && a.rank <= 64 && !(a.bits == 3 && a.rank == 0 && a.M == 1)) {
+    if (tune.max_ctas == 0 && tune.main_ctas == 0 && (a.gate >= 0 || (a.rank <= 64 && !(a.bits == 3 && a.rank == 0 && a.M == 1)))) {
         const Plan pl = make_plan_on(a, tune, 2);
         if (pl.ok) return pl;
     }
@@ -1283,7 +1285,7 @@ const Plan &plan_for(const LinearArgs &a, const GemvTuning &tune)
         Plan plan;
     };
     static thread_local Entry table[16];
-    const int key[9] = {a.M, a.N, a.K, a.bits, a.rank, tune.max_ctas, tune.poll_limit, tune.test_skip_arrive, tune.main_ctas};
+    const int key[9] = {a.M, a.N, a.K, a.gate >= 0 ? -a.bits : a.bits, a.rank, tune.max_ctas, tune.poll_limit, tune.test_skip_arrive, tune.main_ctas};
     unsigned h = 0;
     for (int k : key) h = (h ^ (unsigned)k) * 0x9E3779B1u;
     Entry &e = table[h >> 28];

@@ -245,13 +245,28 @@ void plan(const ThinArgs &a, ThinParams &p, int *cluster)
     }
 }
 
+// The last plan of this host thread is kept: it holds sizes, no addresses, and a step's calls ask for it twice each.
+void plan_for(const ThinArgs &a, ThinParams &p, int *cluster)
+{
+    static thread_local int key[6] = {}, cs = 0;
+    static thread_local ThinParams kept{};
+    const int want[6] = {a.M, a.N, a.K, a.rank, a.t != nullptr, a.s != nullptr};
+    if (cs == 0 || !std::equal(want, want + 6, key)) {
+        kept = ThinParams{};
+        plan(a, kept, &cs);
+        std::copy(want, want + 6, key);
+    }
+    p = kept;
+    *cluster = cs;
+}
+
 template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, cudaStream_t s, int *launches)
 {
     const CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
     ThinParams p{};
     int cs = 1;
-    plan(a, p, &cs);
+    plan_for(a, p, &cs);
     p.t = a.t; p.s = a.s; p.status = status;
     p.part = p.cuts_s > 1 || p.cuts_t > 1 ? static_cast<float *>(a.part) : nullptr;
     p.n_s = p.ntt * p.nrt * p.cuts_s;
@@ -307,7 +322,7 @@ size_t thin_part_bytes(const ThinArgs &a)
 {
     ThinParams p{};
     int cs;
-    plan(a, p, &cs);
+    plan_for(a, p, &cs);
     return p.cuts_s > 1 || p.cuts_t > 1 ? (size_t)(p.cuts_s + p.cuts_t) * p.M * p.rank_pad * sizeof(float) : 0;
 }
 
