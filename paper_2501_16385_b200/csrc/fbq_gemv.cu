@@ -732,9 +732,16 @@ __device__ __forceinline__ bool epilogue(const GemvParams &p, uint8_t *smem, con
         // Tell that this CTA has read t (nobody waits for the add; a t CTA clears up once all have told).
         if (lane == 0) atomicAdd(p.ctr + 1, 1);
         // the largest |sum| of the warp: non-negative floats order like their bit patterns, so one integer reduction does
-        // (a NaN or Inf among them ends up at the top and is clamped below, as before)
-        const uint32_t amax_bits = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));
+        uint32_t amax_bits = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));
         __syncwarp();
+        if (amax_bits > 0x7F7FFFFFu) {                           // an infinite t is its token's alone: the other's scale is that of what is finite
+            amax_bits = 0u;
+            for (int i = lane; i < M * rank; i += 32) {
+                const uint32_t v = __float_as_uint(s_t[i]) & 0x7FFFFFFFu;
+                if (v <= 0x7F7FFFFFu) amax_bits = max(amax_bits, v);
+            }
+            amax_bits = __reduce_max_sync(0xffffffffu, amax_bits);
+        }
         // a power of two that puts the largest |t| near 2^14 keeps both terms inside fp16
         const uint32_t ex = min(max(amax_bits >> 23, 1u), 254u);
         const uint32_t sb = min(max(268u - ex, 1u), 254u);

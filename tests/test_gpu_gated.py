@@ -72,6 +72,72 @@ def test_products_kept_in_8_bits(M, N, K, bits, rank, dtype, fn):
     assert int(codes.abs().max()) <= 127 and bool((pad(codes.abs().int(), (0, -N % 128)).view(M, -1, 128).amax(2) == 127).all())
 
 
+@pytest.mark.parametrize("M", [16, 40, 95, 112, 160, 176, 192, 193, 400, 640, 641])
+@pytest.mark.parametrize("rank", [16, 112, 192, 256])
+def test_products_kept_by_tiles_of_tokens(M, rank):
+    """Every depth of the rings, odd and even numbers of the sub-branch's blocks, both sides of the size at which kernels change."""
+    N, K, bits, dt = 1168, 640, 3 if rank > 128 else 4, torch.bfloat16
+    layer = Layer(fbq, N, K, bits, rank, dt, seed=M, gated=True)
+    x = inputs(M, K, dt, seed=7)
+    h, codes, scales = fbq.gated(x, *layer.tensors, N, 128, bits, save=True)
+    assert fbq.poll_status() == 0
+    p, off = layer.products(x)
+    check(h, *hidden("silu", p, off, dt), "h")
+    step = scales.double().repeat_interleave(128, 1)[:, :N]
+    check(kept64(codes, scales), p, off + step * (0.5 + 128 * 2.0**-22), "kept products")
+
+
+@pytest.mark.parametrize("save", [False, True])
+def test_weights_in_several_launches(save):
+    """A layer whose 16-bit copy of the weights is beyond one launch's scratch: rows in parts."""
+    M, N, K, bits, rank, dt = 700, 131072 + 144, 2176, 4, 16, torch.float16
+    layer = Layer(fbq, N, K, bits, rank, dt, seed=1, gated=True)
+    x = inputs(M, K, dt, seed=2)
+    got = fbq.gated(x, *layer.tensors, N, 128, bits, save=save)
+    p, off = layer.products(x)
+    check(got[0] if save else got, *hidden("silu", p, off, dt), "h")
+    if save:
+        step = got[2].double().repeat_interleave(128, 1)[:, :N]
+        check(kept64(*got[1:]), p, off + step * (0.5 + 128 * 2.0**-22), "kept products")
+
+
+def test_scratch_does_not_grow_in_a_capture():
+    N, K, bits, dt = 272, 256, 4, torch.float16
+    layer = Layer(fbq, N, K, bits, 32, dt, seed=23, gated=True)
+    for M in (50, 700):                                         # both kernels that keep products
+        x = inputs(M, K, dt, seed=M)
+        stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(stream), pytest.raises(fbq.FbqError) as refused:
+            with torch.cuda.graph(graph, stream=stream):
+                fbq.gated(x, *layer.tensors, N, 128, bits, save=True)
+        assert refused.value.code == -2
+        del graph
+        with torch.cuda.stream(stream):
+            h, *_ = fbq.gated(x, *layer.tensors, N, 128, bits, save=True)
+        stream.synchronize()
+        check(h, *hidden("silu", *layer.products(x), dt), "h")
+
+
+@pytest.mark.parametrize("M", [2, 12, 200, 700])
+def test_calls_of_two_streams_at_once(M):
+    N, K, bits, dt = 1040, 1152, 4, torch.float16
+    layer = Layer(fbq, N, K, bits, 32, dt, seed=24, gated=True)
+    xs = [inputs(M, K, dt, seed=i) for i in range(2)]
+    want = [fbq.gated(x, *layer.tensors, N, 128, bits, save=M >= 200) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [None, None]
+    for _ in range(5):
+        for i, x in enumerate(xs):
+            with torch.cuda.stream(streams[i]):
+                got[i] = fbq.gated(x, *layer.tensors, N, 128, bits, save=M >= 200)
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, w)) if M >= 200 else torch.equal(g, w)
+
+
 @pytest.mark.parametrize("M", [1, 3, 40])
 def test_a_gated_layer_is_an_ordinary_layer(M):
     """fbq_gated_layer's rows, checked through fbq.linear of the branches and of the whole, and h of it."""
@@ -115,8 +181,8 @@ def test_large_and_extreme_products(M):
 
 
 @pytest.mark.parametrize("rank", [0, 32])
-@pytest.mark.parametrize("M", [4, 16])
-def test_infinite_x_on_the_split_kernel(M, rank):
+@pytest.mark.parametrize("M", [4, 16, 40, 700])
+def test_infinite_x(M, rank):
     """An infinite x makes every product of its token infinite or NaN as the sum of products does, so h is what the gate makes of that;
     other tokens do not notice."""
     N, K, dt = 272, 384, torch.float16
@@ -138,6 +204,25 @@ def test_infinite_x_on_the_split_kernel(M, rank):
     assert torch.equal(torch.isnan(h[1]), torch.isnan(want.half()))
     finite = ~torch.isnan(want)
     assert torch.equal(h[1].double()[finite], want[finite])
+
+
+@pytest.mark.parametrize("rank", [0, 32])
+def test_infinite_x_of_two_tokens(rank):
+    """The streaming kernel holds x in fixed point: a group with an infinite value is NaN, and so is all of its token, and no other."""
+    N, K, dt = 272, 384, torch.float16
+    layer = Layer(fbq, N, K, 4, rank, dt, seed=13)
+    x = inputs(2, K, dt, seed=14)
+    for call in (fbq.linear, fbq.gated):
+        for bad in (float("inf"), float("-inf"), float("nan")):
+            broken = x.clone()
+            broken[1, 5] = bad
+            out = call(broken, *layer.tensors, N, 128, 4)
+            assert bool(torch.isnan(out[1]).all())
+            p, off = layer.products(torch.stack((x[0], x[0])))   # (the other token's t has its own scale now)
+            if call is fbq.linear:
+                check(out[:1], p[:1], off[:1] + p[:1].abs() * half_step(dt) + 2.0**-24, "y")
+            else:
+                check(out[:1], *(v[:1] for v in hidden("silu", p, off, dt)), "h")
 
 
 def test_rows_of_other_memory_are_left_alone():
