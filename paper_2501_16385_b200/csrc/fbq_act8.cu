@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThr) gate_grad_kernel(const T *__restrict__ d
     }
 }
 
-// Rows of `units` pieces of P: eight of the gate, eight of the up projection, and so on.  `half` > 0: a row of the result has twice the
+// Rows of `units` pieces of P: eight of the gate, eight of the up projection, and so on.  `padded`: a row of the result has twice the
 // pieces, its own in its branch's half, zeros in the other.
 template <typename P>
 __global__ void __launch_bounds__(kThr) interleave_kernel(const P *__restrict__ gate, const P *__restrict__ up, P *__restrict__ out, long long total, int units, int padded)
@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(kThr) interleave_kernel(const P *__restrict__ 
     out[at] = (is_up ? up : gate)[row * units + u];
 }
 
+int groups_of(int K) { return (K - 1) / kKeptGroup + 1; }          // (K + 127 may be beyond 31 bits)
 unsigned blocks_for(long long n, int per) { return (unsigned)((n + per - 1) / per); }
 // Grids have 31 bits.
 bool fits(long long n, int per) { return n <= (long long)per * 0x7FFFFFFF; }
@@ -192,7 +193,7 @@ template <typename F> cudaError_t by_size(long long units, int per_block, F go)
 }
 template <typename T> cudaError_t pack(const void *x, int8_t *codes, float *scales, int M, int K, cudaStream_t s)
 {
-    const int G = (K + kKeptGroup - 1) / kKeptGroup;
+    const int G = groups_of(K);
     return by_size((long long)M * G, kTwice * (kThr / kLanes), [&](auto groups, unsigned grid) {
         using I = decltype(groups);
         if (K % kEach == 0) pack_kernel<T, true, I><<<grid, kThr, 0, s>>>(static_cast<const T *>(x), codes, scales, groups, K, G);
@@ -202,7 +203,7 @@ template <typename T> cudaError_t pack(const void *x, int8_t *codes, float *scal
 template <typename T, int EACH> cudaError_t unpack_by(const int8_t *codes, const float *scales, void *x, int M, int K, cudaStream_t s)
 {
     return by_size((long long)M * (K / EACH), kTwice * kThr, [&](auto units, unsigned grid) {
-        unpack_kernel<T, EACH, decltype(units)><<<grid, kThr, 0, s>>>(codes, scales, static_cast<T *>(x), units, K, (K + kKeptGroup - 1) / kKeptGroup);
+        unpack_kernel<T, EACH, decltype(units)><<<grid, kThr, 0, s>>>(codes, scales, static_cast<T *>(x), units, K, groups_of(K));
     });
 }
 template <typename T> cudaError_t unpack(const int8_t *codes, const float *scales, void *x, int M, int K, cudaStream_t s)
@@ -225,7 +226,7 @@ cudaError_t launch_act8_unpack(const int8_t *codes, const float *scales, void *x
 
 cudaError_t launch_gate_grad(const void *dh, const int8_t *codes, const float *scales, void *dp, int M, int N, int fn, bool bf16, cudaStream_t s)
 {
-    const int per = N / 16, G = (N + kKeptGroup - 1) / kKeptGroup;
+    const int per = N / 16, G = groups_of(N);
     return by_size((long long)M * per, kTwice * kThr, [&](auto units, unsigned grid) {
         using I = decltype(units);
         if (bf16)

@@ -11,6 +11,7 @@
 #include <utility>
 
 #include "fbq_common.cuh"
+#include "fbq_gate.cuh"
 
 namespace fbq {
 void decode_set_test_switch(int t_late);
@@ -782,7 +783,7 @@ int fbq_linear_bf16(const void *x, const uint32_t *qweight, const void *scales, 
 static int check_gated(int M, int N, int K, int group, int bits, int rank, int gate)
 {
     if (!well_formed(M, N, K, group, bits, rank) || (gate != FBQ_GATE_SILU && gate != FBQ_GATE_GELU) || N % 2 || rank % 2) return FBQ_ERR_BADARG;
-    return group == kGroupFast && N % 16 == 0 && rank % 16 == 0 && rank <= kMaxRank && M <= (1 << 22) ? FBQ_OK : FBQ_ERR_UNSUPPORTED;
+    return group == kGroupFast && N % 16 == 0 && rank % 16 == 0 && rank <= kMaxRank && M <= (1 << 22) && N <= kMostSide && K <= kMostSide ? FBQ_OK : FBQ_ERR_UNSUPPORTED;
 }
 
 static bool any_misaligned(std::initializer_list<const void *> ps)
@@ -804,13 +805,18 @@ int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void 
     const size_t sc = (size_t)(K / group) * 2, a_bytes = (size_t)rank * K * 2;
     if (launch_interleave(gate_q, up_q, qweight, F, (size_t)K / 8 * bits, false, s) != cudaSuccess) return FBQ_ERR_CUDA;
     if (launch_interleave(gate_scales, up_scales, scales, F, sc, false, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    if (launch_interleave(gate_zeros, up_zeros, zeros, F, sc, false, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    g_launches += 3;
-    if (rank == 0) return FBQ_OK;
-    if (cudaMemcpyAsync(A, gate_A, a_bytes, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    if (cudaMemcpyAsync(static_cast<char *>(A) + a_bytes, up_A, a_bytes, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    if (launch_interleave(gate_B, up_B, B, F, (size_t)rank * 2, true, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    ++g_launches;
+    g_launches += 2;
+    if (rank > 0) {
+        if (launch_interleave(gate_B, up_B, B, F, (size_t)rank * 2, true, s) != cudaSuccess) return FBQ_ERR_CUDA;
+        ++g_launches;
+        if (cudaMemcpyAsync(A, gate_A, a_bytes, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return FBQ_ERR_CUDA;
+        if (cudaMemcpyAsync(static_cast<char *>(A) + a_bytes, up_A, a_bytes, cudaMemcpyDeviceToDevice, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    }
+    // Copies come last: a kernel that starts before the one in front of it is through, and then reads weights, does not start before a copy is.
+    for (int up = 0; up < 2; ++up)
+        if (cudaMemcpy2DAsync(static_cast<char *>(zeros) + up * kGateUp * sc, 2 * kGateUp * sc, up ? up_zeros : gate_zeros, kGateUp * sc, kGateUp * sc, F / kGateUp,
+                              cudaMemcpyDeviceToDevice, s) != cudaSuccess)
+            return FBQ_ERR_CUDA;
     return FBQ_OK;
 }
 

@@ -12,6 +12,7 @@ namespace fbq {
 
 constexpr int kGroupFast = 128;   // group size of the decode / prefill kernels (Section 5.1)
 constexpr int kMaxRank = 256;
+constexpr int kMostSide = 1 << 30;               // rows or columns of a layer, for calls that count whole tiles of them in 31 bits
 constexpr int kDecodeMaxM = 16, kDecodePreferM = 6;
 
 // Activation-type helpers ---------------------------------------------------

@@ -358,7 +358,7 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
     }
     // The first pass over codes and x would otherwise meet HBM's latency at every block: with all stages in flight that is
     // 0.43 us per block of K against 0.27 of MMAs.  (Where they are larger, a small part of the time is spent on first passes.)
-    if (GRAD ? warp == 3 && p.nft > 0 && p.K == p.K_all : warp == 3) {
+    if (warp == 3 && (!GRAD || p.K == p.K_all)) {
         const size_t cells = (size_t)p.N * p.K, groups = (size_t)p.N * (p.K / kGroupFast) * 2, x_bytes = (size_t)p.M * (GRAD ? p.N : p.K) * 2;
         if (cells <= (size_t)64 << 20) {
             prefetch_share(p.scales, groups);
@@ -760,9 +760,9 @@ int launch_columns(int N, int K)
     return (int)std::min((size_t)K, ((K + n - 1) / n + kFeat - 1) / kFeat * kFeat);
 }
 
-// Columns [k_first, k_first + cols) of dx; `first`: and t.
+// Columns [k_first, k_first + cols) of dx, and where s and t are not there yet (a launch of all columns) those.
 template <int BITS, typename T>
-cudaError_t run_grad(const GradArgs &a, int k_first, int cols, bool first, Workspace &ws, const PrefillTuning &tune, cudaStream_t s)
+cudaError_t run_grad(const GradArgs &a, int k_first, int cols, Workspace &ws, const PrefillTuning &tune, cudaStream_t s)
 {
     DenseParams p{};
     p.x = a.dy; p.qw = a.qw; p.scales = a.scales; p.zeros = a.zeros;
@@ -775,14 +775,13 @@ cudaError_t run_grad(const GradArgs &a, int k_first, int cols, bool first, Works
     p.rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.rank = a.rank;
     p.a_rows = std::min(128, p.rank_pad);
-    p.nft = a.dx ? (cols + kFeat - 1) / kFeat : 0;
+    p.nft = (cols + kFeat - 1) / kFeat;
     p.tok = token_tile(a.M, p.nft, (a.N + kBK - 1) / kBK);
     p.ntt = (a.M + p.tok - 1) / p.tok;
     p.n_t = a.rank > 0 && !a.made ? (a.M + kTTok - 1) / kTTok : 0;
-    p.n_t2 = a.rank > 0 && a.t16 && first ? p.n_t : 0;
+    p.n_t2 = a.t16 ? p.n_t : 0;
     p.nkc = (a.N + kItemK - 1) / kItemK;
-    // (where there are fewer tiles than pairs the others dequantise)
-    const int n_pairs = p.nft > 0 ? pairs_of_device() : std::max(1, std::min(pairs_of_device(), p.n_t + p.n_t2));
+    const int n_pairs = pairs_of_device();                       // (where there are fewer tiles than pairs the others dequantise)
     p.wave_ft = std::max(1, std::min(p.nft, (n_pairs + p.ntt - 1) / p.ntt));
     p.wait_looks = tune.flag_polls > 0 ? (uint32_t)tune.flag_polls : 0u;
     p.test_skip_flag = tune.test_skip_flag;
@@ -790,20 +789,18 @@ cudaError_t run_grad(const GradArgs &a, int k_first, int cols, bool first, Works
     cudaError_t e;
     if ((e = encode_map(&maps[0], matrix_map(a.dy, dt, 2, a.N, a.M, kBK, p.tok / 2, sw))) != cudaSuccess) return e;
     for (int i = 1; i < 9; ++i) maps[i] = maps[0];
-    if (a.dx) {
-        MapSpec out = matrix_map(static_cast<uint16_t *>(a.dx) + k_first, dt, 2, cols, a.M, 128, 16, CU_TENSOR_MAP_SWIZZLE_NONE);
-        out.strides[0] = (cuuint64_t)a.K * 2;
-        if ((e = encode_map(&maps[6], out)) != cudaSuccess) return e;
-        if ((e = cached_map(&maps[2], matrix_map(ws.w16, dt, 2, cols, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
-    }
+    MapSpec out = matrix_map(static_cast<uint16_t *>(a.dx) + k_first, dt, 2, cols, a.M, 128, 16, CU_TENSOR_MAP_SWIZZLE_NONE);
+    out.strides[0] = (cuuint64_t)a.K * 2;
+    if ((e = encode_map(&maps[6], out)) != cudaSuccess) return e;
+    if ((e = cached_map(&maps[2], matrix_map(ws.w16, dt, 2, cols, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
     if (a.rank > 0) {
         if ((e = encode_map(&maps[1], matrix_map(a.dy, dt, 2, a.N, a.M, kBK, kTTok / 2, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&maps[4], matrix_map(a.B, dt, 2, a.rank, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&maps[4], matrix_map(a.B, dt, 2, a.rank, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
         if ((e = encode_map(&maps[5], matrix_map(a.s16, dt, 2, p.rank_pad, a.M, kBK, p.tok / 2, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&maps[7], matrix_map(a.A, dt, 2, a.K, a.rank, kBK, kBK, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&maps[7], matrix_map(a.A, dt, 2, a.K, a.rank, kBK, kBK, sw))) != cudaSuccess) return e;
     }
     if (p.n_t2 > 0) {
-        if ((e = cached_map(&maps[3], matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&maps[3], matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
         if ((e = encode_map(&maps[8], matrix_map(a.x, dt, 2, a.K, a.M, kBK, kTTok / 2, sw))) != cudaSuccess) return e;
     }
     return start<BITS, T, kGrad>(maps, p, n_pairs, tune.pdl != 0, s);
@@ -875,24 +872,24 @@ bool grad_thin_first(const GradArgs &a)
 
 bool grad_supported(int M, int N, int K, int group, int rank)
 {
-    return group == kGroupFast && K % kGroupFast == 0 && N % 8 == 0 && rank % 8 == 0 && rank <= kMaxRank && M <= (1 << 22) && launch_columns(N, K) > 0;
+    return group == kGroupFast && K % kGroupFast == 0 && N % 8 == 0 && rank % 8 == 0 && rank <= kMaxRank && M <= (1 << 22) && K <= kMostSide && launch_columns(N, K) > 0;
 }
 
 void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags)
 {
     const size_t cols = launch_columns(a.N, a.K), nft = (cols + kFeat - 1) / kFeat, nkc = (a.N + kItemK - 1) / kItemK;
-    *w16_bytes = a.dx ? (size_t)a.N * cols * 2 : 16;
+    *w16_bytes = (size_t)a.N * cols * 2;
     *tags = kTagFirst + nft * nkc * kUnits + 2 * ((size_t)(a.M + kTTok - 1) / kTTok) + 32;
 }
 
 cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches)
 {
-    const int cols = a.dx ? launch_columns(a.N, a.K) : a.K;
+    const int cols = launch_columns(a.N, a.K);
     cudaError_t e = cudaSuccess;
-    for (int k = 0; k < a.K && e == cudaSuccess; k += cols) {             // (each makes s anew: rank of `cols` of its operations)
+    for (int k = 0; k < a.K && e == cudaSuccess; k += cols) {
         const int n = std::min(cols, a.K - k);
-        e = a.bits == 4 ? (a.bf16 ? run_grad<4, __nv_bfloat16>(a, k, n, k == 0, ws, tune, s) : run_grad<4, __half>(a, k, n, k == 0, ws, tune, s))
-                        : (a.bf16 ? run_grad<3, __nv_bfloat16>(a, k, n, k == 0, ws, tune, s) : run_grad<3, __half>(a, k, n, k == 0, ws, tune, s));
+        e = a.bits == 4 ? (a.bf16 ? run_grad<4, __nv_bfloat16>(a, k, n, ws, tune, s) : run_grad<4, __half>(a, k, n, ws, tune, s))
+                        : (a.bf16 ? run_grad<3, __nv_bfloat16>(a, k, n, ws, tune, s) : run_grad<3, __half>(a, k, n, ws, tune, s));
         if (e == cudaSuccess) ++*launches;
     }
     return e;

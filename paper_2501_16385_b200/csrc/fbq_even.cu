@@ -711,7 +711,7 @@ cudaError_t launch_even(const EvenArgs &a, int *status, bool pdl, cudaStream_t s
     maps[1] = maps[2] = maps[0];
     if (a.rank > 0) {
         if ((e = encode_map(&maps[1], matrix_map(a.thin, dt, 2, rank_pad, a.M, kBK, box, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&maps[2], grad ? matrix_map(a.factor, dt, 2, a.K, a.rank, kBK, kBK, sw) : matrix_map(a.factor, dt, 2, a.rank, a.N, kBK, kFeat, sw))) !=
+        if ((e = encode_map(&maps[2], grad ? matrix_map(a.factor, dt, 2, a.K, a.rank, kBK, kBK, sw) : matrix_map(a.factor, dt, 2, a.rank, a.N, kBK, kFeat, sw))) !=
             cudaSuccess)
             return e;
     }

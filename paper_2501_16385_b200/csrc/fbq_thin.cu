@@ -275,11 +275,11 @@ template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, 
     cudaError_t e;
     if (a.t) {
         if ((e = encode_map(&xmap, matrix_map(a.x, dt, 2, a.K, a.M, kBK, p.tok, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&amap, matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&amap, matrix_map(a.A, dt, 2, a.K, a.rank, kBK, p.a_rows, sw))) != cudaSuccess) return e;
     }
     if (a.s) {
         if ((e = encode_map(&dymap, matrix_map(a.dy, dt, 2, a.N, a.M, kBK, p.tok, sw))) != cudaSuccess) return e;
-        if ((e = cached_map(&bmap, matrix_map(a.B, dt, 2, a.rank, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
+        if ((e = encode_map(&bmap, matrix_map(a.B, dt, 2, a.rank, a.N, kBK, kBK, sw))) != cudaSuccess) return e;
     }
     if (!a.t) { xmap = dymap; amap = bmap; }
     if (!a.s) { dymap = xmap; bmap = amap; }

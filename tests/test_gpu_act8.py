@@ -80,6 +80,19 @@ def test_more_than_31_bits_of_elements():
     assert bool((back[M // 2] == 1).all())
 
 
+def test_more_than_31_bits_of_single_elements():
+    M, K = 70001, 30701                                         # 2.149e9, rows of no whole pieces
+    codes = torch.zeros((M, K), dtype=torch.int8, device="cuda")
+    scales = torch.ones((M, 240), dtype=torch.float32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(6)
+    codes[-2:] = torch.randint(-127, 128, (2, K), generator=g, device="cuda").to(torch.int8)
+    back = fbq.act8_unpack(codes, scales, torch.bfloat16)
+    assert torch.equal(back[-2:], codes[-2:].to(torch.bfloat16)) and not bool(back[M // 2].any())
+    again, _ = fbq.act8_pack(back)
+    want, _ = to_8_bits(back[-2:])
+    assert torch.equal(again[-2:], want)
+
+
 def test_no_rows_and_views():
     codes, scales = fbq.act8_pack(torch.empty((0, 40), dtype=torch.float16, device="cuda"))
     assert codes.shape == (0, 40) and scales.shape == (0, 1) and fbq.act8_unpack(codes, scales, torch.float16).shape == (0, 40)

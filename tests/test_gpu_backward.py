@@ -88,12 +88,37 @@ def test_many_tiles(M, N, K, bits, rank, dtype):
     check_gradients(got, layer_gradients(layer, dy.double(), zero.expand(M, N), x.double(), zero.expand(M, K), None), rank)
 
 
-def test_weights_in_several_launches():
-    """A layer whose 16-bit copy of the weights is beyond one launch's scratch: columns in parts."""
-    M, N, K, bits, rank, dt = 40, 131072, 2304, 4, 16, torch.bfloat16
+@pytest.mark.parametrize("M,rank", [(40, 16), (800, 16), (800, 0)])
+def test_weights_in_several_launches(M, rank):
+    """A layer whose 16-bit copy of the weights is beyond one launch's scratch: columns in parts (few tokens need no copy)."""
+    N, K, bits, dt = 131072, 2304, 4, torch.bfloat16
     layer = Layer(fbq, N, K, bits, rank, dt, seed=1)
     dy, x = normal(M, N, dt, seed=2, scale=0.1), normal(M, K, dt, seed=3)
     got = fbq.linear_backward(dy, x, *layer.tensors, 128, bits)
+    zero = torch.zeros((1, 1), dtype=torch.float64, device="cuda")
+    check_gradients(got, layer_gradients(layer, dy.double(), zero.expand(M, N), x.double(), zero.expand(M, K), None), rank)
+
+
+@pytest.mark.parametrize("M", [16, 33, 95, 112, 160, 176, 192, 193, 385, 768, 769])
+@pytest.mark.parametrize("rank", [64, 128, 192, 256])
+def test_tiles_of_tokens_and_blocks_of_the_rank(M, rank):
+    """Every depth of the rings, odd and even numbers of the sub-branch's blocks, both sides of the sizes at which kernels change."""
+    N, K, bits, dt = 1160, 640, 3 if rank > 128 else 4, torch.float16
+    layer = Layer(fbq, N, K, bits, rank, dt, seed=M)
+    dy, x = normal(M, N, dt, seed=2, scale=0.1), normal(M, K, dt, seed=3)
+    got = fbq.linear_backward(dy, x, *layer.tensors, 128, bits)
+    assert fbq.poll_status() == 0
+    zero = torch.zeros((1, 1), dtype=torch.float64, device="cuda")
+    check_gradients(got, layer_gradients(layer, dy.double(), zero.expand(M, N), x.double(), zero.expand(M, K), None), rank)
+
+
+@pytest.mark.parametrize("M,N,K,rank", [(333, 20488, 256, 72), (60, 1032, 16640, 200), (1100, 12296, 384, 136)])
+def test_long_contractions_of_the_thin_products(M, N, K, rank):
+    """s and t whose contraction several clusters share."""
+    dt = torch.bfloat16
+    layer = Layer(fbq, N, K, 4, rank, dt, seed=M)
+    dy, x = normal(M, N, dt, seed=2, scale=0.1), normal(M, K, dt, seed=3)
+    got = fbq.linear_backward(dy, x, *layer.tensors, 128, 4)
     zero = torch.zeros((1, 1), dtype=torch.float64, device="cuda")
     check_gradients(got, layer_gradients(layer, dy.double(), zero.expand(M, N), x.double(), zero.expand(M, K), None), rank)
 
