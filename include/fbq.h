@@ -276,19 +276,25 @@ int fbq_linear_batch_hostio(const fbq_problem *problems, int count, int M, int g
  *     h[m][8 i + j] = f(p[m][16 i + j]) * p[m][16 i + 8 + j],      j = 0 .. 7,   f = SiLU or GELU (fbq_gate)
  * fbq_gated_layer lays two projections of [F][K] and one rank (of each branch) out so: a step at load time.  It is an ordinary layer to
  * fbq_linear, fbq_dequant and fbq_linear_backward as well.  qweight, scales, zeros: [2F] rows; A [2 rank][K]; B [2F][2 rank].
- * Domain of the gated calls: group 128, N and (the layer's) rank multiples of 16, rank <= 256; anything else FBQ_ERR_UNSUPPORTED.
+ * Domain of the gated calls: group 128, N and (the layer's) rank multiples of 16, rank <= 256, N and K up to 2^30, M up to 2^22; anything
+ * else FBQ_ERR_UNSUPPORTED.
  * Every pointer is 16-byte aligned. */
 int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void *gate_zeros, const void *gate_A, const void *gate_B,
                     const uint32_t *up_q, const void *up_scales, const void *up_zeros, const void *up_A, const void *up_B, uint32_t *qweight,
                     void *scales, void *zeros, void *A, void *B, int F, int K, int group, int bits, int rank, void *stream);
 
-/* h [M][N/2] of a gated layer, in one launch: p is gated in single precision where its sums are and rounded to the activation
- * type never (h is, once).  x, A, B, h: fp16 or bf16 (act_is_bf16).  At most 2 tokens run on the streaming kernel, 3 to 16 on the split
- * kernel (layer rank up to 128, and where fbq_split_plan has a plan for N rows), the rest on the prompts' kernels; each computes p as it
- * does for fbq_linear.  "gemv" = 0 and "force_kernel" >= 0 leave all of it to the prompts' kernels.
+/* h [M][N/2] of a gated layer: p is gated in single precision where its sums are and rounded to the activation type never (h is,
+ * once).  x, A, B, h: fp16 or bf16 (act_is_bf16).  At most 2 tokens run on the streaming kernel, 3 to 16 on the split kernel (layer rank up
+ * to 128, and where fbq_split_plan has a plan for N rows), each in one launch; each computes p as it does for fbq_linear.  More tokens
+ * run on the prompts' kernels, or up to 640 of a layer that makes more than 148 of their tiles on a kernel that shares the products out
+ * evenly (four launches at most; t and the dequantised weights are rounded once to the activation type, as in the prompts' kernels).
+ * "gemv" = 0 and "force_kernel" >= 0 leave the fewest tokens to the others too.
  *   kept, kept_scales   NULL, or what the backward pass needs of p in 8 bits: codes [M][N] and one scale per 128 columns of a row,
- *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M run on the prompts' dense kernel
- *       (scratch: a 16-bit copy of the weights, up to 512 MB per stream). */
+ *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M up to 640 run on the kernel that
+ *       shares products out, of more on the prompts' dense kernel (scratch: a 16-bit copy of the weights, up to 512 MB per stream, which they
+ *       cannot do without).
+ * Scratch of the sharing kernel: its sums (up to 29 MB), M x rank values of 16 bits, and partial sums of those; it grows as described at
+ * fbq_linear, and a call that would grow it during a capture returns FBQ_ERR_UNSUPPORTED and queues nothing. */
 int fbq_gated(const void *x, const uint32_t *qweight, const void *scales, const void *zeros, const void *A, const void *B, void *h,
               int8_t *kept, float *kept_scales, int M, int N, int K, int group, int bits, int rank, int gate, int act_is_bf16, void *stream);
 
@@ -304,10 +310,10 @@ int fbq_act8_unpack(const int8_t *codes, const float *scales, void *x, int M, in
  * dy [M][N], x and dx [M][K], dA [rank][K], dB [N][rank], all in the activation type (act_is_bf16).  x is given so or, with x == NULL, as
  * x8 [M][K] with x8_scales (fbq_act8_pack).  dx may be NULL, and dA and dB may both be (x then as well); rank == 0 has neither.
  * M == 0: dA and dB are set to zero.  Sums are fp32; s, t and the dequantised weights are rounded once to the activation type where they
- * become operands.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, rank <= 256; else
+ * become operands.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, N <= 2^21, rank <= 256; else
  * FBQ_ERR_UNSUPPORTED.  Every pointer is 16-byte aligned; outputs overlap no input and not each other.
- * Scratch per stream: a 16-bit copy of the weights (up to 512 MB), M x (2 rank, rounded up to 64) and, for x8, M x K values of 16 bits, and
- * partial sums of dA and dB; it grows as described at fbq_linear, and a call that would grow it during a capture returns
+ * Scratch per stream: above 768 tokens a 16-bit copy of the weights (up to 512 MB), up to there the sums that
+ * CTAs share (up to 29 MB); M x (2 rank, rounded up to 64) and, for x8, M x K values of 16 bits, and partial sums of s, t, dA and dB; it grows as described at fbq_linear, and a call that would grow it during a capture returns
  * FBQ_ERR_UNSUPPORTED and queues nothing.  Graphs captured on one stream share its scratch: replay them one after another. */
 int fbq_linear_backward(const void *dy, const void *x, const int8_t *x8, const float *x8_scales, const uint32_t *qweight,
                         const void *scales, const void *zeros, const void *A, const void *B, void *dx, void *dA, void *dB, int M, int N, int K,
@@ -387,7 +393,8 @@ int fbq_split_plan(int M, int N, int K, int group, int bits, int rank, int act_i
  *                   fbq_reconstruct_step is held to (a slab of 256 rows and what the rank needs come on top)
  *   "pdl"           1 = launch with programmatic dependent launch (default), 0 = plain.  With 1 a decode,
  *                   prefill or reconstruction kernel may start while the kernel before it on the stream still runs: it sets
- *                   itself up, and the decode kernels already fetch qweight, scales, zeros, A and B, before
+ *                   itself up, and the decode kernels already fetch qweight, scales, zeros, A and B (the kernel of
+ *                   gated layers and backward passes of few hundred tokens qweight, scales and zeros), before
  *                   they wait for that kernel; x, y and the scratch are touched only after the wait.  So
  *                   the weight operands must not be written by the launch directly before (x may be)
  *   "decode_t_late" test switch: 1 = contribute to t after the main loop, which drives

@@ -611,10 +611,19 @@ constexpr uint32_t kTNone = 0x80000000u;                     // -0.0: what a slo
 __device__ __forceinline__ uint32_t t_enc(float v) { const uint32_t w = __float_as_uint(v); return w ? w : kTNone; }
 __device__ __forceinline__ uint32_t t_min(uint32_t m, const uint4 &w) { return __vimin3_u32(m, __vimin3_u32(w.x, w.y, w.z), w.w); }
 
+// The largest |v| of what is finite (NaN where nothing is): an infinite t is its token's alone, and must not set the scale of the
+// other token's.  v * 0 + |v| is |v|, or NaN, which a maximum passes over (a second look where the
+// largest is infinite took 0.13 us of every launch).
+__device__ __forceinline__ float finite_size(float v) { return fmaf(v, 0.f, fabsf(v)); }
+__device__ __forceinline__ float largest_finite(float4 v)
+{
+    return fmaxf(fmaxf(finite_size(v.x), finite_size(v.y)), fmaxf(finite_size(v.z), finite_size(v.w)));
+}
+
 // One look at exactly eight t slots with at most 128 entries: straight-line code, a lane takes four consecutive
 // entries and has its eight 16-byte loads in flight at once (the common shapes: the looks are what a main CTA's
 // epilogue waits with, and a lean look is a fast look).  Adds the slots in slot order into s_t, returns whether
-// every entry was there; amax = largest |sum|.
+// every entry was there; amax = largest finite |sum|.
 __device__ __forceinline__ bool look8(const uint32_t *slots, size_t slot_elems, int nent, int lane, float *s_t, float &amax)
 {
     const int nq = nent >> 2, q = min(lane, nq - 1);          // lanes past the last four entries repeat them (and do not store)
@@ -632,7 +641,7 @@ __device__ __forceinline__ bool look8(const uint32_t *slots, size_t slot_elems, 
         v.w += __uint_as_float(pv[u].w);
     }
     if (lane < nq) *reinterpret_cast<float4 *>(s_t + 4 * lane) = v;
-    amax = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
+    amax = fmaxf(largest_finite(v), 0.f);
     return mn != 0u;
 }
 
@@ -660,7 +669,7 @@ __device__ __forceinline__ bool look_slots(const uint32_t *tpart, size_t slot_el
             }
         }
         *reinterpret_cast<float4 *>(s_t + 4 * q) = v;
-        amax = fmaxf(amax, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+        amax = fmaxf(amax, largest_finite(v));
     }
     return mn != 0u;
 }
@@ -732,16 +741,8 @@ __device__ __forceinline__ bool epilogue(const GemvParams &p, uint8_t *smem, con
         // Tell that this CTA has read t (nobody waits for the add; a t CTA clears up once all have told).
         if (lane == 0) atomicAdd(p.ctr + 1, 1);
         // the largest |sum| of the warp: non-negative floats order like their bit patterns, so one integer reduction does
-        uint32_t amax_bits = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));
+        const uint32_t amax_bits = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));
         __syncwarp();
-        if (amax_bits > 0x7F7FFFFFu) {                           // an infinite t is its token's alone: the other's scale is that of what is finite
-            amax_bits = 0u;
-            for (int i = lane; i < M * rank; i += 32) {
-                const uint32_t v = __float_as_uint(s_t[i]) & 0x7FFFFFFFu;
-                if (v <= 0x7F7FFFFFu) amax_bits = max(amax_bits, v);
-            }
-            amax_bits = __reduce_max_sync(0xffffffffu, amax_bits);
-        }
         // a power of two that puts the largest |t| near 2^14 keeps both terms inside fp16
         const uint32_t ex = min(max(amax_bits >> 23, 1u), 254u);
         const uint32_t sb = min(max(268u - ex, 1u), 254u);

@@ -46,6 +46,7 @@ def test_gated_domain():
     for call in (gated, gated_backward):
         assert call(N=24) == UNSUPPORTED and call(N=31) == BADARG and call(rank=8) == UNSUPPORTED and call(rank=9) == BADARG
         assert call(gate=2) == BADARG and call(gate=-1) == BADARG
+    assert gated(N=(1 << 30) + 16) == UNSUPPORTED and gated(K=(1 << 30) + 128) == UNSUPPORTED
     assert linear_backward(N=12) == UNSUPPORTED and linear_backward(rank=4) == UNSUPPORTED
     assert linear_backward(N=1 << 22, K=128) == UNSUPPORTED                    # not even 256 columns of a 16-bit copy fit the scratch
 
