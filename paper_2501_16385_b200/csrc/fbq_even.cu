@@ -6,13 +6,12 @@
 //
 // Up to a few hundred tokens a weight is used too seldom to be dequantised in a pass of its own (the dense kernel's 16-bit copy costs 4
 // bytes a weight through L2 beside the half byte of its code), and tiles are fewer than SMs or fill a second wave badly.  So a CTA turns
-// codes into the operand in shared memory, 128 features for up to 192 tokens, and the pairs of blocks of all tiles, in order, are cut into equal
+// codes into the operand on chip, 128 features for up to 192 tokens, and the pairs of blocks of all tiles, in order, are cut into equal
 // ranges, one per CTA:
 //
 //   warp 2       copies the packed codes of a pair of blocks, 128 rows x one quantisation group, warp 3 their scales and zero points
-//   warps 8-23   four groups of four dequantise a pair in turn, a row's 128 codes a thread, into two stages of the operands (of some 2500 cycles that
-//                a group then takes, half go into waits, fences and loops; two groups of eight with 64 codes a thread: 34 us for 77 tokens, 27 so)
-//   warp 0       copies the tokens by TMA, and both operands of the sub-branch's blocks
+//   warps 8-23   two groups of eight dequantise a pair in turn, half a row a thread, and copy the tokens' block by TMA as soon as its stage
+//                is free, and both operands of the sub-branch's blocks
 //   warp 1       issues tcgen05.mma 128 features x tokens x 16
 //   warps 4-7    epilogue: a tile that is the range's own is written; of one that several ranges share each stores its fp32 sums
 //
@@ -21,12 +20,17 @@
 // where nine share a tile: one SM reads what nine have written.)  The sub-branch's blocks are done where the tile's first ones are.
 // All waits are bounded.
 //
-// Forward, features are rows of W and the operand is K-major: a pair of blocks is one group of each row.  Grad, features are its columns,
-// 128 of them one group; a pair of blocks is 128 rows of it, and the operand is MN-major: rows are written as they lie.
+// Forward, features are rows of W: a pair of blocks is one group of each row, and a thread's weights are a row of the operand, which goes to tensor
+// memory as it is (128 lanes x 32 columns a block; the multiplication reads it there and not from shared memory).  Grad, features are W's
+// columns, 128 of them one group; a pair of blocks is 128 rows of it, and the operand is MN-major in shared memory: rows are written as they lie.
 //
-// What a pair of blocks passes through (codes, operand, MMAs, free again) takes some 2500 cycles and the warps are through with one in 600, so
-// what counts is how many are on their way.  256 features a CTA, which reads x half as often, leaves room for one and a half pairs: 77 tokens of
-// 4096 -> 2 x 11008 38 us.  Pairs of CTAs with cta_group::2 were slower still (the dequantising warps' fence towards the asynchronous proxy).
+// What bounds it: the chain of a pair, stage free -> operand written -> MMAs issued and done -> free, with the three pairs that fit on their way,
+// some 1000 cycles a pair at 77 tokens (INT3) and 1190 at 333 (Grad, tiles of 176), where the MMAs alone would take 320 and 700.  4096 -> 2 x 11008
+// at 77 tokens takes 30 us of a call's 40, 22016 -> 4096 (dx) at 333 tokens 66 of 100.  Of single things left out (for timing) none gives more than a
+// tenth: dequantisation 8 %, three of four MMAs 9, x 1 (Grad 9), codes 1.  Earlier forms, us of the two calls: a warp that copies all of x, whose 40
+// instructions a block each wait their turn among 24 warps, 42.9 and 105; four groups of four warps, 128 codes a thread, 41.5 and 98; operands in shared
+// memory forward too, 41 and -; one block per look of the MMA warp, 43.5 and 98; 256 features a CTA, one and a half pairs on their way, 38 for the kernel
+// alone; pairs of CTAs with cta_group::2, slower still (the dequantising warps' fence towards the asynchronous proxy).
 #include <algorithm>
 #include <type_traits>
 
@@ -43,11 +47,12 @@ using namespace ptx;
 constexpr int kBK = 64, kFeat = 128;
 constexpr uint32_t kWBytes = kFeat * kBK * 2u, kBox = kWBytes / 2;
 constexpr int kMostTok = 192, kMostStages = 8;
-constexpr int kDqWarp = 8, kGroups = 4, kGroupWarps = 4, kThreads = (kDqWarp + kGroups * kGroupWarps) * 32;
+constexpr int kDqWarp = 8, kGroups = 2, kGroupWarps = 8, kMakers = kGroupWarps / 2, kThreads = (kDqWarp + kGroups * kGroupWarps) * 32;
 constexpr int kRing = 4;                         // pairs of blocks whose codes and scales are there or on their way
 constexpr uint32_t kCodeBytes = 128u * 64u, kSlotBytes = kCodeBytes + 512u;      // codes (INT3: 48 of 64 bytes a row), scales and zero points
 static_assert(kMostStages <= 8, "");
-constexpr int kGo = 8;                           // pairs whose stages can be free and not yet written: less than half of these (see `dequantise`)
+constexpr int kFree = 32;                        // blocks whose stages' being free is told apart: more than the groups' pairs and their sub-branch's blocks (see `dequantise`)
+static_assert(kGroups * (2 + kMaxRank / kBK) <= kFree, "");
 constexpr int kScaleAhead = 3;                   // pairs whose scales a loading warp has requested
 constexpr uint32_t kYBytes = 32u * 128u * 2u;    // staged part of an output tile: 32 tokens
 constexpr uint32_t kFixed = kRing * kSlotBytes + 2 * kYBytes + 512 + 512;     // ring, staging, largest |p|, barriers
@@ -64,6 +69,7 @@ struct EvenParams {
     int M, F, D, K;           // tokens, features, contraction, columns of W
     int tok, ntt, nkp, slab;  // tokens of a tile, token tiles, pairs of blocks of the contraction, blocks of the sub-branch
     int stages, gate, kept_pitch;
+    uint32_t acc;             // columns of an accumulator; forward the weights' operands are behind two of them
     long long pairs;          // of all tiles
     void *y;                  // of the adding launch: h or dx, codes
     int8_t *kept;
@@ -240,86 +246,122 @@ __device__ __forceinline__ bool load_scales(const EvenParams &p, int range, uint
     }
 }
 
+// Warps 8-23.  A pair is one group's, half a row a thread; the first of a block's makers copies x of it.  The sub-branch's blocks are
+// copied by the group whose turn comes next.
 template <int BITS, typename T, int MODE>
-__device__ __forceinline__ bool dequantise(const EvenParams &p, int range, uint32_t sbase, uint32_t stage_bytes, uint32_t ring, uint32_t full0, uint32_t go0,
-                                           uint32_t rfull0, uint32_t rempty0, volatile int *quit)
+__device__ __forceinline__ bool dequantise(const EvenParams &p, int range, const CUtensorMap *xmap, const CUtensorMap *tmap, const CUtensorMap *bmap, uint32_t tmem,
+                                           uint32_t sbase, uint32_t stage_bytes, uint32_t ring, uint32_t full0, uint32_t free0, uint32_t rfull0, uint32_t rempty0,
+                                           volatile int *quit)
 {
     constexpr bool GRAD = MODE == kGrad;
     constexpr int NW = BITS == 4 ? 4 : 3;
     const int warp = (threadIdx.x >> 5) - kDqWarp, group = warp / kGroupWarps, w = warp % kGroupWarps, lane = threadIdx.x & 31;
-    // A thread's row of the pair.  Forward the pair's blocks are the row's halves; Grad the row's half chooses the block and the codes' halves are the
-    // operand's boxes.  Eight neighbouring lanes store to eight rows: different banks in the 128-byte swizzle, as they load them from different
-    // banks (INT4: the 64-byte swizzle of the copy).
-    const int row = 32 * w + lane;
-    const uint32_t r = GRAD ? row & 63 : row;
-    const uint32_t dst = sbase + r * 128u + ((r & 7u) << 4);                 // unit j: ^ (j << 4)
-    const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + ((((uint32_t)row >> 1) & 3u) << 4) : (uint32_t)row * 48u;
+    // A thread's half a row of the pair.  Forward the pair's blocks are the row's halves; Grad the row's half chooses the block and the codes' halves
+    // are the operand's boxes.  Eight neighbouring lanes store to eight rows: different banks in the 128-byte swizzle, as they load them from
+    // different banks (INT4: the 64-byte swizzle of the copy).
+    const int q = w & 3, row = 32 * q + lane;
+    const uint32_t half = (uint32_t)w >> 2, block = GRAD ? (uint32_t)q >> 1 : half;
+    const bool copies = w == (GRAD ? 2 * (int)block : 4 * (int)block);
+    const uint32_t r = row & 63;
+    const uint32_t dst = sbase + half * kBox + r * 128u + ((r & 7u) << 4);   // Grad: unit j: ^ (j << 4)
+    const uint32_t wcols = tmem + ((uint32_t)(32 * q) << 16) + 2u * p.acc;             // forward: of this warp's rows
+    const uint32_t src = BITS == 4 ? (uint32_t)row * 64u + (((((uint32_t)row >> 1) & 3u) ^ (2u * half)) << 4) : (uint32_t)row * 48u + half * 24u;
     Pieces pc(p, range);
     uint32_t s = 0;                                              // stage of the next block
-    uint32_t q = 0;                                              // pairs so far
+    uint32_t u = 0;                                              // blocks so far
     uint32_t slot = 0, rphase = 0;                               // of the ring
     int turn = 0;                                                // whose pair it is
-    const uint32_t stages = (uint32_t)p.stages;
-    auto announce = [&](uint32_t stage) {
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(full0 + 8u * stage);
+    bool before = true;                                          // nothing of what the launch before wrote has been read
+    const uint32_t stages = (uint32_t)p.stages, xbytes = (uint32_t)p.tok * (kBK * 2u);
+    // A block's stage is free.  There is a barrier for each of kFree blocks in a row, not for each stage: a wait knows a phase only from its
+    // neighbours, and a group looks at every other pair.  When it waits for block b it has seen b - kFree or a later one become free, and
+    // b + kFree does not before b is written.
+    auto free_stage = [&](uint32_t b) { return __all_sync(0xffffffffu, umma::wait(free0 + 8u * (b % kFree), (b / kFree) & 1u, quit)); };
+    auto after_launch = [&]() {
+        if (before) pdl_wait();
+        before = false;
     };
     while (pc.next()) {
-        const int n = pc.kp1 - pc.kp0;
+        const int n = pc.kp1 - pc.kp0, ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok;
 #pragma unroll 1
         for (int k = 0; k < n; ++k) {
             const uint32_t s1 = s + 1 == stages ? 0u : s + 1;    // the pair's second stage
             if (turn == group) {
                 const uint32_t at = ring + slot * kSlotBytes;
                 if (!__all_sync(0xffffffffu, umma::wait(rfull0 + 8u * slot, rphase, quit))) return false;
-                uint32_t c[4 * NW];
+                uint32_t c[2 * NW];
                 if constexpr (BITS == 4) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         const uint4 a = lds128(at + (src ^ (uint32_t)(i << 4)));
                         c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 3; ++i) {
-                        const uint4 a = lds128(at + src + 16u * i);
-                        c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
-                    }
+                    for (int i = 0; i < 3; ++i)
+                        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(c[2 * i]), "=r"(c[2 * i + 1]) : "r"(at + src + 8u * i) : "memory");
                 }
                 uint32_t sz;
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sz) : "r"(at + kCodeBytes + (uint32_t)row * 4u) : "memory");
                 const float fs = __half2float(__ushort_as_half((unsigned short)(sz & 0xFFFFu))), fz = __half2float(__ushort_as_half((unsigned short)(sz >> 16)));
-                const uint32_t mine = GRAD && row >= 64 ? s1 : s;
-                const uint32_t to0 = dst + mine * stage_bytes, to1 = GRAD ? to0 + kBox : dst + s1 * stage_bytes;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(rempty0 + 8u * slot);                 // (this warp has its codes in registers)
-                // half a row at a time, in registers before its stage is waited for
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    uint32_t d[16], out[32];
-                    Dequant<BITS, T>::run(c + 2 * NW * i, fs, fz, d);
-                    natural_pairs<BITS>(d, out);
-                    Dequant<BITS, T>::run(c + 2 * NW * i + NW, fs, fz, d);
-                    natural_pairs<BITS>(d, out + 16);
-                    // The pair's stages are free: the copying warp, which waits for every block's, tells by a barrier per pair.  (A group that waited for
-                    // a stage's own barrier would have to look at every phase of it: one that passes two between looks it misses, or takes an old one
-                    // for the next.)  Eight of them are told apart although a wait knows a phase only from its neighbours: kMostStages / 2 pairs at most
-                    // are free before this group's is written, and the last eight before it have been.
-                    if (i == 0 && !__all_sync(0xffffffffu, umma::wait(go0 + 8u * (q % kGo), (q / kGo) & 1u, quit))) return false;
-                    const uint32_t to = i ? to1 : to0;
+                // (in registers before the stage is waited for)
+                uint32_t d[16], out[32];
+                Dequant<BITS, T>::run(c, fs, fz, d);
+                natural_pairs<BITS>(d, out);
+                Dequant<BITS, T>::run(c + NW, fs, fz, d);
+                natural_pairs<BITS>(d, out + 16);
+                const uint32_t stage = block ? s1 : s;
+                if (!free_stage(u + block)) return false;
+                if (copies) {
+                    after_launch();
+                    if (umma::elect_one()) tma_load_2d(sbase + kWBytes + stage * stage_bytes, xmap, (2 * (pc.kp0 + k) + (int)block) * kBK, m0, full0 + 8u * stage);
+                    __syncwarp();
+                }
+                if constexpr (GRAD) {
+                    const uint32_t to = dst + stage * stage_bytes;
 #pragma unroll
                     for (uint32_t j = 0; j < 8; ++j) sts128(to ^ (j << 4), out + 4 * j);
-                    if (i == 0 && !GRAD) announce(s);
+                    fence_proxy_async();
+                } else {
+                    umma::fence_after();
+                    umma::st32(wcols + 32u * stage, out);
+                    umma::wait_st();
+                    umma::fence_before();
                 }
-                announce(GRAD ? mine : s1);
+                __syncwarp();
+                // (x's bytes may arrive before they are announced: a block is whole when its makers have arrived, too)
+                if (lane == 0) {
+                    if (copies) mbar_expect_tx(full0 + 8u * stage, xbytes);
+                    else mbar_arrive(full0 + 8u * stage);
+                }
             }
-            ++q;
+            u += 2;
             s = s1 + 1 == stages ? 0u : s1 + 1;
             if (++turn == kGroups) turn = 0;
             if (++slot == kRing) { slot = 0; rphase ^= 1u; }
         }
-        if (pc.owner()) s = (s + (uint32_t)p.slab) % stages;     // the sub-branch's stages are made by copies
+        for (int j = 0; pc.owner() && j < p.slab; ++j) {         // the sub-branch's blocks, whole copies
+            if (turn == group && w == 0) {
+                if (!free_stage(u)) return false;
+                after_launch();
+                if (umma::elect_one()) {
+                    const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes;
+                    mbar_expect_tx(bar, xbytes + kWBytes);
+                    for (int m = 1; m < kMakers; ++m) mbar_arrive(bar);              // (for the warps that have nothing to make)
+                    tma_load_2d(wt + kWBytes, tmap, j * kBK, m0, bar);
+                    if (GRAD) {
+                        for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, bmap, ft * kFeat + 64 * h, j * kBK, bar);
+                    } else {
+                        tma_load_2d(wt, bmap, j * kBK, ft * kFeat, bar);
+                    }
+                }
+                __syncwarp();
+            }
+            ++u;
+            if (++s == stages) s = 0;
+        }
     }
     return true;
 }
@@ -333,35 +375,32 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap cmap, const EvenParams p)
 {
     constexpr bool GRAD = MODE == kGrad;
-    constexpr int kMakers = GRAD ? kGroupWarps / 2 : kGroupWarps;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t sbase = smem_u32(smem), stage_bytes = kWBytes + (uint32_t)p.tok * (kBK * 2u), y_off = (uint32_t)p.stages * stage_bytes;
     const uint32_t ring = sbase + y_off + 2 * kYBytes, bars = kRing * kSlotBytes + 512u;
-    const uint32_t full0 = ring + bars, empty0 = full0 + 8u * kMostStages, accf0 = empty0 + 8u * kMostStages, acce0 = accf0 + 16u, rfull0 = acce0 + 16u,
-                   rempty0 = rfull0 + 8u * kRing, go0 = rempty0 + 8u * kRing;
+    const uint32_t full0 = ring + bars, free0 = full0 + 8u * kMostStages, accf0 = free0 + 8u * kFree, acce0 = accf0 + 16u, rfull0 = acce0 + 16u,
+                   rempty0 = rfull0 + 8u * kRing;
     float *amax = reinterpret_cast<float *>(smem + y_off + 2 * kYBytes + kRing * kSlotBytes);
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 16u * kMostStages + 32u + 16u * kRing + 8u * kGo);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + y_off + 2 * kYBytes + bars + 8u * kMostStages + 8u * kFree + 32u + 16u * kRing);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, range = (int)blockIdx.x;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) {
-            mbar_init(full0 + 8u * i, 1 + kMakers);               // the copying lane, and the warps that make a block
-            mbar_init(empty0 + 8u * i, 1);
-        }
+        for (int i = 0; i < p.stages; ++i) mbar_init(full0 + 8u * i, kMakers);          // the warps that make a block
+        for (int i = 0; i < kFree; ++i) mbar_init(free0 + 8u * i, 1);
         for (int i = 0; i < kRing; ++i) {
             mbar_init(rfull0 + 8u * i, 32 + 1);                  // every copying lane's codes, and the scales
             mbar_init(rempty0 + 8u * i, kGroupWarps);
         }
-        for (int i = 0; i < kGo; ++i) mbar_init(go0 + 8u * i, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(accf0 + 8u * i, 1);
             mbar_init(acce0 + 8u * i, 4);
         }
         *quit = 0;
         fence_barrier_init();
+        for (int i = 0; i < p.stages; ++i) mbar_arrive(free0 + 8u * i);
         prefetch_tensormap(&xmap);
         prefetch_tensormap(&ymap);
         if (p.slab) {
@@ -377,80 +416,41 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
 
-    if (warp == 0) {
-        // =================================================== copies
-        if (lane == 0) {
-            pdl_wait();                                          // (codes, scales and zero points are weights: the others do not wait)
-            uint32_t s = 0, phase = 1u, q = 0;
-            bool first = true;
-            const uint32_t xbytes = (uint32_t)p.tok * (kBK * 2u), x0 = sbase + kWBytes;
-            auto free_stage = [&]() { return first || umma::wait(empty0 + 8u * s, phase, quit); };
-            auto next_stage = [&]() {
-                if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; first = false; }
-            };
-#pragma unroll 1
-            for (Pieces pc(p, range); ok && pc.next();) {
-                const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, end = 2 * pc.kp1 * kBK;
-#pragma unroll 1
-                for (int c0 = 2 * pc.kp0 * kBK; c0 < end; c0 += kBK) {
-                    if (!free_stage()) { ok = false; break; }
-                    if (c0 & kBK) {                              // both stages of the pair are free
-                        mbar_arrive(go0 + 8u * (q % kGo));
-                        ++q;
-                    }
-                    mbar_expect_tx(full0 + 8u * s, xbytes);
-                    tma_load_2d(x0 + s * stage_bytes, &xmap, c0, m0, full0 + 8u * s);
-                    next_stage();
-                }
-#pragma unroll 1
-                for (int c0 = 0; ok && pc.owner() && c0 < p.slab * kBK; c0 += kBK) {
-                    if (!free_stage()) { ok = false; break; }
-                    const uint32_t bar = full0 + 8u * s, wt = sbase + s * stage_bytes;
-                    mbar_expect_tx(bar, xbytes + kWBytes);
-                    tma_load_2d(wt + kWBytes, &tmap, c0, m0, bar);
-                    if (GRAD) {
-                        for (int h = 0; h < 2; ++h) tma_load_2d(wt + h * kBox, &bmap, ft * kFeat + 64 * h, c0, bar);
-                    } else {
-                        tma_load_2d(wt, &bmap, c0, ft * kFeat, bar);
-                    }
-                    for (int k = 0; k < kMakers; ++k) mbar_arrive(bar);              // (for the warps that have nothing to make)
-                    next_stage();
-                }
-            }
-        }
-        __syncwarp();
-    } else if (warp == 1) {
+    if (warp == 1) {
         // =================================================== MMAs
         // The whole warp walks the loop and one elected lane issues: the MMAs' operands stay in uniform registers.  Two blocks at a time.
         const uint32_t idesc = umma::idesc_f16(P2<T>::kFmt, kFeat, (uint32_t)p.tok) | (GRAD ? umma::kIdescMnA : 0u);
-        const uint32_t wstep = GRAD ? 2048u >> 4 : 2u;
+        const uint32_t wstep = GRAD ? 2048u >> 4 : 2u, wcols = tmem + 2u * p.acc;
         const uint64_t wd0 = GRAD ? umma::desc_mn128(sbase, kBox) : umma::desc_k128(sbase), xd0 = umma::desc_k128(sbase + kWBytes);
-        uint32_t s = 0, phase = 0, it = 0;
+        uint32_t s = 0, phase = 0, it = 0, next = (uint32_t)p.stages;        // the block that the next one done makes room for
 #pragma unroll 1
         for (Pieces pc(p, range); ok && pc.next(); ++it) {
-            const uint32_t buf = it & 1u, use = it >> 1, d = tmem + buf * 256u;
+            const uint32_t buf = it & 1u, use = it >> 1, d = tmem + buf * p.acc;
             ok = __all_sync(0xffffffffu, use == 0 || umma::wait(acce0 + 8u * buf, (use - 1u) & 1u, quit));
-            const int n = 2 * (pc.kp1 - pc.kp0) + (pc.owner() ? p.slab : 0);
+            const int own = 2 * (pc.kp1 - pc.kp0), n = own + (pc.owner() ? p.slab : 0);
 #pragma unroll 1
             for (int i = 0; i < n && ok; i += 2) {
                 const bool two = i + 1 < n;
                 const uint32_t s0 = s, s1 = s + 1 == (uint32_t)p.stages ? 0u : s + 1, ph0 = phase, ph1 = s1 ? phase : phase ^ 1u;
-                ok = umma::wait(full0 + 8u * s0, ph0, quit);
-                if (two) ok = umma::wait(full0 + 8u * s1, ph1, quit) && ok;
-                ok = __all_sync(0xffffffffu, ok);
+                const uint32_t look = two && (lane & 1) ? s1 : s0;
+                ok = __all_sync(0xffffffffu, umma::wait(full0 + 8u * look, two && (lane & 1) ? ph1 : ph0, quit));
                 umma::fence_after();
                 if (ok && umma::elect_one()) {
-                    auto block = [&](uint32_t stage, bool more) {
+                    auto block = [&](uint32_t stage, uint32_t room, bool more) {
                         const uint64_t wd = wd0 + stage * (stage_bytes >> 4), xd = xd0 + stage * (stage_bytes >> 4);
 #pragma unroll
-                        for (int j = 0; j < kBK / 16; ++j) umma::mma(d, wd + wstep * j, xd + 2 * j, idesc, more || j > 0);
-                        umma::commit(empty0 + 8u * stage);
+                        for (int j = 0; j < kBK / 16; ++j) {
+                            if (!GRAD && i < own) umma::mma_ts(d, wcols + 32u * stage + 8u * j, xd + 2 * j, idesc, more || j > 0);
+                            else umma::mma(d, wd + wstep * j, xd + 2 * j, idesc, more || j > 0);
+                        }
+                        umma::commit(free0 + 8u * (room % kFree));
                     };
-                    block(s0, i > 0);
-                    if (two) block(s1, true);
+                    block(s0, next, i > 0);
+                    if (two) block(s1, next + 1, true);
                     if (i + 2 >= n) umma::commit(accf0 + 8u * buf);
                 }
                 __syncwarp();
+                next += two ? 2 : 1;
                 s = two ? s1 : s0;
                 phase = two ? ph1 : ph0;
                 if (++s == (uint32_t)p.stages) { s = 0; phase ^= 1u; }
@@ -470,7 +470,7 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             umma::fence_after();
             const int ft = pc.tile / p.ntt, m0 = (pc.tile - ft * p.ntt) * p.tok, m_end = min(p.M, m0 + p.tok);
             {
-                const uint32_t lanes = tmem + buf * 256u + ((uint32_t)(32 * wq) << 16);
+                const uint32_t lanes = tmem + buf * p.acc + ((uint32_t)(32 * wq) << 16);
                 const int n = ft * kFeat + 32 * wq + lane;
                 const size_t part_at = (size_t)(2 * range + pc.owner()) * p.tok * kFeat + 32 * wq + lane;
 #pragma unroll 1
@@ -539,10 +539,10 @@ even_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         if (threadIdx.x == 4 * 32) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp >= kDqWarp) {
-        ok = dequantise<BITS, T, MODE>(p, range, sbase, stage_bytes, ring, full0, go0, rfull0, rempty0, quit);
+        ok = dequantise<BITS, T, MODE>(p, range, &xmap, &tmap, &bmap, tmem, sbase, stage_bytes, ring, full0, free0, rfull0, rempty0, quit);
     } else if (warp == 2) {
         ok = load_codes<BITS, MODE>(p, range, ring, rfull0, rempty0, quit);
-    } else {
+    } else if (warp == 3) {
         ok = load_scales<MODE>(p, range, ring, rfull0, rempty0, quit);
     }
     if (!ok) {
@@ -695,6 +695,8 @@ cudaError_t launch_even(const EvenArgs &a, int *status, bool pdl, cudaStream_t s
     const int rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.slab = rank_pad / kBK;
     p.stages = (int)std::min<uint32_t>(kMostStages, (kSmemMost - kFixed) / (kWBytes + p.tok * (kBK * 2u)));
+    p.acc = (uint32_t)(p.tok + 31) / 32 * 32;
+    if (!grad) p.stages = std::min(p.stages, (int)((512u - 2u * p.acc) / 32u));
     p.gate = a.gate;
     p.kept_scales = a.kept_scales;
     p.kept_pitch = (p.F + kKeptGroup - 1) / kKeptGroup;
