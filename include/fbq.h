@@ -286,12 +286,12 @@ int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void 
 /* h [M][N/2] of a gated layer: p is gated in single precision where its sums are and rounded to the activation type never (h is,
  * once).  x, A, B, h: fp16 or bf16 (act_is_bf16).  At most 2 tokens run on the streaming kernel, 3 to 16 on the split kernel (layer rank up
  * to 128, and where fbq_split_plan has a plan for N rows), each in one launch; each computes p as it does for fbq_linear.  More tokens
- * run on the prompts' kernels, or up to 640 of a layer that makes more than 148 of their tiles on a kernel that shares the products out
- * evenly (four launches at most; t and the dequantised weights are rounded once to the activation type, as in the prompts' kernels).
+ * run on the prompts' kernels, or up to 900 of a layer that makes many of their tiles on a kernel that shares the products out evenly
+ * (four launches at most; t and the dequantised weights are rounded once to the activation type, as in the prompts' kernels).
  * "gemv" = 0 and "force_kernel" >= 0 leave the fewest tokens to the others too.
  *   kept, kept_scales   NULL, or what the backward pass needs of p in 8 bits: codes [M][N] and one scale per 128 columns of a row,
- *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M up to 640 run on the kernel that
- *       shares products out, of more on the prompts' dense kernel (scratch: a 16-bit copy of the weights, up to 512 MB per stream, which they
+ *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M up to 512 (900 of wide layers) run on
+ *       the kernel that shares products out, of more on the prompts' dense kernel (scratch: a 16-bit copy of the weights, up to 512 MB per stream, which they
  *       cannot do without).
  * Scratch of the sharing kernel: its sums (up to 29 MB), M x rank values of 16 bits, and partial sums of those; it grows as described at
  * fbq_linear, and a call that would grow it during a capture returns FBQ_ERR_UNSUPPORTED and queues nothing. */

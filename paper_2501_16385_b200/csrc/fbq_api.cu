@@ -287,25 +287,28 @@ int gated_kernel(const LinearArgs &a)
 }
 
 // Which calls dequantise weights where they are multiplied, with the blocks shared out evenly (fbq_even.cu), the sub-branch's thin products in a
-// launch before.  Backward passes, us, this / the dense kernel (INT4, rank 64; the first is the gated block's, 4096 -> 2 x 11008):
-//                    77 tokens    512       768       1024      1536      2048
-//   4096 <- 22016    57 / 248  144 / 192  191 / 199 261 / 218 371 / 372 511 / 421
-//   2048 <- 11008    39 / 131   72 / 109   85 / 111  97 / 116 127 / 142 185 / 165
-//   11008 <- 4096    36 /  72   83 / 103  105 / 125 146 / 135 190 / 186 295 / 228
-//   4096 <- 4096     25 /  62   43 /  55   52 /  57  72 /  59  88 /  99 129 / 109
-// so up to 768 tokens; in thousands of them more where the dense kernel's tiles (256 x 256 on 74 pairs) leave most of a wave empty, which
-// is not followed up here.
-constexpr int kEvenMost = 768, kEvenMostGated = 640;
+// launch before.  Backward passes, us, this / the dense kernel (INT4, rank 64; 4096 x 4096 INT3, rank 16; the first two are the gated block's):
+//                        77 tokens    320       512       768       900       1024      1280
+//   4096 <- 2 x 11008    60 / 189   97 / 189 136 / 193 184 / 203 220 / 216 259 / 225 310 / 363
+//   2048 <- 2 x 5504     42 /  99   53 / 103  65 / 110  77 / 114  87 / 115  98 / 117 107 / 134
+//   11008 <- 4096        37 /  71   66 / 110  88 / 120 113 / 130 130 / 132 145 / 138 169 / 142
+//   4096 <- 4096         26 /  48   35 /  52  44 /  55  54 /  56  65 /  59  73 /  61  78 /  97
+// so up to 768 tokens; above, where the dense kernel's tiles (256 x 256 on 74 pairs) leave most of a wave empty (4096 <- 2 x 11008 at 1280), it
+// is the dense kernel's all the same.
+constexpr int kEvenMost = 768;
 bool even_takes(int M) { return M <= kEvenMost; }
-// Gated blocks: where the tiles of the kernel that dequantises per tile (128 rows x up to 256 tokens, K cut where they are few) fit the SMs at once
-// that one is ahead, this / it: 2048 -> 2 x 5504 at 77 tokens 23 / 18 us, 256 33 / 24; 4096 -> 2 x 11008 42 / 60 and 76 / 74, at 512 (dense) 120 / 127,
-// 768 162 / 153.
+// Gated blocks, this / the kernel that dequantises per tile (128 rows x up to 256 tokens, K cut where they are few) or the dense one:
+//                        77 tokens    256       320       512       640       768       900       1024
+//   4096 -> 2 x 11008    40 / 60    68 / 75   74 / 105 106 / 128 129 / 146 145 / 155 174 / 186 196 / 184
+//   2048 -> 2 x 5504     22 / 18    32 / 24   35 / 40   44 / 46   51 / 46   56 / 47   63 / 65   71 / 67
+// Where the former's tiles fit the SMs at once that one is ahead; above 512 tokens this one is while the dense kernel's tiles are more than two
+// waves of pairs.  What is kept is written by this and the dense kernel alone.
+constexpr int kEvenAnyGated = 512, kEvenMostGated = 900;
 bool gated_even_takes(const LinearArgs &a)
 {
-    if (a.M > kEvenMostGated) return false;
-    if (a.kept) return true;
     const long long tiles = (long long)((a.N + 127) / 128) * ((a.M + 255) / 256);
-    return tiles > 148;
+    if (a.M > kEvenAnyGated) return a.M <= kEvenMostGated && tiles > 2 * 2 * 74;
+    return a.kept || tiles > 148;
 }
 size_t padded256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t thin_bytes(int M, int rank) { return padded256((size_t)M * ((rank + 63) / 64 * 64) * 2); }

@@ -11,7 +11,7 @@ namespace fbq {
 constexpr int kGateUp = 8;
 
 // f(v) = v S(z), S the logistic function: z = v (SiLU), or 2 sqrt(2/pi) (v + 0.044715 v^3), which makes 0.5 v (1 + tanh(z / 2)) of it
-// (GELU).  Errors are a few 2^-24 of f, and for z < -1 of |z| 2^-23 of it: far below the rounding of a 16-bit output.
+// (GELU).  Errors are a few 2^-24 of f, and for z < -1 of |z| 2^-23 of it: far below the rounding of a 16-bit output; below z = -87, where f is under 2^-119, it is 0.
 constexpr float kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282143484f;     // 2 sqrt(2/pi), times 0.044715
 __device__ __forceinline__ float gate_arg(int fn, float v) { return fn == FBQ_GATE_GELU ? v * fmaf(kGelu3, v * v, kGelu1) : v; }
 __device__ __forceinline__ float gate_value(int fn, float v) { return __fdividef(v, 1.f + __expf(-gate_arg(fn, v))); }

@@ -4,7 +4,8 @@
 // Both are D[c][j] = sum_m Q[m][c] P[m][j]: Q wide (x or dy), P narrow (s or t), the contraction over tokens, which are the rows of both as
 // they lie.  A CTA takes 128 columns of Q and all of P's: tcgen05.mma 128 x rank x 16 with both operands MN-major, straight from TMA
 // boxes of 64 columns x 64 tokens; nothing is transposed.  Q is read once, P (1 MB at 4096 tokens) stays in L2.  What bounds it is the
-// stream of Q, so two CTAs share an SM and each keeps its stages of 24 to 48 KB in flight.
+// stream of Q, so two CTAs share an SM and each keeps its stages of 24 to 48 KB in flight: 4096 tokens of x [4096] and dy [22016] at rank 128 take 43 us
+// (214 MB, 5.0 TB/s), 1024 of 11008 and 4096 at rank 64 10 and 3.5 for the sums (31 MB, most of it still in L2).
 // Few columns (or a bound on CTAs) leave SMs idle, so the tokens are cut into S slices; their fp32 sums go through scratch and a second
 // launch adds them in order (results do not depend on timing; no counter has to be cleared after a launch that was given up).
 #include <algorithm>

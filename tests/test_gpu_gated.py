@@ -72,7 +72,7 @@ def test_products_kept_in_8_bits(M, N, K, bits, rank, dtype, fn):
     assert int(codes.abs().max()) <= 127 and bool((pad(codes.abs().int(), (0, -N % 128)).view(M, -1, 128).amax(2) == 127).all())
 
 
-@pytest.mark.parametrize("M", [16, 40, 95, 112, 160, 176, 192, 193, 400, 640, 641])
+@pytest.mark.parametrize("M", [16, 40, 95, 112, 160, 176, 192, 193, 400, 512, 513])
 @pytest.mark.parametrize("rank", [16, 112, 192, 256])
 def test_products_kept_by_tiles_of_tokens(M, rank):
     """Every depth of the rings, odd and even numbers of the sub-branch's blocks, both sides of the size at which kernels change."""
@@ -83,6 +83,20 @@ def test_products_kept_by_tiles_of_tokens(M, rank):
     assert fbq.poll_status() == 0
     p, off = layer.products(x)
     check(h, *hidden("silu", p, off, dt), "h")
+    step = scales.double().repeat_interleave(128, 1)[:, :N]
+    check(kept64(codes, scales), p, off + step * (0.5 + 128 * 2.0**-22), "kept products")
+
+
+@pytest.mark.parametrize("M", [513, 900, 901])
+def test_wide_layers_of_hundreds_of_tokens(M):
+    """Both sides of the size at which the kernel of a wide layer changes."""
+    N, K, bits, rank, dt = 20016, 256, 4, 32, torch.float16
+    layer = Layer(fbq, N, K, bits, rank, dt, seed=M, gated=True)
+    x = inputs(M, K, dt, seed=7)
+    h, codes, scales = fbq.gated(x, *layer.tensors, N, 128, bits, save=True)
+    p, off = layer.products(x)
+    check(h, *hidden("silu", p, off, dt), "h")
+    check(fbq.gated(x, *layer.tensors, N, 128, bits), *hidden("silu", p, off, dt), "h")
     step = scales.double().repeat_interleave(128, 1)[:, :N]
     check(kept64(codes, scales), p, off + step * (0.5 + 128 * 2.0**-22), "kept products")
 
