@@ -294,7 +294,8 @@ int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void 
  *       the kernel that shares products out, of more on the prompts' dense kernel (scratch: a 16-bit copy of the weights, up to 512 MB per stream, which they
  *       cannot do without).
  * Scratch of the sharing kernel: its sums (up to 29 MB), M x rank values of 16 bits, and partial sums of those; it grows as described at
- * fbq_linear, and a call that would grow it during a capture returns FBQ_ERR_UNSUPPORTED and queues nothing. */
+ * fbq_linear, a call that would grow it during a capture returns FBQ_ERR_UNSUPPORTED and queues nothing, and graphs captured on one stream
+ * share it: replay them one after another. */
 int fbq_gated(const void *x, const uint32_t *qweight, const void *scales, const void *zeros, const void *A, const void *B, void *h,
               int8_t *kept, float *kept_scales, int M, int N, int K, int group, int bits, int rank, int gate, int act_is_bf16, void *stream);
 

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/fbq.h"
 
 namespace fbq {
@@ -14,6 +16,20 @@ constexpr int kGroupFast = 128;   // group size of the decode / prefill kernels 
 constexpr int kMaxRank = 256;
 constexpr int kMostSide = 1 << 30;               // rows or columns of a layer, for calls that count whole tiles of them in 31 bits
 constexpr int kDecodeMaxM = 16, kDecodePreferM = 6;
+
+// What is set once on each device of the process, by its number: a kernel's attributes belong to the device that was current.
+class PerDevice {
+    std::atomic<unsigned long long> on{0};
+    static unsigned long long bit()
+    {
+        int dev = 0;
+        return cudaGetDevice(&dev) == cudaSuccess && dev < 64 ? 1ull << dev : 0ull;
+    }
+
+public:
+    bool there() const { return (on.load(std::memory_order_relaxed) & bit()) != 0; }
+    void set() { on.fetch_or(bit(), std::memory_order_relaxed); }
+};
 
 // Activation-type helpers ---------------------------------------------------
 template <typename T> struct ActTraits;

@@ -685,10 +685,10 @@ cudaError_t start(const CUtensorMap (&maps)[9], const DenseParams &p, int n_pair
 {
     auto kern = dense_kernel<BITS, T, MODE>;
     constexpr size_t smem = MODE == kKept ? kSmemKept : kSmem;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         if (const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(2 * n_pairs));

@@ -644,10 +644,10 @@ template <int BITS, typename T, int MODE>
 cudaError_t start(const CUtensorMap (&maps)[5], const EvenParams &p, bool pdl, cudaStream_t s, int *launches)
 {
     auto kern = even_kernel<BITS, T, MODE>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         if (const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost + 1024); e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)p.ranges);

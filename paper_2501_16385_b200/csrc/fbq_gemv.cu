@@ -1310,15 +1310,15 @@ cudaError_t launch_variant(const Plan &pl, const CUtensorMap &wmap, const CUtens
                            cudaStream_t s)
 {
     auto kern = gemv_kernel<BITS, T, M, RANKED, GATED>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
         if (e != cudaSuccess) return e;
         // Always the largest shared-memory carve-out: launches with different dynamic sizes then share one SM
         // configuration, so the CTAs of consecutive launches can be resident side by side.
         e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(pl.p.n_t + pl.p.n_main));

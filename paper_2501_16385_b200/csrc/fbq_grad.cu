@@ -218,10 +218,10 @@ template <typename T> cudaError_t run(const void *dy, const void *x, const void 
     if ((e = encode_map(&tmap, matrix_map(t16, dt, 2, p.rank_pad, p.M, 64, kTok, sw))) != cudaSuccess) return e;
     const size_t smem = (size_t)p.stages * (2 + p.rank_pad / 64) * kBox + 1024;
     auto kern = factor_kernel<T>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmemMost + 1024))) != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cudaLaunchAttribute at[1];

@@ -1216,11 +1216,11 @@ cudaError_t launch_kernel(const CUtensorMap &xmap, const CUtensorMap &wmap, cons
                           const CUtensorMap &ymap, const CUtensorMap &tmap, const PrefillParams &p, unsigned grid, cudaStream_t s)
 {
     auto kern = prefill_kernel<BITS, T, TOK, GATED>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem<TOK>::kTotal);
         if (e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(grid);
@@ -1240,11 +1240,11 @@ cudaError_t launch_pair_kernel(const CUtensorMap &xmap, const CUtensorMap &wmap,
                                const CUtensorMap &ymap, const PrefillParams &p, unsigned grid, cudaStream_t s)
 {
     auto kern = prefill_pair_kernel<BITS, T>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairSmem::kTotal);
         if (e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(grid);

@@ -1094,13 +1094,13 @@ const Shape &shape_for(const LinearArgs *a, int count, int max_ctas)          //
 template <int BITS, typename T, int MT, bool GATED> cudaError_t launch_one(const Shape &s, bool pdl, cudaStream_t st)
 {
     auto kern = split_kernel<BITS, T, MT, GATED>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemAll);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.clusters << s.sp.cs_log2));

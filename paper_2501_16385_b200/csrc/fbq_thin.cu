@@ -284,11 +284,11 @@ template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, 
     if (!a.t) { xmap = dymap; amap = bmap; }
     if (!a.s) { dymap = xmap; bmap = amap; }
     auto kern = thin_kernel<T>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem)) != cudaSuccess) return e;
         if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(clusters * cs));
