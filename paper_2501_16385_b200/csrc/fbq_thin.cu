@@ -31,7 +31,8 @@ struct ThinParams {
     int M, rank_pad, a_rows;
     int tok, ntt, nrt;        // tokens of a tile, tiles, tiles of the rank
     int cuts_s, cuts_t;       // clusters that share a tile's contraction
-    int n_s;                  // clusters of s, before those of t
+    int n_first;              // clusters of the one of s and t whose take longer, before the other's
+    bool s_first;
     float *part;              // [cut][M][rank_pad] of s, then of t, or none: no contraction is cut
     int blocks_t, blocks_s;   // of the contractions
 };
@@ -60,8 +61,8 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cs));
     crank = cluster_ctarank();
     int cluster = (int)(blockIdx.x / cs);
-    const bool of_s = cluster < p.n_s;
-    if (!of_s) cluster -= p.n_s;
+    const bool first = cluster < p.n_first, of_s = first == p.s_first;
+    if (!first) cluster -= p.n_first;
     const int cuts = of_s ? p.cuts_s : p.cuts_t, cut = cluster % cuts;
     cluster /= cuts;
     const int rt = cluster % p.nrt, m0 = cluster / p.nrt * p.tok, row0 = rt * kRows;
@@ -199,9 +200,11 @@ template <typename T> __global__ void __launch_bounds__(256) thin_add_kernel(con
 }
 
 // The plan: CTAs of a cluster, tokens of a tile, and clusters that share a tile's contraction, such that what a CTA has to go through takes
-// least.  It reads some 60 bytes a nanosecond (A or B once per tile of tokens) and spends 4 us besides; clusters wait for one another where
-// more are wanted than the GPU holds at a time (one CTA per SM, and a cluster stays within one of the processing clusters).  Cuts cost
-// a launch and their sums' way through L2.  22016 rows of B at 333 tokens, rank 128: 22 us with eight CTAs a tile of 48 tokens and no cuts, 12 + 3 now.
+// least.  It reads some 60 bytes a nanosecond (A or B once per tile of tokens) and spends 4 us besides; where clusters are more than the GPU
+// holds at a time (one CTA per SM, and a cluster stays within one of the processing clusters) the longer ones go first and the others fill the
+// gaps, half of one's time late.  Cuts cost a launch and their sums' way through L2.  Sum of both launches, us, rank 128, against cuts by powers of
+// two and s always first: 22016 rows of B and 4096 of A at 100 tokens 18 -> 12, 700 24 -> 20, 4096 83 -> 60; 4096 and 11008 at 400 17.5 -> 14;
+// tiles of 256 tokens in two stages 86 for the 77 of the first launch.
 void plan(const ThinArgs &a, ThinParams &p, int *cluster)
 {
     p.M = a.M;
@@ -220,19 +223,14 @@ void plan(const ThinArgs &a, ThinParams &p, int *cluster)
             const int ntt = (a.M + tok - 1) / tok, sets = ntt * p.nrt;
             if (tok > 16 && (a.M + tok - 17) / (tok - 16) == ntt) continue;          // (fewer tokens make as many tiles)
             auto piece = [&](int blocks, int cuts) { return (double)((blocks + cs * cuts - 1) / (cs * cuts)) * (kABytes + tok * kBK * 2) / 60e3 + 4.0; };
-            for (int cut = 1; cut <= 8; cut *= 2) {
+            for (int cut = 1; cut <= 8; ++cut) {
                 // of s and t the longer contraction is cut more often
                 const int cuts_s = p.blocks_s ? std::max(1, std::min(cut, cut * p.blocks_s / most)) : 0, cuts_t = p.blocks_t ? std::max(1, std::min(cut, cut * p.blocks_t / most)) : 0;
-                double longest = 0, all = 0;
-                if (cuts_s) {
-                    longest = piece(p.blocks_s, cuts_s);
-                    all = sets * cuts_s * longest;
-                }
-                if (cuts_t) {
-                    longest = std::max(longest, piece(p.blocks_t, cuts_t));
-                    all += sets * cuts_t * piece(p.blocks_t, cuts_t);
-                }
-                const double cost = std::max(longest, all / resident[c]) + (cut > 1 ? 8.0 : 0.0);
+                const double of_s = cuts_s ? piece(p.blocks_s, cuts_s) : 0, of_t = cuts_t ? piece(p.blocks_t, cuts_t) : 0;
+                const double longest = std::max(of_s, of_t), all = sets * (cuts_s * of_s + cuts_t * of_t);
+                const double last = cuts_s && cuts_t ? std::min(of_s, of_t) : longest;
+                const int count = sets * (cuts_s + cuts_t);
+                const double cost = (count <= resident[c] ? longest + 3.0 : std::max(longest, all / resident[c] + last / 2)) + (cut > 1 ? 8.0 : 0.0);
                 if (cost >= least) continue;
                 least = cost;
                 *cluster = cs;
@@ -240,6 +238,7 @@ void plan(const ThinArgs &a, ThinParams &p, int *cluster)
                 p.ntt = ntt;
                 p.cuts_s = cuts_s;
                 p.cuts_t = cuts_t;
+                p.s_first = of_s >= of_t;
             }
         }
     }
@@ -269,8 +268,8 @@ template <typename T> cudaError_t run(const ThinArgs &a, int *status, bool pdl, 
     plan_for(a, p, &cs);
     p.t = a.t; p.s = a.s; p.status = status;
     p.part = p.cuts_s > 1 || p.cuts_t > 1 ? static_cast<float *>(a.part) : nullptr;
-    p.n_s = p.ntt * p.nrt * p.cuts_s;
-    const int clusters = p.n_s + p.ntt * p.nrt * p.cuts_t;
+    p.n_first = p.ntt * p.nrt * (p.s_first ? p.cuts_s : p.cuts_t);
+    const int clusters = p.ntt * p.nrt * (p.cuts_s + p.cuts_t);
     CUtensorMap xmap, dymap, amap, bmap;
     cudaError_t e;
     if (a.t) {
