@@ -33,7 +33,7 @@
 // take their share of issue slots and L2, then 0.43 us per K block against 0.31 us of MMAs at that clock: the SMs read 32 KB
 // each per block from L2.  The weights' operand made in shared memory by each pair (20 KB per block) was measured
 // as well: 0.7 us per block, the producers' hand-shake with the other CTA's MMAs is slower than the copies.
-// Gated layers (the epilogue gates p, and keeps it in 8 bits): 22016 x 4096 at 1024 tokens 179 us (1.03 PFLOP/s, 4.65 waves of tiles that cost five),
+// Gated layers (the epilogue gates p, and keeps it in 8 bits): 22016 x 4096 at 1024 tokens 179 us (1.03 PFLOP/s, 430 tiles of 208 tokens),
 // 27648 x 5120 at 4000 with p kept 880 (1.29).  Backward pass (dx, all operands but the tokens MN-major): 4096 <- 22016 at 4096 tokens 610 us
 // (1.21 PFLOP/s), 13824 <- 5120 475 (1.22).
 #include <cuda.h>

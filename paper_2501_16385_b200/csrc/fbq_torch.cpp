@@ -5,6 +5,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -186,6 +187,9 @@ int size_arg(int64_t n)
 }
 int64_t groups_of(int64_t columns) { return (columns + 127) / 128; }
 
+// A new tensor on the current device, without the dispatcher's detours.
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type) { return at::Tensor(at::detail::empty_cuda(shape, type, at::Device(at::kCUDA), std::nullopt)); }
+
 struct Layer {
     void *q, *s, *z, *A = nullptr, *B = nullptr;
     int rank = 0;
@@ -271,14 +275,14 @@ PyObject *py_gated(PyObject *, PyObject *const *v, Py_ssize_t n)
         void *stream = stream_arg(v[12]);
         at::Tensor h, codes, scales;
         if (v[11] == Py_None) {
-            h = at::empty({M, N / 2}, x.options());
+            h = fresh({M, N / 2}, act);
         } else {
             operand(v[11], "h", act, {M, N / 2});
             h = THPVariable_Unpack(v[11]);
         }
         if (save) {
-            codes = at::empty({M, N}, x.options().dtype(at::kChar));
-            scales = at::empty({M, groups_of(N)}, x.options().dtype(at::kFloat));
+            codes = fresh({M, N}, at::kChar);
+            scales = fresh({M, groups_of(N)}, at::kFloat);
         }
         const int m = size_arg(M), k = size_arg(K);
         const int rc = without_gil([&] {
@@ -298,7 +302,7 @@ PyObject *py_act8_pack(PyObject *, PyObject *const *v, Py_ssize_t n)
         const at::ScalarType act = act_type(x, "x");
         const int64_t M = x.size(0), K = x.size(1);
         void *px = operand(v[0], "x", act, {M, K}), *stream = stream_arg(v[1]);
-        const at::Tensor codes = at::empty({M, K}, x.options().dtype(at::kChar)), scales = at::empty({M, groups_of(K)}, x.options().dtype(at::kFloat));
+        const at::Tensor codes = fresh({M, K}, at::kChar), scales = fresh({M, groups_of(K)}, at::kFloat);
         const int m = size_arg(M), k = size_arg(K);
         const int rc = without_gil([&] { return fbq_act8_pack(px, (int8_t *)codes.data_ptr(), (float *)scales.data_ptr(), m, k, act == at::kBFloat16, stream); });
         return rc == FBQ_OK ? results({codes, scales}) : PyLong_FromLong(rc);
@@ -314,7 +318,7 @@ PyObject *py_act8_unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
         void *pc = operand(v[0], "codes", at::kChar, {M, K}), *ps = operand(v[1], "scales", at::kFloat, {M, groups_of(K)});
         const bool bf16 = PyObject_IsTrue(v[2]) == 1;
         void *stream = stream_arg(v[3]);
-        const at::Tensor x = at::empty({M, K}, codes.options().dtype(bf16 ? at::kBFloat16 : at::kHalf));
+        const at::Tensor x = fresh({M, K}, bf16 ? at::kBFloat16 : at::kHalf);
         const int m = size_arg(M), k = size_arg(K);
         const int rc = without_gil([&] { return fbq_act8_unpack((const int8_t *)pc, (const float *)ps, x.data_ptr(), m, k, bf16, stream); });
         return rc == FBQ_OK ? THPVariable_Wrap(x) : PyLong_FromLong(rc);
@@ -347,10 +351,10 @@ PyObject *py_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
         }
         void *stream = stream_arg(v[16]);
         at::Tensor dx, dA, dB;
-        if (want_dx) dx = at::empty({M, K}, dy.options());
+        if (want_dx) dx = fresh({M, K}, act);
         if (want_factors && l.rank > 0) {
-            dA = at::empty({l.rank, K}, dy.options());
-            dB = at::empty({N, l.rank}, dy.options());
+            dA = fresh({l.rank, K}, act);
+            dB = fresh({N, l.rank}, act);
         }
         auto at_of = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
         const int m = size_arg(M), nn = size_arg(N), k = size_arg(K);
