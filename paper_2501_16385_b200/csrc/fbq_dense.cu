@@ -857,11 +857,11 @@ cudaError_t launch_dense(const LinearArgs &a, Workspace &ws, const PrefillTuning
 
 // Tiles of s and t among those of dx cost a wave of pairs where they do not fit into the last one, and from some thousand tokens on more than a
 // launch of their own before this one.  Measured (us, in this launch / before it; INT4, rank 64, 4096 x 4096 INT3, rank 16):
-//                   768 tokens    1024       1536       2048       4096
-//   4096 <- 22016   200 / 218  220 / 239  448 / 387  481 / 430  881 / 815
-//   2048 <- 11008   112 / 130  116 / 128  171 / 144  181 / 175  311 / 326
-//   11008 <- 4096   150 / 125  164 / 135  199 / 201  249 / 233  502 / 449
-//   4096 <- 4096     57 /  68   59 /  73   99 / 101  108 / 108  185 / 181
+//                   776 tokens    1024       1280       1536       2048       4096
+//   4096 <- 22016   205 / 216  221 / 238  441 / 353  448 / 373  480 / 421  845 / 786
+//   2048 <- 11008   115 / 125  117 / 129  169 / 133  172 / 142  180 / 154  309 / 306
+//   11008 <- 4096   150 / 125  164 / 129  168 / 135  199 / 186  245 / 221  458 / 457
+//   4096 <- 4096     58 /  70   60 /  73   99 /  97  101 / 101  102 / 111  176 / 188
 // A tile of s has as many blocks as one of dx, one of t K / N as many.
 bool grad_thin_first(const GradArgs &a)
 {
