@@ -289,18 +289,18 @@ int gated_kernel(const LinearArgs &a)
 // Which calls dequantise weights where they are multiplied, with the blocks shared out evenly (fbq_even.cu), the sub-branch's thin products in a
 // launch before.  Backward passes, us, this / the dense kernel (INT4, rank 64; 4096 x 4096 INT3, rank 16; the first two are the gated block's):
 //                        77 tokens    320       512       768       900       1024      1280
-//   4096 <- 2 x 11008    60 / 189   97 / 189 136 / 193 184 / 203 220 / 216 259 / 225 310 / 363
-//   2048 <- 2 x 5504     42 /  99   53 / 103  65 / 110  77 / 114  87 / 115  98 / 117 107 / 134
-//   11008 <- 4096        37 /  71   66 / 110  88 / 120 113 / 130 130 / 132 145 / 138 169 / 142
-//   4096 <- 4096         26 /  48   35 /  52  44 /  55  54 /  56  65 /  59  73 /  61  78 /  97
+//   4096 <- 2 x 11008    59 / 195  101 / 188 135 / 190 182 / 200 215 / 215 253 / 221 301 / 394
+//   2048 <- 2 x 5504     41 / 100   53 / 103  66 / 109  77 / 113  87 / 115  94 / 118 109 / 149
+//   11008 <- 4096        37 /  71   60 / 110  84 / 121 107 / 125 126 / 126 141 / 130 184 / 150
+//   4096 <- 4096         25 /  49   35 /  51  44 /  55  54 /  57  65 /  59  73 /  60  87 / 108
 // so up to 768 tokens; above, where the dense kernel's tiles (256 x 256 on 74 pairs) leave most of a wave empty (4096 <- 2 x 11008 at 1280), it
 // is the dense kernel's all the same.
 constexpr int kEvenMost = 768;
 bool even_takes(int M) { return M <= kEvenMost; }
 // Gated blocks, this / the kernel that dequantises per tile (128 rows x up to 256 tokens, K cut where they are few) or the dense one:
 //                        77 tokens    256       320       512       640       768       900       1024
-//   4096 -> 2 x 11008    40 / 60    68 / 75   74 / 105 106 / 128 129 / 146 145 / 155 174 / 186 196 / 184
-//   2048 -> 2 x 5504     22 / 18    32 / 24   35 / 40   44 / 46   51 / 46   56 / 47   63 / 65   71 / 67
+//   4096 -> 2 x 11008    40 / 60    68 / 74   73 / 105 105 / 127 128 / 144 144 / 154 173 / 186 195 / 183
+//   2048 -> 2 x 5504     23 / 19    35 / 24   35 / 40   47 / 45   51 / 46   59 / 47   64 / 66   71 / 68
 // Where the former's tiles fit the SMs at once that one is ahead; above 512 tokens this one is while the dense kernel's tiles are more than two
 // waves of pairs.  What is kept is written by this and the dense kernel alone.
 constexpr int kEvenAnyGated = 512, kEvenMostGated = 900;
