@@ -52,8 +52,18 @@ cudaError_t encode_map(CUtensorMap *out, const MapSpec &m)
         encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
     }
     const cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = encode(out, m.type, (cuuint32_t)m.ndim, const_cast<void *>(m.base), m.dims, m.strides, m.box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              m.swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    auto go = [&] {
+        return encode(out, m.type, (cuuint32_t)m.ndim, const_cast<void *>(m.base), m.dims, m.strides, m.box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, m.swizzle,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = go();
+    if (r == CUDA_ERROR_INVALID_CONTEXT) {                       // a host thread that has launched nothing yet: the runtime would give it its device's at the launch
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e == cudaSuccess) e = cudaSetDevice(dev);
+        if (e != cudaSuccess) return e;
+        r = go();
+    }
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
