@@ -23,6 +23,10 @@
  *     Calls are asynchronous: the return value reports host-side validation and
  *     launch errors only.  Calls on one stream run in order; calls on different
  *     streams may run concurrently (each stream gets its own scratch space).
+ *     Any number of host threads may call, on one stream too: the launches of a
+ *     call are queued together, none of another thread's call between them
+ *     (fbq_linear_noalloc has rules of its own; options are set while no other
+ *     thread calls).
  *   - Return value: FBQ_OK or a negative fbq_status.
  *   - The library runs CUDA kernels only.  There is no CPU fallback: without a
  *     usable device every compute entry point returns FBQ_ERR_CUDA.

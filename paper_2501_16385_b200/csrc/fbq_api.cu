@@ -5,10 +5,10 @@
 #include <atomic>
 #include <cstring>
 #include <initializer_list>
-#include <iterator>
 #include <map>
 #include <mutex>
 #include <utility>
+#include <vector>
 
 #include "fbq_common.cuh"
 #include "fbq_gate.cuh"
@@ -24,7 +24,14 @@ void prefill_set_test(int skip_flag, int flag_polls);
 namespace {
 
 std::mutex g_mu;
-std::map<std::pair<int, cudaStream_t>, Workspace> g_ws;
+// A stream's scratch.  Calls hand values from launch to launch through it at places that are the same for every call, so a call holds the lock from
+// its first launch to its last: of two host threads on one stream one queues all of its launches, then the other.  A call
+// within a call, a linear of a batch say, holds it already.  Entries stay where they are for the life of the process.
+struct StreamScratch {
+    Workspace ws;
+    std::recursive_mutex mu;
+};
+std::map<std::pair<int, cudaStream_t>, StreamScratch> g_ws;
 std::atomic<long long> g_launches{0};
 
 struct Options {
@@ -194,12 +201,31 @@ cudaError_t grow(P *&ptr, size_t &have, size_t need, size_t elem, cudaStream_t s
     return cudaSuccess;
 }
 
-Workspace *workspace_for(cudaStream_t s)
+// The scratch of a stream of the current device, held by this thread; none without a device.
+class HeldWorkspace {
+    std::unique_lock<std::recursive_mutex> held;
+    Workspace *ws = nullptr;
+
+public:
+    HeldWorkspace() = default;
+    explicit HeldWorkspace(StreamScratch &s) : held(s.mu), ws(&s.ws) {}
+    explicit operator bool() const { return ws != nullptr; }
+    Workspace *get() const { return ws; }
+    Workspace *operator->() const { return ws; }
+    Workspace &operator*() const { return *ws; }
+};
+HeldWorkspace workspace_for(cudaStream_t s)
 {
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
-    std::lock_guard<std::mutex> lk(g_mu);
-    return &g_ws[std::make_pair(dev, s)];
+    if (cudaGetDevice(&dev) != cudaSuccess) return HeldWorkspace();
+    // what this thread was given last, as a rule what it wants again
+    static thread_local std::pair<int, cudaStream_t> last{-1, nullptr};
+    static thread_local StreamScratch *scratch = nullptr;
+    if (last.first != dev || last.second != s) {
+        std::lock_guard<std::mutex> lk(g_mu);                    // (not held while a thread waits for the stream's)
+        scratch = &g_ws[last = std::make_pair(dev, s)];
+    }
+    return HeldWorkspace(*scratch);
 }
 
 int grow_status(cudaError_t e) { return e == cudaErrorStreamCaptureUnsupported ? FBQ_ERR_UNSUPPORTED : FBQ_ERR_CUDA; }
@@ -261,14 +287,14 @@ int run_gemv_batch(const LinearArgs *a, int count, cudaStream_t s)
 {
     for (int i = 0; i < count; ++i)
         if (const int rc = check_args(a[i]); rc != FBQ_OK) return rc;
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     GemvTuning gt = g_opt.gemv;
     gt.pdl = g_opt.decode.pdl;
     size_t slots = 0;
     int nc = 0, launches = 0;
     if (!batch_plan_exists(a, count, gt, &slots, &nc)) return FBQ_ERR_UNSUPPORTED;
-    if (a[0].M > kGemvMaxM) return run_split(a, count, gt, ws, s);
+    if (a[0].M > kGemvMaxM) return run_split(a, count, gt, ws.get(), s);
     size_t have_c = (size_t)ws->n_counters;
     cudaError_t e;
     if ((e = grow(ws->tslots, ws->tslots_floats, slots, sizeof(float), s)) != cudaSuccess) return grow_status(e);
@@ -360,7 +386,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
     if (a.M == 0) return FBQ_OK;
     if (const int rc = check_args(a); rc != FBQ_OK) return rc;
 
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     int kernel = a.gate < 0 ? select_kernel(a.M, a.N, a.K, a.group, a.bits, a.rank, a.bf16) : gated_kernel(a);
     if (kernel == FBQ_KERNEL_NONE) return FBQ_ERR_UNSUPPORTED;
@@ -372,7 +398,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         gt.pdl = g_opt.decode.pdl;
         if (tune.max_ctas > 0) gt.max_ctas = tune.max_ctas;
         if (gt.max_ctas == 0) gt.max_ctas = ws->gemv_ctas;
-        if (split_plan_exists(&a, 1, gt)) return run_split(&a, 1, gt, ws, s);
+        if (split_plan_exists(&a, 1, gt)) return run_split(&a, 1, gt, ws.get(), s);
     }
     if (kernel == FBQ_KERNEL_DECODE && g_opt.use_gemv && a.M <= kGemvMaxM && gemv_supported(a)) {
         GemvTuning gt = g_opt.gemv;
@@ -426,7 +452,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
             return FBQ_ERR_CUDA;
         }
     }
-    if (a.gate >= 0 && kernel == FBQ_KERNEL_PREFILL && gated_even_takes(a)) return run_gated_even(a, ws, s);
+    if (a.gate >= 0 && kernel == FBQ_KERNEL_PREFILL && gated_even_takes(a)) return run_gated_even(a, ws.get(), s);
     if (kernel == FBQ_KERNEL_PREFILL) {
         size_t have_c = (size_t)ws->n_counters, need_t = 0, need_p = 0;
         int need_c = 0;
@@ -487,7 +513,7 @@ int run_backward(Backward &b, cudaStream_t s)
     GradArgs &g = b.g;
     const bool factors = g.rank > 0 && b.dA, unpack = factors && b.x8;
     if (!factors && !g.dx) return FBQ_OK;
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     size_t need = 0;
     auto place = [&](size_t bytes) {
@@ -498,8 +524,8 @@ int run_backward(Backward &b, cudaStream_t s)
     const bool even = even_takes(g.M), thin_first = g.rank > 0 && (even || grad_thin_first(g));
     ThinArgs t{};
     t.M = g.M; t.N = g.N; t.K = g.K; t.rank = g.rank; t.bf16 = g.bf16;
-    t.s = ws;                                                    // (any address: where it will be is not known yet)
-    t.t = factors ? ws : nullptr;
+    t.s = ws.get();                                              // (any address: where it will be is not known yet)
+    t.t = factors ? ws.get() : nullptr;
     const size_t M = g.M, thin = thin_bytes(g.M, g.rank);
     const size_t x_at = place(unpack ? M * g.K * 2 : 0), dy_at = place(b.kept ? M * g.N * 2 : 0), s_at = place(thin), t_at = place(factors ? thin : 0),
                  part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), thin_at = place(thin_first ? thin_part_bytes(t) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
@@ -558,7 +584,7 @@ int run_backward(Backward &b, cudaStream_t s)
 template <typename N, typename F>
 int with_scratch(N need, cudaStream_t s, F f, void *spare = nullptr, size_t spare_bytes = 0)
 {
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     int launches = 0, rc = FBQ_ERR_CUDA;
     size_t have_c = (size_t)ws->n_counters;
@@ -997,11 +1023,11 @@ static int host_batch(const LinearArgs *in, const fbq_problem *problems, int cou
     LinearArgs a[FBQ_BATCH_MAX];
     size_t y_bytes = 0;
     auto padded = [](size_t n) { return (n + 255) & ~(size_t)255; };
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     std::copy(in, in + count, a);
     BatchX x;
-    if (const int rc = place_batch_x(a, count, M, ws, s, x); rc != FBQ_OK) return rc;
+    if (const int rc = place_batch_x(a, count, M, ws.get(), s, x); rc != FBQ_OK) return rc;
     char *sy = static_cast<char *>(ws->stage_y);
     cudaError_t e;
     bool staged[FBQ_BATCH_MAX];
@@ -1061,7 +1087,7 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
     // staging buffers kept per stream, on the stream the problem runs on.
     auto stage_y = [&](LinearArgs &la, cudaStream_t st) -> int {
         if (!host_io) return FBQ_OK;
-        Workspace *ws = workspace_for(st);
+        const HeldWorkspace ws = workspace_for(st);
         if (!ws || !la.y) return ws ? FBQ_ERR_BADARG : FBQ_ERR_CUDA;
         const size_t yb = (size_t)M * la.N * 2;
         if (void *alias = direct_y_alias(la.y, yb)) {
@@ -1076,16 +1102,16 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
     };
     auto stage_in = [&](LinearArgs &la, cudaStream_t st) -> int {
         if (!host_io) return FBQ_OK;
-        Workspace *ws = workspace_for(st);
+        const HeldWorkspace ws = workspace_for(st);
         if (!ws) return FBQ_ERR_CUDA;
         BatchX x;
-        if (const int rc = place_batch_x(&la, 1, M, ws, st, x); rc != FBQ_OK) return rc;
+        if (const int rc = place_batch_x(&la, 1, M, ws.get(), st, x); rc != FBQ_OK) return rc;
         if (copy_in(x.n, x.src, x.dst, x.bytes, st) != cudaSuccess) return FBQ_ERR_CUDA;
         return stage_y(la, st);
     };
     auto stage_out = [&](const LinearArgs &la, void *y_host, cudaStream_t st) -> int {
         if (!host_io) return FBQ_OK;
-        Workspace *ws = workspace_for(st);
+        const HeldWorkspace ws = workspace_for(st);
         if (!ws || la.y != ws->stage_y) return FBQ_OK;      // written in place
         return cudaMemcpyAsync(y_host, la.y, (size_t)M * la.N * 2, cudaMemcpyDeviceToHost, st) == cudaSuccess ? FBQ_OK : FBQ_ERR_CUDA;
     };
@@ -1111,14 +1137,14 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
         // One after the other on the caller's stream (prefill-sized problems fill the GPU by themselves).  x from host buffers
         // comes over at the start, shared x once, unless that takes much staging space: one by one each copy would wait for the linear
         // before.
+        const HeldWorkspace ws = workspace_for(main);            // (from the first copy to the last)
+        if (!ws) return FBQ_ERR_CUDA;
         size_t x_bytes = 0;
         for (int i = 0; i < count; ++i) x_bytes += (size_t)M * a[i].K * 2;
         const bool together = host_io && x_bytes <= 8 * kGatherMost;
         if (together) {
-            Workspace *ws = workspace_for(main);
-            if (!ws) return FBQ_ERR_CUDA;
             BatchX x;
-            if (const int rc = place_batch_x(a, count, M, ws, main, x); rc != FBQ_OK) return rc;
+            if (const int rc = place_batch_x(a, count, M, ws.get(), main, x); rc != FBQ_OK) return rc;
             // as few gathers as take kGatherMost each
             for (int first = 0, n; first < x.n; first += n) {
                 size_t part = x.bytes[first];
@@ -1151,7 +1177,7 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
                 misaligned16(a[i].y))
                 return FBQ_ERR_ALIGN;
         }
-        Workspace *ws = workspace_for(main);
+        const HeldWorkspace ws = workspace_for(main);
         if (!ws) return FBQ_ERR_CUDA;
         size_t pf = 0, tf = 0;
         int nc = 0;
@@ -1212,7 +1238,7 @@ int fbq_linear_hostio(const void *x_host, const uint32_t *qweight, const void *s
     if (M == 0) return FBQ_OK;
     if (!x_host || !y_host) return FBQ_ERR_BADARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     const size_t xb = (size_t)M * K * 2, yb = (size_t)M * N * 2;
     char *sx = static_cast<char *>(ws->stage_x), *sy = static_cast<char *>(ws->stage_y);
@@ -1238,7 +1264,7 @@ int fbq_sub_branch_unfused(const void *x, const void *A, const void *B, void *y,
     if (M == 0) return FBQ_OK;
     if (!x || !A || !B || !y) return FBQ_ERR_BADARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     cudaError_t e;
     if ((e = grow(ws->t_gen, ws->t_gen_floats, (size_t)M * rank + ((size_t)M * N + 1) / 2 + 4, sizeof(float), s)) != cudaSuccess)
@@ -1275,7 +1301,7 @@ int fbq_set_option(const char *name, int value)
 int fbq_set_stream_option(void *stream, const char *name, int value)
 {
     if (!name || strcmp(name, "gemv_ctas") || value < 0) return FBQ_ERR_BADARG;
-    Workspace *ws = workspace_for(static_cast<cudaStream_t>(stream));
+    const HeldWorkspace ws = workspace_for(static_cast<cudaStream_t>(stream));
     if (!ws) return FBQ_ERR_CUDA;
     ws->gemv_ctas = value;
     return FBQ_OK;
@@ -1294,9 +1320,9 @@ long long fbq_launch_count(void) { return g_launches.load(); }
 int fbq_poll_status(void *stream)
 {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cudaStreamSynchronize(s) != cudaSuccess) return FBQ_ERR_CUDA;
-    Workspace *ws = workspace_for(s);
+    const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
+    if (cudaStreamSynchronize(s) != cudaSuccess) return FBQ_ERR_CUDA;
     // the fixed scratch array of fbq_linear_noalloc has a status word of its own (shared by all streams)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return FBQ_ERR_CUDA;
@@ -1319,18 +1345,24 @@ int fbq_poll_status(void *stream)
 int fbq_debug_read_trace(void *stream, void *host_buf, size_t bytes)
 {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (cudaStreamSynchronize(s) != cudaSuccess) return FBQ_ERR_CUDA;
-    Workspace *ws = workspace_for(s);
-    if (!ws || !ws->trace || !host_buf || bytes > kTraceBytes) return FBQ_ERR_BADARG;
+    const HeldWorkspace ws = workspace_for(s);
+    if (!ws || cudaStreamSynchronize(s) != cudaSuccess) return FBQ_ERR_CUDA;
+    if (!ws->trace || !host_buf || bytes > kTraceBytes) return FBQ_ERR_BADARG;
     return cudaMemcpy(host_buf, ws->trace, bytes, cudaMemcpyDeviceToHost) == cudaSuccess ? FBQ_OK : FBQ_ERR_CUDA;
 }
 
 int fbq_release_workspaces(void)
 {
     if (cudaDeviceSynchronize() != cudaSuccess) return FBQ_ERR_CUDA;
-    std::lock_guard<std::mutex> lk(g_mu);
-    for (auto &kv : g_ws) {
-        Workspace &w = kv.second;
+    std::vector<StreamScratch *> all;
+    {
+        std::lock_guard<std::mutex> lk(g_mu);
+        for (auto &kv : g_ws) all.push_back(&kv.second);
+    }
+    for (StreamScratch *scratch : all) {
+        std::lock_guard<std::recursive_mutex> lk(scratch->mu);
+        if (cudaDeviceSynchronize() != cudaSuccess) return FBQ_ERR_CUDA;         // (what another thread has queued meanwhile)
+        Workspace &w = scratch->ws;
         cudaFree(w.partial);
         cudaFree(w.t);
         cudaFree(w.t_gen);
@@ -1344,12 +1376,9 @@ int fbq_release_workspaces(void)
         cudaFree(w.split);
         cudaFree(w.grad);
         cudaFree(w.rec);
-    }
-    for (auto it = g_ws.begin(); it != g_ws.end();) {            // what is left of a stream are its options
-        const int gemv_ctas = it->second.gemv_ctas;
-        it->second = Workspace{};
-        it->second.gemv_ctas = gemv_ctas;
-        it = gemv_ctas ? std::next(it) : g_ws.erase(it);
+        const int gemv_ctas = w.gemv_ctas;                       // what is left of a stream are its options
+        w = Workspace{};
+        w.gemv_ctas = gemv_ctas;
     }
     return FBQ_OK;
 }
