@@ -964,6 +964,7 @@ struct BatchLanes {
     cudaStream_t side[FBQ_BATCH_MAX] = {};
     cudaEvent_t fork = nullptr, join[FBQ_BATCH_MAX] = {};
     int n = 0;
+    std::mutex forked;            // from the fork of a batch to its last join: an event recorded anew by another host thread would stand for that one's stream
 };
 static std::map<int, BatchLanes> g_lanes;
 
@@ -1199,6 +1200,7 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
     // stream by events.
     BatchLanes *lanes = lanes_for(count);
     if (!lanes) return FBQ_ERR_CUDA;
+    std::lock_guard<std::mutex> lk(lanes->forked);
     if (cudaEventRecord(lanes->fork, main) != cudaSuccess) return FBQ_ERR_CUDA;
     int rc = FBQ_OK;
     int forked = 0;
