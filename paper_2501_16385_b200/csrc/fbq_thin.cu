@@ -1,5 +1,5 @@
 // The sub-branch's thin products for few hundred tokens, sm_100a:  t = x.A^T  and  s = dy.B,  [M][rank], rounded once to the activation
-// type (they are tensor-core operands of the launch behind this one).
+// type (they are tensor-core operands of the launch behind this one); entries up to the next multiple of 64 are zeros.
 //
 // Little arithmetic over long contractions, so what counts is how many SMs read: a cluster of CTAs takes a tile of tokens and up to 128
 // entries of the rank and cuts the contraction (tcgen05.mma, the rank's entries are the rows, tokens the columns; A is K-major, B as
@@ -28,7 +28,7 @@ static_assert(kMostTok * kRows * 4u <= kSmem - 1024, "the sums take the stages' 
 struct ThinParams {
     void *t, *s;              // [M][rank_pad]
     int *status;
-    int M, rank_pad, a_rows;
+    int M, rank, rank_pad, a_rows;
     int tok, ntt, nrt;        // tokens of a tile, tiles, tiles of the rank
     int cuts_s, cuts_t;       // clusters that share a tile's contraction
     int n_first;              // clusters of the one of s and t whose take longer, before the other's
@@ -172,6 +172,7 @@ thin_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         for (uint32_t k = 0; k < kMostCluster; ++k) w[k] = k < cs ? ld_cluster(mapa_shared(sbase + (uint32_t)(c * kRows + j) * 4u, k)) : 0.f;
 #pragma unroll
         for (int k = 0; k < kMostCluster; ++k) v += w[k];
+        if (row0 + j >= p.rank) v = 0.f;                         // (an infinite x times the zeros of an entry that is not there)
         const size_t to = (size_t)(m0 + c) * p.rank_pad + row0 + j;
         if (p.part) part[to] = v;
         else out[to] = to_bits16<T>(v);
@@ -208,6 +209,7 @@ template <typename T> __global__ void __launch_bounds__(256) thin_add_kernel(con
 void plan(const ThinArgs &a, ThinParams &p, int *cluster)
 {
     p.M = a.M;
+    p.rank = a.rank;
     p.rank_pad = (a.rank + kBK - 1) / kBK * kBK;
     p.a_rows = std::min(kRows, p.rank_pad);
     p.nrt = (p.rank_pad + kRows - 1) / kRows;
