@@ -499,11 +499,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
                             for (int j = 0; j < 32; ++j) sp[j * kBN] = to_bits16<T>(__uint_as_float(v[j]));
                         }
                     } else if (p.t16) {
-                        if (nn < p.rank_pad) {               // rounded once, here; rows of A beyond the rank are zero fill
+                        if (nn < p.rank_pad) {               // rounded once, here; 0 beyond the rank, where the MMAs have x times zero fill: NaN for an infinite x
                             unsigned short *tp = static_cast<unsigned short *>(p.t16) + (size_t)(m0 + c) * p.rank_pad + nn;
 #pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (m0 + c + j < p.M) tp[(size_t)j * p.rank_pad] = to_bits16<T>(__uint_as_float(v[j]));
+                                if (m0 + c + j < p.M) tp[(size_t)j * p.rank_pad] = nn < p.rank ? to_bits16<T>(__uint_as_float(v[j])) : (unsigned short)0;
                         }
                     } else {
                         if (nn < p.rank) {                   // 32 lanes = 32 consecutive rank indices: 128-byte stores

@@ -49,7 +49,7 @@ def test_gradient(M, N, K, rank, dtype):
 
 @pytest.mark.parametrize("M", [5, 40, 200, 513])
 @pytest.mark.parametrize("rank,dtype", [(16, torch.float16), (80, torch.bfloat16), (128, torch.float16)])
-@pytest.mark.parametrize("save", [True])
+@pytest.mark.parametrize("save", [False, True])
 def test_gated(M, rank, dtype, save):
     N, K = 272, 384
     layer = layer_of(N, K, rank, dtype)
@@ -65,3 +65,17 @@ def test_gated(M, rank, dtype, save):
     assert torch.equal(h[others], first[others]) and same(h[1], want)
     if save:
         assert bool(torch.isnan(got[2][1]).all()) and all(torch.equal(a[others], b[others]) for a, b in zip(got[1:], clean[1:]))
+
+
+@pytest.mark.parametrize("M", [17, 100, 200, 700])
+@pytest.mark.parametrize("rank,dtype", [(8, torch.float16), (72, torch.bfloat16), (128, torch.float16)])
+def test_prompt(M, rank, dtype):
+    N, K = 264, 384
+    layer = layer_of(N, K, rank, dtype)
+    x = normal(M, K, dtype, 2)
+    clean = fbq.linear(x, *layer.tensors, N, 128, 4)
+    x[1, 5] = math.inf
+    y = fbq.linear(x, *layer.tensors, N, 128, 4)
+    assert fbq.poll_status() == 0
+    others = [m for m in range(M) if m != 1]
+    assert torch.equal(y[others], clean[others]) and same(y[1], infinite(layer.W[:, 5]))
