@@ -4,6 +4,10 @@ Tensors are torch CUDA tensors (PyTorch supplies device memory and streams);
 their data pointers and the current stream's handle are passed straight to the
 C ABI declared in include/fbq.h: by the native module _fbq_torch for the calls
 of a decode loop, through ctypes for the rest.
+
+``stream`` (a torch.cuda.Stream, default: the current one) is the stream that a call
+is queued on.  The tensors that it returns are memory of that stream, as if it had been
+current: inputs have to be ready on it, another stream that uses the results waits for it.
 """
 from __future__ import annotations
 
@@ -111,6 +115,14 @@ def _stream(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _outputs_of(stream):
+    """Context in which new tensors are memory of ``stream``, on which the call will write them."""
+    import torch
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    return torch.cuda.stream(stream)                             # (None: nothing changes)
+
+
 def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -127,7 +139,8 @@ def pack(codes, bits: int, stream=None):
     nw = packed_words(N, K, bits)
     if nw == 0:
         raise FbqError(-1, "fbq_packed_words")
-    q = torch.empty(nw, dtype=torch.int32, device=codes.device)
+    with _outputs_of(stream):
+        q = torch.empty(nw, dtype=torch.int32, device=codes.device)
     fn = lib().fbq_pack_int4 if bits == 4 else lib().fbq_pack_int3
     _check(fn(_ptr(codes), _ptr(q), N, K, _stream(stream)), "fbq_pack_int%d" % bits)
     return q
@@ -135,14 +148,16 @@ def pack(codes, bits: int, stream=None):
 
 def unpack(qweight, N: int, K: int, bits: int, stream=None):
     import torch
-    codes = torch.empty((N, K), dtype=torch.uint8, device=qweight.device)
+    with _outputs_of(stream):
+        codes = torch.empty((N, K), dtype=torch.uint8, device=qweight.device)
     _check(lib().fbq_unpack(_ptr(qweight), _ptr(codes), N, K, bits, _stream(stream)), "fbq_unpack")
     return codes
 
 
 def dequant(qweight, scales, zeros, N: int, K: int, group: int, bits: int, stream=None):
     import torch
-    W = torch.empty((N, K), dtype=torch.float32, device=qweight.device)
+    with _outputs_of(stream):
+        W = torch.empty((N, K), dtype=torch.float32, device=qweight.device)
     _check(lib().fbq_dequant(_ptr(qweight), _ptr(scales), _ptr(zeros), _ptr(W), N, K, group, bits,
                              _stream(stream)), "fbq_dequant")
     return W
@@ -204,10 +219,11 @@ def quantize_feedback(W, A, B, group: int, bits: int, want_wf: bool = False, str
     N, K = W.shape
     rank = 0 if A is None else A.shape[0]
     bf16 = 1 if (A is not None and A.dtype == torch.bfloat16) else 0
-    codes = torch.empty((N, K), dtype=torch.uint8, device=W.device)
-    scales = torch.empty((N, K // group), dtype=torch.float16, device=W.device)
-    zeros = torch.empty((N, K // group), dtype=torch.float16, device=W.device)
-    wf = torch.empty((N, K), dtype=torch.float32, device=W.device) if want_wf else None
+    with _outputs_of(stream):
+        codes = torch.empty((N, K), dtype=torch.uint8, device=W.device)
+        scales = torch.empty((N, K // group), dtype=torch.float16, device=W.device)
+        zeros = torch.empty((N, K // group), dtype=torch.float16, device=W.device)
+        wf = torch.empty((N, K), dtype=torch.float32, device=W.device) if want_wf else None
     _check(lib().fbq_quantize_feedback(_ptr(W), _ptr(A), _ptr(B), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(wf),
                                        N, K, group, bits, rank, bf16, _stream(stream)), "fbq_quantize_feedback")
     return codes, scales, zeros, wf
@@ -218,7 +234,8 @@ def gram(X, stream=None):
     import torch
     assert X.is_cuda and X.dtype == torch.float32 and X.is_contiguous()
     T, K = X.shape
-    H = torch.empty((K, K), dtype=torch.float32, device=X.device)
+    with _outputs_of(stream):
+        H = torch.empty((K, K), dtype=torch.float32, device=X.device)
     _check(lib().fbq_gram(_ptr(X), _ptr(H), T, K, _stream(stream)), "fbq_gram")
     return H
 
@@ -232,10 +249,11 @@ def reconstruct_step(W, H, A, B, lr: float, group: int, bits: int, workspace=Non
     for t in (W, H, A, B):
         assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous()
     need = int(lib().fbq_reconstruct_workspace_floats(N, K, rank))
-    if workspace is None or workspace.numel() < need:
-        workspace = torch.empty(need, dtype=torch.float32, device=W.device)
-    if loss is None:
-        loss = torch.zeros(1, dtype=torch.float32, device=W.device)
+    with _outputs_of(stream):
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(need, dtype=torch.float32, device=W.device)
+        if loss is None:
+            loss = torch.zeros(1, dtype=torch.float32, device=W.device)
     _check(lib().fbq_reconstruct_step(_ptr(W), _ptr(H), _ptr(A), _ptr(B), float(lr), _ptr(loss), _ptr(workspace), N, K,
                                       group, bits, rank, _stream(stream)), "fbq_reconstruct_step")
     return loss, workspace
@@ -300,10 +318,11 @@ def gated_layer(gate, up, group: int, bits: int, stream=None):
     if ranks[0] != ranks[1]:
         raise ValueError("both branches have one rank, got %d and %d" % tuple(ranks))
     r = ranks[0]
-    q = torch.empty(packed_words(2 * F, K, bits), dtype=torch.int32, device=dev)
-    s, z = (torch.empty((2 * F, K // group), dtype=torch.float16, device=dev) for _ in range(2))
-    A = torch.empty((2 * r, K), dtype=act, device=dev) if r else None
-    B = torch.empty((2 * F, 2 * r), dtype=act, device=dev) if r else None
+    with _outputs_of(stream):
+        q = torch.empty(packed_words(2 * F, K, bits), dtype=torch.int32, device=dev)
+        s, z = (torch.empty((2 * F, K // group), dtype=torch.float16, device=dev) for _ in range(2))
+        A = torch.empty((2 * r, K), dtype=act, device=dev) if r else None
+        B = torch.empty((2 * F, 2 * r), dtype=act, device=dev) if r else None
     _check(lib().fbq_gated_layer(*(_ptr(t) for t in (*gate, *up, q, s, z, A, B)), F, K, group, bits, r, _stream(stream)), "fbq_gated_layer")
     return q, s, z, A, B
 

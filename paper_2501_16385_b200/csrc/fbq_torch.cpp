@@ -7,6 +7,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <initializer_list>
@@ -43,6 +44,20 @@ bool stream_of(PyObject *o, void **out)
     Py_DECREF(h);
     return !PyErr_Occurred();
 }
+
+// While it lives new tensors are memory of `stream`, on which the call will write them, also where another stream is current: a block of that
+// one's may still be written by work that it has queued, and one that is dropped goes back to those whose work is in order with the call.
+class OutputsOf {
+    c10::cuda::OptionalCUDAStreamGuard guard;
+
+public:
+    explicit OutputsOf(void *stream)
+    {
+        const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream();
+        if (static_cast<void *>(current.stream()) != stream)
+            guard.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), current.device_index()));
+    }
+};
 
 // linear(x, qweight, scales, zeros, A, B, N, group, bits, y, stream) -> y, or the error code of the call
 PyObject *py_linear(PyObject *, PyObject *const *v, Py_ssize_t n)
@@ -83,6 +98,7 @@ PyObject *py_linear(PyObject *, PyObject *const *v, Py_ssize_t n)
         if (!stream_of(v[10], &stream)) return nullptr;
         PyObject *y;
         if (v[9] == Py_None) {
+            const OutputsOf there(stream);
             y = THPVariable_Wrap(at::empty({M, (int64_t)N}, x.options()));
             if (!y) return nullptr;
         } else {
@@ -187,7 +203,7 @@ int size_arg(int64_t n)
 }
 int64_t groups_of(int64_t columns) { return (columns + 127) / 128; }
 
-// A new tensor on the current device, without the dispatcher's detours.
+// A new tensor of the current device and stream (OutputsOf), without the dispatcher's detours: 0.5 us less, and dispatch modes do not see it.
 at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type) { return at::Tensor(at::detail::empty_cuda(shape, type, at::Device(at::kCUDA), std::nullopt)); }
 
 struct Layer {
@@ -273,6 +289,7 @@ PyObject *py_gated(PyObject *, PyObject *const *v, Py_ssize_t n)
         void *px = operand(v[0], "x", act, {M, K});
         const Layer l = layer_of(v + 1, N, K, group, bits, act);
         void *stream = stream_arg(v[12]);
+        const OutputsOf there(stream);
         at::Tensor h, codes, scales;
         if (v[11] == Py_None) {
             h = fresh({M, N / 2}, act);
@@ -302,6 +319,7 @@ PyObject *py_act8_pack(PyObject *, PyObject *const *v, Py_ssize_t n)
         const at::ScalarType act = act_type(x, "x");
         const int64_t M = x.size(0), K = x.size(1);
         void *px = operand(v[0], "x", act, {M, K}), *stream = stream_arg(v[1]);
+        const OutputsOf there(stream);
         const at::Tensor codes = fresh({M, K}, at::kChar), scales = fresh({M, groups_of(K)}, at::kFloat);
         const int m = size_arg(M), k = size_arg(K);
         const int rc = without_gil([&] { return fbq_act8_pack(px, (int8_t *)codes.data_ptr(), (float *)scales.data_ptr(), m, k, act == at::kBFloat16, stream); });
@@ -318,6 +336,7 @@ PyObject *py_act8_unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
         void *pc = operand(v[0], "codes", at::kChar, {M, K}), *ps = operand(v[1], "scales", at::kFloat, {M, groups_of(K)});
         const bool bf16 = PyObject_IsTrue(v[2]) == 1;
         void *stream = stream_arg(v[3]);
+        const OutputsOf there(stream);
         const at::Tensor x = fresh({M, K}, bf16 ? at::kBFloat16 : at::kHalf);
         const int m = size_arg(M), k = size_arg(K);
         const int rc = without_gil([&] { return fbq_act8_unpack((const int8_t *)pc, (const float *)ps, x.data_ptr(), m, k, bf16, stream); });
@@ -350,6 +369,7 @@ PyObject *py_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
             x = operand(v[4], "x", act, {M, K});
         }
         void *stream = stream_arg(v[16]);
+        const OutputsOf there(stream);
         at::Tensor dx, dA, dB;
         if (want_dx) dx = fresh({M, K}, act);
         if (want_factors && l.rank > 0) {
