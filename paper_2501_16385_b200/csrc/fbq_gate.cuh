@@ -15,14 +15,15 @@ constexpr int kGateUp = 8;
 constexpr float kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282143484f;     // 2 sqrt(2/pi), times 0.044715
 __device__ __forceinline__ float gate_arg(int fn, float v) { return fn == FBQ_GATE_GELU ? v * fmaf(kGelu3, v * v, kGelu1) : v; }
 __device__ __forceinline__ float gate_value(int fn, float v) { return __fdividef(v, 1.f + __expf(-gate_arg(fn, v))); }
-// f(v) and f'(v) = S + v S (1 - S) z'.  Beyond |v| = 32 the second term is 0 in single precision for both functions (S (1 - S) <= e^-32,
-// times v z'), and for GELU its factors would be 0 and infinite.
+// f(v) and f'(v) = S + v S (1 - S) z'.  Above v = 32 the second term is below the last place of S in single precision for both functions (1 - S <= e^-32,
+// times v z'), and it is left out: GELU's z' and an f that is infinite would make NaN of it.  Below -32 it is the larger one of SiLU's, |v| times S, and GELU has neither: S is 0, and
+// z' may be infinite.
 __device__ __forceinline__ void gate_both(int fn, float v, float &f, float &df)
 {
     const float s = __fdividef(1.f, 1.f + __expf(-gate_arg(fn, v)));
     const float dz = fn == FBQ_GATE_GELU ? fmaf(3.f * kGelu3, v * v, kGelu1) : 1.f;
     f = v * s;
-    df = fabsf(v) > 32.f ? s : fmaf(f * (1.f - s), dz, s);
+    df = (fn == FBQ_GATE_GELU ? fabsf(v) : v) > 32.f ? s : fmaf(f * (1.f - s), dz, s);
 }
 
 // Eight bits: kKeptGroup consecutive columns of a row share a scale.  scale = max|v| / 127, code = rint(v * (127 / max|v|)), each step
