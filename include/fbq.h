@@ -294,9 +294,9 @@ int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void 
  * (four launches at most; t and the dequantised weights are rounded once to the activation type, as in the prompts' kernels).
  * "gemv" = 0 and "force_kernel" >= 0 leave the fewest tokens to the others too.
  *   kept, kept_scales   NULL, or what the backward pass needs of p in 8 bits: codes [M][N] and one scale per 128 columns of a row,
- *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M up to 512 (900 of wide layers) run on
- *       the kernel that shares products out, of more on the prompts' dense kernel (scratch: a 16-bit copy of the weights, up to 512 MB per stream, which they
- *       cannot do without).
+ *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M up to 512 (900 of wide layers; any M where K is
+ *       above 2^20) run on the kernel that shares products out, of more on the prompts' dense kernel (scratch: a 16-bit copy of the weights, up to 512 MB per
+ *       stream, which they cannot do without: FBQ_ERR_CUDA where device memory is used up, FBQ_ERR_UNSUPPORTED where a capture would have to grow it).
  * Scratch of the sharing kernel: its sums (up to 29 MB), M x rank values of 16 bits, and partial sums of those; it grows as described at
  * fbq_linear, a call that would grow it during a capture returns FBQ_ERR_UNSUPPORTED and queues nothing, and graphs captured on one stream
  * share it: replay them one after another. */

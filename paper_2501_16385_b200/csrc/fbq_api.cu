@@ -333,6 +333,7 @@ constexpr int kEvenAnyGated = 512, kEvenMostGated = 900;
 bool gated_even_takes(const LinearArgs &a)
 {
     const long long tiles = (long long)((a.N + 127) / 128) * ((a.M + 255) / 256);
+    if (a.kept && !dense_has_room(a.N, a.K)) return true;        // (layers of K above 2^20)
     if (a.M > kEvenAnyGated) return a.M <= kEvenMostGated && tiles > 2 * 2 * 74;
     return a.kept || tiles > 148;
 }

@@ -216,6 +216,7 @@ void dense_workspace_need(const LinearArgs &a, size_t *w16_bytes, size_t *tags, 
 cudaError_t launch_dense(const LinearArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);
 
 bool prefill_supported(const LinearArgs &a);
+bool dense_has_room(int N, int K);             // a tile's rows of W16 fit its scratch (fbq_dense.cu)
 bool prefill_dense(const LinearArgs &a);       // the dense kernel is the faster one for this call (fbq_dense.cu)
 void prefill_workspace_need(const LinearArgs &a, int *counters, size_t *t_floats, size_t *partial_floats);
 // dense: by the dense kernel, whose scratch (dense_workspace_need) is there

@@ -824,6 +824,8 @@ bool prefill_dense(const LinearArgs &a)
     return nft * ((a.M + tok - 1) / tok) > 3 * pairs_of_device();
 }
 
+bool dense_has_room(int N, int K) { return launch_rows(N, K) > 0; }
+
 void dense_workspace_need(const LinearArgs &a, size_t *w16_bytes, size_t *tags, size_t *t_floats)
 {
     const size_t rows = launch_rows(a.N, a.K), nft = (rows + kFeat - 1) / kFeat, nkc = (a.K + kItemK - 1) / kItemK;
@@ -835,6 +837,7 @@ void dense_workspace_need(const LinearArgs &a, size_t *w16_bytes, size_t *tags, 
 cudaError_t launch_dense(const LinearArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches)
 {
     const int rows = launch_rows(a.N, a.K);
+    if (rows == 0) return cudaErrorInvalidConfiguration;
     cudaError_t e = cudaSuccess;
     for (int n0 = 0; n0 < a.N && e == cudaSuccess; n0 += rows) {          // (each makes t anew: rank of `rows` of its operations)
         LinearArgs c = a;
