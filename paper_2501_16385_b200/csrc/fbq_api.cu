@@ -320,9 +320,9 @@ int gated_kernel(const LinearArgs &a)
 //   11008 <- 4096        37 /  71   60 / 110  84 / 121 107 / 125 126 / 126 141 / 130 184 / 150
 //   4096 <- 4096         25 /  49   35 /  51  44 /  55  54 /  57  65 /  59  73 /  60  87 / 108
 // so up to 768 tokens; above, where the dense kernel's tiles (256 x 256 on 74 pairs) leave most of a wave empty (4096 <- 2 x 11008 at 1280), it
-// is the dense kernel's all the same.
+// is the dense kernel's all the same, but for layers that its scratch has no room for (N above 2^20).
 constexpr int kEvenMost = 768;
-bool even_takes(int M) { return M <= kEvenMost; }
+bool even_takes(const GradArgs &g) { return g.M <= kEvenMost || !grad_dense_has_room(g.N, g.K); }
 // Gated blocks, this / the kernel that dequantises per tile (128 rows x up to 256 tokens, K cut where they are few) or the dense one:
 //                        77 tokens    256       320       512       640       768       900       1024
 //   4096 -> 2 x 11008    40 / 60    68 / 74   73 / 105 105 / 127 128 / 144 144 / 154 173 / 186 195 / 183
@@ -522,7 +522,7 @@ int run_backward(Backward &b, cudaStream_t s)
         need += padded256(bytes);
         return at;
     };
-    const bool even = even_takes(g.M), thin_first = g.rank > 0 && (even || grad_thin_first(g));
+    const bool even = even_takes(g), thin_first = g.rank > 0 && (even || grad_thin_first(g));
     ThinArgs t{};
     t.M = g.M; t.N = g.N; t.K = g.K; t.rank = g.rank; t.bf16 = g.bf16;
     t.s = ws.get();                                              // (any address: where it will be is not known yet)

@@ -14,6 +14,7 @@ namespace fbq {
 
 constexpr int kGroupFast = 128;   // group size of the decode / prefill kernels (Section 5.1)
 constexpr int kMaxRank = 256;
+constexpr int kMostGradRows = 1 << 21;           // N of a backward pass
 constexpr int kMostSide = 1 << 30;               // rows or columns of a layer, for calls that count whole tiles of them in 31 bits
 constexpr int kDecodeMaxM = 16, kDecodePreferM = 6;
 
@@ -180,6 +181,7 @@ struct GradArgs {
     bool bf16;
 };
 bool grad_thin_first(const GradArgs &a);        // s and t are better made by launch_thin
+bool grad_dense_has_room(int N, int K);         // a tile's columns of W16 fit its scratch
 bool grad_supported(int M, int N, int K, int group, int rank);
 void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags);
 cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches);

@@ -878,8 +878,9 @@ bool grad_thin_first(const GradArgs &a)
 
 bool grad_supported(int M, int N, int K, int group, int rank)
 {
-    return group == kGroupFast && K % kGroupFast == 0 && N % 8 == 0 && rank % 8 == 0 && rank <= kMaxRank && M <= (1 << 22) && K <= kMostSide && launch_columns(N, K) > 0;
+    return group == kGroupFast && K % kGroupFast == 0 && N % 8 == 0 && rank % 8 == 0 && rank <= kMaxRank && M <= (1 << 22) && K <= kMostSide && N <= kMostGradRows;
 }
+bool grad_dense_has_room(int N, int K) { return launch_columns(N, K) > 0; }
 
 void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags)
 {
@@ -891,6 +892,7 @@ void grad_workspace_need(const GradArgs &a, size_t *w16_bytes, size_t *tags)
 cudaError_t launch_grad(const GradArgs &a, Workspace &ws, const PrefillTuning &tune, cudaStream_t s, int *launches)
 {
     const int cols = launch_columns(a.N, a.K);
+    if (cols == 0) return cudaErrorInvalidConfiguration;
     cudaError_t e = cudaSuccess;
     for (int k = 0; k < a.K && e == cudaSuccess; k += cols) {
         const int n = std::min(cols, a.K - k);
