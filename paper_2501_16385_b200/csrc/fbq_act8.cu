@@ -192,20 +192,27 @@ unsigned blocks_for(long long n, int per) { return (unsigned)((n + per - 1) / pe
 // Grids have 31 bits.
 bool fits(long long n, int per) { return n <= (long long)per * 0x7FFFFFFF; }
 
+// A launch whose status is its own (the runtime's last error may be another call's).
+template <typename... P, typename... A> cudaError_t launch(void (*kern)(P...), unsigned grid, cudaStream_t s, A... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kThr);
+    cfg.stream = s;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
 // `go` with the number of units in 32 bits where they and what a block may count beyond them fit, else in 64.
 template <typename F> cudaError_t by_size(long long units, int per_block, F go)
 {
     if (!fits(units, per_block)) return cudaErrorInvalidConfiguration;
     const unsigned grid = blocks_for(units, per_block);
-    if (units < (1ll << 31)) go((unsigned)units, grid);
-    else go(units, grid);
-    return cudaGetLastError();
+    return units < (1ll << 31) ? go((unsigned)units, grid) : go(units, grid);
 }
 template <typename T, int EACH, bool WIDE> cudaError_t pack_by(const void *x, int8_t *codes, float *scales, int M, int K, cudaStream_t s)
 {
     const int G = groups_of(K);
     return by_size((long long)M * G, kTwice * (kThr * EACH / kKeptGroup), [&](auto groups, unsigned grid) {
-        pack_kernel<T, EACH, WIDE, decltype(groups)><<<grid, kThr, 0, s>>>(static_cast<const T *>(x), codes, scales, groups, K, G);
+        return launch(pack_kernel<T, EACH, WIDE, decltype(groups)>, grid, s, static_cast<const T *>(x), codes, scales, groups, K, G);
     });
 }
 template <typename T> cudaError_t pack(const void *x, int8_t *codes, float *scales, int M, int K, cudaStream_t s)
@@ -217,7 +224,7 @@ template <typename T> cudaError_t pack(const void *x, int8_t *codes, float *scal
 template <typename T, int EACH> cudaError_t unpack_by(const int8_t *codes, const float *scales, void *x, int M, int K, cudaStream_t s)
 {
     return by_size((long long)M * (K / EACH), kTwice * kThr, [&](auto units, unsigned grid) {
-        unpack_kernel<T, EACH, decltype(units)><<<grid, kThr, 0, s>>>(codes, scales, static_cast<T *>(x), units, K, groups_of(K));
+        return launch(unpack_kernel<T, EACH, decltype(units)>, grid, s, codes, scales, static_cast<T *>(x), units, K, groups_of(K));
     });
 }
 template <typename T> cudaError_t unpack(const int8_t *codes, const float *scales, void *x, int M, int K, cudaStream_t s)
@@ -243,10 +250,11 @@ cudaError_t launch_gate_grad(const void *dh, const int8_t *codes, const float *s
     const int per = N / 16, G = groups_of(N);
     return by_size((long long)M * per, kTwice * kThr, [&](auto units, unsigned grid) {
         using I = decltype(units);
-        if (bf16)
-            gate_grad_kernel<__nv_bfloat16, I><<<grid, kThr, 0, s>>>(static_cast<const __nv_bfloat16 *>(dh), codes, scales, static_cast<__nv_bfloat16 *>(dp), units, (I)per, G, fn);
-        else
-            gate_grad_kernel<__half, I><<<grid, kThr, 0, s>>>(static_cast<const __half *>(dh), codes, scales, static_cast<__half *>(dp), units, (I)per, G, fn);
+        auto go = [&](auto type) {
+            using T = decltype(type);
+            return launch(gate_grad_kernel<T, I>, grid, s, static_cast<const T *>(dh), codes, scales, static_cast<T *>(dp), units, per, G, fn);
+        };
+        return bf16 ? go(__nv_bfloat16{}) : go(__half{});
     });
 }
 
@@ -258,8 +266,7 @@ cudaError_t launch_interleave(const void *gate, const void *up, void *out, int F
         const int units = (int)(bytes / sizeof(P));
         const long long total = 2ll * F * (padded ? 2 : 1) * units;
         if (!fits(total, kThr)) return cudaErrorInvalidConfiguration;
-        interleave_kernel<P><<<blocks_for(total, kThr), kThr, 0, s>>>(static_cast<const P *>(gate), static_cast<const P *>(up), static_cast<P *>(out), total, units, padded);
-        return cudaGetLastError();
+        return launch(interleave_kernel<P>, blocks_for(total, kThr), s, static_cast<const P *>(gate), static_cast<const P *>(up), static_cast<P *>(out), total, units, padded);
     };
     if (bytes % 16 == 0) return go(uint4{});
     if (bytes % 4 == 0) return go(uint32_t{});

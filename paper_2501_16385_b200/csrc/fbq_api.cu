@@ -174,27 +174,32 @@ int select_kernel(int M, int N, int K, int group, int bits, int rank, bool bf16)
 
 // Grows a device buffer; zero-fills it on `s` (the invariants of the decode
 // kernel's scratch space start from zero).  The old buffer is released only
-// after the stream has drained.
+// after the stream has drained.  What fails is told by the return value alone: the runtime's last error is cleared, or the next launch of this host
+// thread, anybody's, would be told of it.
 template <typename P>
 cudaError_t grow(P *&ptr, size_t &have, size_t need, size_t elem, cudaStream_t s)
 {
     if (need <= have) return cudaSuccess;
+    auto failed = [](cudaError_t e) {
+        (void)cudaGetLastError();
+        return e;
+    };
     cudaError_t e;
     // Allocating (and, for a buffer that exists, synchronising and freeing) is illegal while `s` is being
     // captured into a graph, and a graph captured earlier would keep the old pointers: refuse instead.
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     if (cudaStreamIsCapturing(s, &cap) == cudaSuccess && cap != cudaStreamCaptureStatusNone) return cudaErrorStreamCaptureUnsupported;
     if (ptr) {
-        if ((e = cudaStreamSynchronize(s)) != cudaSuccess) return e;
-        if ((e = cudaFree(ptr)) != cudaSuccess) return e;
+        if ((e = cudaStreamSynchronize(s)) != cudaSuccess) return failed(e);
+        if ((e = cudaFree(ptr)) != cudaSuccess) return failed(e);
         ptr = nullptr;
         have = 0;
     }
     void *q = nullptr;
-    if ((e = cudaMalloc(&q, need * elem)) != cudaSuccess) return e;
+    if ((e = cudaMalloc(&q, need * elem)) != cudaSuccess) return failed(e);
     if ((e = cudaMemsetAsync(q, 0, need * elem, s)) != cudaSuccess) {
         cudaFree(q);
-        return e;
+        return failed(e);
     }
     ptr = static_cast<P *>(q);
     have = need;
@@ -470,8 +475,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
             ws->w16 = w16;
             if (e == cudaSuccess) e = grow(ws->tags, ws->n_tags, need_tags, sizeof(uint32_t), s);
             dense = e == cudaSuccess;
-            if (e == cudaErrorMemoryAllocation) (void)cudaGetLastError();
-            else if (!dense && e != cudaErrorStreamCaptureUnsupported) return FBQ_ERR_CUDA;
+            if (!dense && e != cudaErrorMemoryAllocation && e != cudaErrorStreamCaptureUnsupported) return FBQ_ERR_CUDA;
             if (!dense && a.kept) return grow_status(e);
             if (dense) need_t = std::max(need_t, tf);
         }
@@ -609,7 +613,6 @@ int with_scratch(N need, cudaStream_t s, F f, void *spare = nullptr, size_t spar
             g_launches += launches;
             return rc;
         }
-        (void)cudaGetLastError();
         if (e != cudaErrorMemoryAllocation) return FBQ_ERR_CUDA;
     }
     if (need(0) <= spare_bytes) rc = f(0, spare, status, &launches);
