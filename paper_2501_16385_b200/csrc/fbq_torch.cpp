@@ -196,6 +196,12 @@ int int_arg(PyObject *o)
     if (v > 0x7FFFFFFF || v < -0x7FFFFFFFl) bad_value("a size does not fit 32 bits");
     return (int)v;
 }
+bool bool_arg(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw BadOperand();                               // (what has no truth value: a tensor of several elements, say)
+    return v != 0;
+}
 int size_arg(int64_t n)
 {
     if (n > 0x7FFFFFFF) bad_value("a size does not fit 31 bits");
@@ -284,7 +290,7 @@ PyObject *py_gated(PyObject *, PyObject *const *v, Py_ssize_t n)
         const at::ScalarType act = act_type(x, "x");
         const int64_t M = x.size(0), K = x.size(1);
         const int N = int_arg(v[6]), group = int_arg(v[7]), bits = int_arg(v[8]), gate = int_arg(v[9]);
-        const bool save = PyObject_IsTrue(v[10]) == 1;
+        const bool save = bool_arg(v[10]);
         if (N < 2) bad_value("N must be positive");
         void *px = operand(v[0], "x", act, {M, K});
         const Layer l = layer_of(v + 1, N, K, group, bits, act);
@@ -334,7 +340,7 @@ PyObject *py_act8_unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
         const at::Tensor &codes = tensor_of(v[0], "codes", 2);
         const int64_t M = codes.size(0), K = codes.size(1);
         void *pc = operand(v[0], "codes", at::kChar, {M, K}), *ps = operand(v[1], "scales", at::kFloat, {M, groups_of(K)});
-        const bool bf16 = PyObject_IsTrue(v[2]) == 1;
+        const bool bf16 = bool_arg(v[2]);
         void *stream = stream_arg(v[3]);
         const OutputsOf there(stream);
         const at::Tensor x = fresh({M, K}, bf16 ? at::kBFloat16 : at::kHalf);
@@ -349,7 +355,7 @@ PyObject *py_act8_unpack(PyObject *, PyObject *const *v, Py_ssize_t n)
 PyObject *py_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
 {
     return guarded(n, 17, [&]() -> PyObject * {
-        const bool gated = PyObject_IsTrue(v[0]) == 1, want_dx = PyObject_IsTrue(v[14]) == 1, want_factors = PyObject_IsTrue(v[15]) == 1;
+        const bool gated = bool_arg(v[0]), want_dx = bool_arg(v[14]), want_factors = bool_arg(v[15]);
         const char *what = gated ? "dh" : "dy";
         const at::Tensor &dy = tensor_of(v[1], what, 2);
         const at::ScalarType act = act_type(dy, what);
