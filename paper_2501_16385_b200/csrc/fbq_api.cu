@@ -339,8 +339,8 @@ bool gated_even_takes(const LinearArgs &a)
 {
     const long long tiles = (long long)((a.N + 127) / 128) * ((a.M + 255) / 256);
     if (a.kept && !dense_has_room(a.N, a.K)) return true;        // (layers of K above 2^20)
-    if (a.M > kEvenAnyGated) return a.M <= kEvenMostGated && tiles > 2 * 2 * 74;
-    return a.kept || tiles > 148;
+    if (a.M > kEvenAnyGated) return a.M <= kEvenMostGated && tiles > 4 * (sms_of_device() / 2);      // (two waves of pairs, of two of these tiles each)
+    return a.kept || tiles > sms_of_device();
 }
 size_t padded256(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t thin_bytes(int M, int rank) { return padded256((size_t)M * ((rank + 63) / 64 * 64) * 2); }

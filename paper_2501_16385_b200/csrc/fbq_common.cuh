@@ -32,6 +32,18 @@ public:
     void set() { on.fetch_or(bit(), std::memory_order_relaxed); }
 };
 
+// SMs of the current device (a B200's where there is none to ask), asked for once on each.
+inline int sms_of_device()
+{
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 // Activation-type helpers ---------------------------------------------------
 template <typename T> struct ActTraits;
 template <> struct ActTraits<__half> {

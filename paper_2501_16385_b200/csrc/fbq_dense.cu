@@ -130,11 +130,6 @@ __device__ __forceinline__ void store_v8(void *p, const uint32_t *v)
                  : "memory");
 }
 
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c0), "r"(c1), "r"(src) : "memory");
-}
-
 // Whole warp: every lane looks (`there`, an acquiring load) until the first `group` lanes see what they wait for; returns how
 // many whole groups of lanes do from there on, or 0 when the bound is hit.  Votes order no memory: the warp barrier carries
 // what the lanes have acquired to the one lane that issues the copies.
@@ -635,16 +630,7 @@ dense_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ C
 constexpr CUtensorMapDataType dt = CU_TENSOR_MAP_DATA_TYPE_UINT16;
 constexpr CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
 
-int pairs_of_device()
-{
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0, sms = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
-        n = std::max(1, sms / 2);
-    }
-    return n;
-}
+int pairs_of_device() { return std::max(1, sms_of_device() / 2); }
 
 // Token tiles: a wave of tiles takes 2 cycles per token column and K element (never less than the copies of the weight
 // operand take) plus what a tile costs besides, so among the tile widths that M can be cut into the one with the least

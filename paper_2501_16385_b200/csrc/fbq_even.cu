@@ -97,10 +97,6 @@ __device__ __forceinline__ void sts128(uint32_t addr, const uint32_t *v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c0), "r"(c1), "r"(src) : "memory");
-}
 __device__ __forceinline__ uint32_t ldg_u16(const __half *p)
 {
     uint32_t v;
@@ -622,15 +618,6 @@ template <typename T, int MODE> __global__ void __launch_bounds__(kFeat) add_ker
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-int sms_of_device()
-{
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
-    }
-    return n;
-}
 // Tokens of a tile: all of them up to kMostTok, else equal parts, in sixteens.
 void token_tiles(int M, int *tok, int *ntt)
 {

@@ -185,15 +185,6 @@ template <typename T> __global__ void __launch_bounds__(256) factor_add_kernel(c
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
-int sms_of_device()
-{
-    static int n = 0;
-    if (n == 0) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
-    }
-    return n;
-}
 void plan(FactorParams &p)
 {
     p.rank_pad = (p.rank + 63) / 64 * 64;
