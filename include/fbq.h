@@ -131,6 +131,8 @@ int fbq_dequant(const uint32_t *qweight, const uint16_t *scales, const uint16_t 
  * required: where it cannot be had, in a capture or because memory is used up, the prefill kernel that
  * does without it runs, with the same rounding of weights and t.)  So: run
  * the largest shape of every kind once on a stream, outside capture, before capturing on it.
+ * A graph uses the scratch of the stream that it was captured on wherever it is replayed: its replays, those of other graphs
+ * captured there and calls on that stream must not run at the same time.
  * After FBQ_ERR_TIMEOUT the stream's counters are unfinished: call fbq_poll_status (it resets
  * them) before issuing more work on that stream. */
 int fbq_linear(const void *x, const uint32_t *qweight, const void *scales, const void *zeros,
@@ -315,7 +317,7 @@ int fbq_act8_unpack(const int8_t *codes, const float *scales, void *x, int M, in
  * dy [M][N], x and dx [M][K], dA [rank][K], dB [N][rank], all in the activation type (act_is_bf16).  x is given so or, with x == NULL, as
  * x8 [M][K] with x8_scales (fbq_act8_pack).  dx may be NULL, and dA and dB may both be (x then as well); rank == 0 has neither.
  * M == 0: dA and dB are set to zero.  Sums are fp32; s, t and the dequantised weights are rounded once to the activation type where they
- * become operands.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, N <= 2^21, K <= 2^30,
+ * become operands, and so is x of x8: in fp16 s and t are infinite above 65504 and lose bits below 2^-14, so scale the loss such that dy's products stay between.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, N <= 2^21, K <= 2^30,
  * M <= 2^22, rank <= 256; else FBQ_ERR_UNSUPPORTED.  Every pointer is 16-byte aligned; outputs overlap no input and not each other.
  * Scratch per stream: above 768 tokens a 16-bit copy of the weights (up to 512 MB; none where N is above 2^20), up to there the sums that
  * CTAs share (up to 29 MB); M x (2 rank, rounded up to 64) and, for x8, M x K values of 16 bits, and partial sums of s, t, dA and dB; it grows as described at fbq_linear, and a call that would grow it during a capture returns
@@ -326,7 +328,7 @@ int fbq_linear_backward(const void *dy, const void *x, const int8_t *x8, const f
 
 /* Backward pass of fbq_gated for dh [M][N/2], from the products it kept:
  *     dp[gate] = dh * p[up] * f'(p[gate]),   dp[up] = dh * f(p[gate])
- * (rounded once to the activation type, M x N more values of scratch), and from there as fbq_linear_backward with dy = dp, whose limits (N <= 2^21)
+ * (rounded once to the activation type, in fp16 to its range as well; M x N more values of scratch), and from there as fbq_linear_backward with dy = dp, whose limits (N <= 2^21)
  * hold beside those of the gated calls.  Where B holds
  * the other branch's zeros dB is 0, so that a step along it leaves them. */
 int fbq_gated_backward(const void *dh, const int8_t *kept, const float *kept_scales, const void *x, const int8_t *x8, const float *x8_scales,

@@ -1,8 +1,8 @@
 // Activations in 8 bits: the form in which a training step keeps them between its passes, and what the gated block's backward
 // pass makes of it.  All three kernels are bound by memory: one pass, 16 bytes a lane and access where rows allow, the lanes of a kernel with
 // two accesses each on their way, places in 32 bits where they fit (a division of 64 bits takes as long as the rest of a lane's work).
-// 4096 x 11008 bf16: pack 28.6 us (135 MB, 4.7 TB/s), unpack 25 (5.4 TB/s); dp of the gated block, 4096 x 22016, 67 us
-// (361 MB, 5.4 TB/s).
+// 4096 x 11008 bf16: pack 27.5 us (135 MB, 4.9 TB/s), unpack 27 (5.0 TB/s); dp of the gated block, 4096 x 22016, 67 us
+// (361 MB, 5.4 TB/s).  Rows of no whole pieces of eight (11004, 11007; a layer's are always whole) go value by value: 78 and 111 us.
 #include "fbq_common.cuh"
 #include "fbq_dequant.cuh"
 #include "fbq_gate.cuh"
@@ -59,7 +59,7 @@ __device__ __forceinline__ void pack_group(const T *src, const uint4 (&raw)[EACH
 }
 
 // 128 / EACH lanes take a group: the largest |v| crosses lanes once, codes and values do not.  WIDE: rows of whole units of EACH.  (Sixteen values a lane
-// share the scale's two divisions and take three steps across lanes: 28.6 us for 4096 x 11008, eight 37.)
+// share the scale's two divisions and take three steps across lanes: 27.5 us for 4096 x 11008; eight 33 for 4096 x 11000.)
 template <typename T, int EACH, bool WIDE, typename I>
 __global__ void __launch_bounds__(kThr) pack_kernel(const T *__restrict__ x, int8_t *__restrict__ codes, float *__restrict__ scales, I groups, int K, int G)
 {

@@ -324,8 +324,9 @@ int gated_kernel(const LinearArgs &a)
 //   2048 <- 2 x 5504     41 / 100   53 / 103  66 / 109  77 / 113  87 / 115  94 / 118 109 / 149
 //   11008 <- 4096        37 /  71   60 / 110  84 / 121 107 / 125 126 / 126 141 / 130 184 / 150
 //   4096 <- 4096         25 /  49   35 /  51  44 /  55  54 /  57  65 /  59  73 /  60  87 / 108
-// so up to 768 tokens; above, where the dense kernel's tiles (256 x 256 on 74 pairs) leave most of a wave empty (4096 <- 2 x 11008 at 1280), it
-// is the dense kernel's all the same, but for layers that its scratch has no room for (N above 2^20).
+// so up to 768 tokens, the last of these sizes at which this is ahead for all four layers.  Above, the dense kernel's tiles (256 x 256 on 74 pairs) fill their last wave or
+// leave most of it empty: at 1024 it is ahead by 8 to 22 % for three of them, at 1280 this by 24 to 37 %.  The rule goes by tokens alone, and all of those are the dense
+// kernel's, but for layers that its scratch has no room for (N above 2^20).
 constexpr int kEvenMost = 768;
 bool even_takes(const GradArgs &g) { return g.M <= kEvenMost || !grad_dense_has_room(g.N, g.K); }
 // Gated blocks, this / the kernel that dequantises per tile (128 rows x up to 256 tokens, K cut where they are few) or the dense one:

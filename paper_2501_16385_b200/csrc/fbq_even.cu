@@ -24,9 +24,12 @@
 // memory as it is (128 lanes x 32 columns a block; the multiplication reads it there and not from shared memory).  Grad, features are W's
 // columns, 128 of them one group; a pair of blocks is 128 rows of it, and the operand is MN-major in shared memory: rows are written as they lie.
 //
-// What bounds it: the chain of a pair, stage free -> operand written -> MMAs issued and done -> free, with the three pairs that fit on their way,
-// some 1000 cycles a pair at 77 tokens (INT3) and 1190 at 333 (Grad, tiles of 176), where the MMAs alone would take 320 and 700.  4096 -> 2 x 11008
-// at 77 tokens takes 30 us of a call's 40, 22016 -> 4096 (dx) at 333 tokens 66 of 100.  Of single things left out (for timing) none gives more than a
+// What bounds it: the chain of a pair, stage free -> operand written -> MMAs issued and done -> free, with the pairs that fit on their way: three at 77
+// tokens (six stages), two at 333 (Grad, tiles of 176: four stages).  From the times of layers of different depths (rank 0, both launches) a pair takes 0.50 us
+// at 77 tokens (INT3; 2048 to 16384 deep 23.7, 32.7, 52.3, 89.7), 990 cycles where its MMAs alone would take 320, and 0.78 us at 333 (5504 to 22016 deep 26.9,
+// 40.9, 55.4, 70.6), 1530 cycles where they would take 700; beyond that, codes and dy larger than L2, 0.97.  What is in no pair, the launch, the first pair's way
+// through the ring, the last one's epilogue and the adding launch, is 13 to 14 us of a call.  4096 -> 2 x 11008 at 77 tokens takes 30 us of a call's 39, 22016 -> 4096 (dx) at
+// 333 tokens 66 of 107.  Of single things left out (for timing) none gives more than a
 // tenth: dequantisation 8 %, three of four MMAs 9, x 1 (Grad 9), codes 1.  Earlier forms, us of the two calls: a warp that copies all of x, whose 40
 // instructions a block each wait their turn among 24 warps, 42.9 and 105; four groups of four warps, 128 codes a thread, 41.5 and 98; operands in shared
 // memory forward too, 41 and -; one block per look of the MMA warp, 43.5 and 98; 256 features a CTA, one and a half pairs on their way, 38 for the kernel
