@@ -1857,11 +1857,11 @@ template <int BITS, typename T, int MT, bool HEAVY, bool I8>
 cudaError_t launch_variant(const DecodeParams &p, const CUtensorMap &wmap, const Plan &pl, bool pdl, cudaStream_t s)
 {
     auto kern = decode_kernel<BITS, T, MT, HEAVY, I8>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
         if (e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(pl.n_t + pl.R * pl.SK));
@@ -1942,11 +1942,11 @@ template <int BITS, typename T, int MT, bool HEAVY, bool I8>
 cudaError_t launch_batch_variant(const DecodeBatch &b, size_t smem, bool pdl, cudaStream_t s)
 {
     auto kern = decode_batch_kernel<BITS, T, MT, HEAVY, I8>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
         if (e != cudaSuccess) return e;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)b.first[b.count]);

@@ -1473,12 +1473,12 @@ cudaError_t launch_gemv_batch(const LinearArgs *a, int count, Workspace &ws, con
         g.first_main[i] = g.n_t + main_ctas;
         main_ctas += g.p[i].n_main;
     }
-    auto launch = [&](auto kern, bool &attr_set) {
-        if (!attr_set) {
+    auto launch = [&](auto kern, PerDevice &attr_set) {
+        if (!attr_set.there()) {
             cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, (int)cudaSharedmemCarveoutMaxShared);
             if (e != cudaSuccess) return e;
-            attr_set = true;
+            attr_set.set();
         }
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3((unsigned)(g.n_t + main_ctas));
@@ -1499,7 +1499,7 @@ cudaError_t launch_gemv_batch(const LinearArgs *a, int count, Workspace &ws, con
     auto go = [&](auto bits, auto type) {
         using T = typename decltype(type)::type;
         constexpr int B = decltype(bits)::value;
-        static bool set[4] = {};
+        static PerDevice set[4];
         if (a[0].rank == 0) return a[0].M == 1 ? launch(gemv_batch_kernel<B, T, 1, false>, set[0]) : launch(gemv_batch_kernel<B, T, 2, false>, set[1]);
         return a[0].M == 1 ? launch(gemv_batch_kernel<B, T, 1, true>, set[2]) : launch(gemv_batch_kernel<B, T, 2, true>, set[3]);
     };

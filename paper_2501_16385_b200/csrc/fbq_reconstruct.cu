@@ -539,10 +539,10 @@ bool product(cudaStream_t s, const Operand &P, const Operand &Q, ProductParams p
     CUtensorMap pmap, qmap;
     if (operand_map(&pmap, P, 128) != cudaSuccess || operand_map(&qmap, Q, p.nt / 2) != cudaSuccess) return false;
     auto kern = product_kernel<MODE>;
-    static bool attr_set = false;
-    if (!attr_set) {
+    static PerDevice attr_set;
+    if (!attr_set.there()) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess) return false;
-        attr_set = true;
+        attr_set.set();
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(2 * std::min(pairs(), n_work)));
