@@ -108,12 +108,13 @@ int fbq_dequant(const uint32_t *qweight, const uint16_t *scales, const uint16_t 
  * Well formed means bits in {3,4}, group a multiple of 8 (4 bits) or 32
  * (3 bits) dividing K, rank >= 0.  Zero points are taken as stored: every kernel accepts
  * integer-valued fp16 zero points of either sign and beyond 2^bits - 1 (what fbq_quantize_feedback
- * produces for groups that do not straddle zero); the decode and generic kernels any fp16 value.
+ * produces for groups that do not straddle zero); the decode and generic kernels any fp16 value.  (The tensor-core kernels of prompts, gated
+ * blocks and backward passes hold q - z exactly for zero points from -3072 to 1024, in bf16 from -384 to 128, and rounded to the type beyond.)
  * Accumulation is fp32; t = x.A^T stays fp32 in the decode and
  * generic kernels (where a decode kernel multiplies it with B on tensor cores it enters as
  * two 16-bit terms, the rounded value and the remainder, two TF32 terms in the split kernel) and is rounded once to the activation
- * type in the prefill kernel (which also rounds the dequantised weights s*(q-z) once to that
- * type).  At M <= 2 the decode kernels read x in fixed point per group of 128, exact to 2^-17
+ * type in the prefill kernel (which also rounds the dequantised weights s*(q-z) to that
+ * type: fp16 once, bf16 the scale first and then the product).  At M <= 2 the decode kernels read x in fixed point per group of 128, exact to 2^-17
  * of the group's largest element; a group that holds an Inf or a NaN makes its token's outputs NaN.  The
  * split kernel reads x exactly (fp16 beside an |x| of 1024 and more, INT4 4096, of the same token: to 2^-19), and
  * an Inf or a NaN goes into the outputs as in the sum of products.  The other decode kernel's 16-bit form
@@ -293,7 +294,7 @@ int fbq_gated_layer(const uint32_t *gate_q, const void *gate_scales, const void 
  * once).  x, A, B, h: fp16 or bf16 (act_is_bf16).  At most 2 tokens run on the streaming kernel, 3 to 16 on the split kernel (layer rank up
  * to 128, and where fbq_split_plan has a plan for N rows), each in one launch; each computes p as it does for fbq_linear.  More tokens
  * run on the prompts' kernels, or up to 900 of a layer that makes many of their tiles on a kernel that shares the products out evenly
- * (four launches at most; t and the dequantised weights are rounded once to the activation type, as in the prompts' kernels).
+ * (four launches at most).  On both t and the dequantised weights are rounded once to the activation type.
  * "gemv" = 0 and "force_kernel" >= 0 leave the fewest tokens to the others too.
  *   kept, kept_scales   NULL, or what the backward pass needs of p in 8 bits: codes [M][N] and one scale per 128 columns of a row,
  *       [M][ceil(N/128)], as fbq_act8_pack would make them of p in single precision.  Such calls of any M up to 512 (900 of wide layers; any M where K is

@@ -278,9 +278,7 @@ __device__ __forceinline__ bool dequantise(const DenseParams &p, uint32_t tag, u
         uint32_t out[NP][16];
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
-            uint32_t d[16];
-            Dequant<BITS, T>::run(c.w[j], __half2float(c.s[j]), __half2float(c.z[j]), d);
-            natural_pairs<BITS>(d, out[j]);
+            DequantNatural<BITS, T, MODE != kLinear>::run(c.w[j], __half2float(c.s[j]), __half2float(c.z[j]), out[j]);
             if (j == 0 && done >= 0) announce(done);
             if (row + kPassRows * j >= p.N || k0 >= p.K) continue;
             T *dst = static_cast<T *>(p.w16) + (size_t)(row + kPassRows * j) * p.K + k0;

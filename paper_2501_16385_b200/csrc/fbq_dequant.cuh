@@ -99,10 +99,26 @@ template <int BITS> __device__ __forceinline__ constexpr int pair_hi(int p)
 }
 
 // s*(q - z) for 32 consecutive codes of one weight row (half a K block), as 16 packed pairs
-// in the order above.  q - z is exact (exponent trick, integer-valued z); the product is
+// in the order above.  q - z is exact (exponent trick, integer-valued z; bf16: |128 + z| up to 256); the product is
 // rounded once to the activation type.  w: 4 words (INT4) or one run of 3 words (INT3).
-template <int BITS, typename T> struct Dequant;
-template <> struct Dequant<4, __half> {
+//
+// bf16 holds 8 of an fp16 scale's 11 bits.  Without ONCE s is rounded to them first, the product after it; with ONCE s enters in two parts, s2 + lo:
+// (q - z) lo is exact, and the fma rounds the whole once.  That is one instruction a pair more; dx is then 0.0024 from 64 bits where it is 0.0028
+// else, h of a gated layer 0.0029 for 0.0037.  Gated blocks and backward passes take it: 0 to 1 % of a call, of the even kernel's INT3 calls 4 % (77
+// tokens 40.2 -> 42.0 us).  Prompts of a linear keep the results that they had (with it 4096 -> 11008 and back at 1024 tokens took 100 -> 103 and 82 -> 86 us).
+template <int BITS, typename T, bool ONCE = false> struct Dequant;
+template <bool ONCE> __device__ __forceinline__ uint32_t scale_rest(float s)
+{
+    if (!ONCE) return 0u;
+    const float rest = s - __bfloat162float(__float2bfloat16_rn(s));
+    return P2<__nv_bfloat16>::splat(rest == rest ? rest : 0.f);          // (an infinite scale has none)
+}
+template <bool ONCE> __device__ __forceinline__ uint32_t scaled(uint32_t d, uint32_t s2, uint32_t lo)
+{
+    using P = P2<__nv_bfloat16>;
+    return ONCE ? P::fma(d, s2, P::mul(d, lo)) : P::mul(d, s2);
+}
+template <bool ONCE> struct Dequant<4, __half, ONCE> {
     static __device__ __forceinline__ void run(const uint32_t *w, float s, float z, uint32_t *out)
     {
         const uint32_t c0 = P2<__half>::splat(1024.f + z), c1 = P2<__half>::splat(-(64.f + z)), s2 = P2<__half>::splat(s);
@@ -116,19 +132,19 @@ template <> struct Dequant<4, __half> {
         }
     }
 };
-template <> struct Dequant<4, __nv_bfloat16> {
+template <bool ONCE> struct Dequant<4, __nv_bfloat16, ONCE> {
     static __device__ __forceinline__ void run(const uint32_t *w, float s, float z, uint32_t *out)
     {
         using P = P2<__nv_bfloat16>;
-        const uint32_t c0 = P::splat(128.f + z), s2 = P::splat(s);   // 0x4300 | q is 128 + q in bf16
+        const uint32_t c0 = P::splat(128.f + z), s2 = P::splat(s), lo = scale_rest<ONCE>(s);   // 0x4300 | q is 128 + q in bf16
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                out[4 * i + e] = P::mul(P::sub(pf_lop3(w[i] >> (4 * e), 0x000F000Fu, 0x43004300u), c0), s2);
+                out[4 * i + e] = scaled<ONCE>(P::sub(pf_lop3(w[i] >> (4 * e), 0x000F000Fu, 0x43004300u), c0), s2, lo);
     }
 };
-template <> struct Dequant<3, __half> {
+template <bool ONCE> struct Dequant<3, __half, ONCE> {
     static __device__ __forceinline__ void run(const uint32_t *w, float s, float z, uint32_t *out)
     {
         using P = P2<__half>;
@@ -152,27 +168,27 @@ template <> struct Dequant<3, __half> {
         }
     }
 };
-template <> struct Dequant<3, __nv_bfloat16> {
+template <bool ONCE> struct Dequant<3, __nv_bfloat16, ONCE> {
     static __device__ __forceinline__ void run(const uint32_t *w, float s, float z, uint32_t *out)
     {
         using P = P2<__nv_bfloat16>;
-        const uint32_t c0 = P::splat(128.f + z), n1 = P::splat(-(16.f + z)), s2 = P::splat(s);
+        const uint32_t c0 = P::splat(128.f + z), n1 = P::splat(-(16.f + z)), s2 = P::splat(s), lo = scale_rest<ONCE>(s);
         {
             const uint32_t *v = w;
             uint32_t *o = out;
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
                 const uint32_t a = v[i], b = v[i] >> 6, c = v[i] >> 12;
-                o[5 * i + 0] = P::mul(P::sub(pf_lop3(a, 0x00070007u, 0x43004300u), c0), s2);
-                o[5 * i + 1] = P::mul(P::fma(pf_lop3(a, 0x00380038u, 0x43004300u), 0x3E003E00u, n1), s2);
-                o[5 * i + 2] = P::mul(P::sub(pf_lop3(b, 0x00070007u, 0x43004300u), c0), s2);
-                o[5 * i + 3] = P::mul(P::fma(pf_lop3(b, 0x00380038u, 0x43004300u), 0x3E003E00u, n1), s2);
-                o[5 * i + 4] = P::mul(P::sub(pf_lop3(c, 0x00070007u, 0x43004300u), c0), s2);
+                o[5 * i + 0] = scaled<ONCE>(P::sub(pf_lop3(a, 0x00070007u, 0x43004300u), c0), s2, lo);
+                o[5 * i + 1] = scaled<ONCE>(P::fma(pf_lop3(a, 0x00380038u, 0x43004300u), 0x3E003E00u, n1), s2, lo);
+                o[5 * i + 2] = scaled<ONCE>(P::sub(pf_lop3(b, 0x00070007u, 0x43004300u), c0), s2, lo);
+                o[5 * i + 3] = scaled<ONCE>(P::fma(pf_lop3(b, 0x00380038u, 0x43004300u), 0x3E003E00u, n1), s2, lo);
+                o[5 * i + 4] = scaled<ONCE>(P::sub(pf_lop3(c, 0x00070007u, 0x43004300u), c0), s2, lo);
             }
             uint32_t l = pf_lop3(v[0] >> 15, 0x00010001u, 0x43004300u);
             l = pf_lop3(v[1] >> 14, 0x00020002u, l);
             l = pf_lop3(v[2] >> 13, 0x00040004u, l);
-            o[15] = P::mul(P::sub(l, c0), s2);
+            o[15] = scaled<ONCE>(P::sub(l, c0), s2, lo);
         }
     }
 };
@@ -200,6 +216,32 @@ template <int BITS> __device__ __forceinline__ void natural_pairs(const uint32_t
         out[p] = pf_prmt(d[a], d[b], (hb ? 0x7600u : 0x5400u) | (ha ? 0x32u : 0x10u));
     }
 }
+
+// The 32 values in natural order, each rounded once where ONCE.
+template <int BITS, typename T, bool ONCE> struct DequantNatural {
+    static __device__ __forceinline__ void run(const uint32_t *w, float s, float z, uint32_t *out)
+    {
+        uint32_t d[16];
+        Dequant<BITS, T, ONCE>::run(w, s, z, d);
+        natural_pairs<BITS>(d, out);
+    }
+};
+// INT4 to bf16: neighbours are a byte's two halves, so a byte of the word and the same one of the word shifted by four are the pair as they are
+// put together (21 instructions a word with ONCE, where pairs (j, j + 4) put in order afterwards take 23).
+template <> struct DequantNatural<4, __nv_bfloat16, true> {
+    static __device__ __forceinline__ void run(const uint32_t *w, float s, float z, uint32_t *out)
+    {
+        using P = P2<__nv_bfloat16>;
+        const uint32_t c0 = P::splat(128.f + z), s2 = P::splat(s), lo = scale_rest<true>(s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t high = w[i] >> 4;
+#pragma unroll
+            for (uint32_t b = 0; b < 4; ++b)
+                out[4 * i + b] = scaled<true>(P::sub(pf_lop3(pf_prmt(w[i], high, b | (4u + b) << 8), 0x000F000Fu, 0x43004300u), c0), s2, lo);
+        }
+    }
+};
 
 template <typename T> __device__ __forceinline__ unsigned short to_bits16(float v)
 {

@@ -306,11 +306,9 @@ __device__ __forceinline__ bool dequantise(const EvenParams &p, int range, const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(rempty0 + 8u * slot);                 // (this warp has its codes in registers)
                 // (in registers before the stage is waited for)
-                uint32_t d[16], out[32];
-                Dequant<BITS, T>::run(c, fs, fz, d);
-                natural_pairs<BITS>(d, out);
-                Dequant<BITS, T>::run(c + NW, fs, fz, d);
-                natural_pairs<BITS>(d, out + 16);
+                uint32_t out[32];
+                DequantNatural<BITS, T, true>::run(c, fs, fz, out);
+                DequantNatural<BITS, T, true>::run(c + NW, fs, fz, out + 16);
                 const uint32_t stage = block ? s1 : s;
                 if (!free_stage(u + block)) return false;
                 if (copies) {

@@ -304,9 +304,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__
                     if (g >= 2 && !wait_looks(emptyb + 8u * b, ephase)) { dead = true; break; }
                     uint32_t wb[16];
                     if (row_ok) {
-                        uint32_t d[16];
-                        Dequant<BITS, T>::run(w[b], sc, ze, d);
-                        natural_pairs<BITS>(d, wb);
+                        DequantNatural<BITS, T, GATED>::run(w[b], sc, ze, wb);
                     } else {
 #pragma unroll
                         for (int c = 0; c < 16; ++c) wb[c] = 0u;
@@ -904,9 +902,7 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_const
                     if (i >= kStages && !wait_looks(empty0 + 8u * s, (uint32_t)(i / kStages - 1) & 1u)) { dead = true; break; }
                     uint32_t wb[16];
                     if (row_ok) {
-                        uint32_t d[16];
-                        Dequant<BITS, T>::run(w[b], sc, ze, d);
-                        natural_pairs<BITS>(d, wb);
+                        DequantNatural<BITS, T, false>::run(w[b], sc, ze, wb);
                     } else {
 #pragma unroll
                         for (int c = 0; c < 16; ++c) wb[c] = 0u;
