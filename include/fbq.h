@@ -121,8 +121,8 @@ int fbq_dequant(const uint32_t *qweight, const uint16_t *scales, const uint16_t 
  * (M >= 3) divides x by up to 16 (INT4) or 64 (INT3) in the activation type, which rounds fp16 below 2^-10 (2^-8), and
  * makes an Inf NaN.
  * Summation order is fixed for a given shape and grid size (results are
- * reproducible run to run), except for t in the other decode kernel at M >= 3, which is
- * accumulated with floating-point atomics.
+ * reproducible run to run), except for t in the other decode kernel (ranks that are no
+ * multiple of 16, say), which is accumulated with floating-point atomics.
  * Scratch and CUDA graphs: the library keeps scratch buffers per (device, stream) and grows them
  * the first time a stream sees a larger shape.  Growing allocates (and, for a buffer that exists,
  * synchronises the stream and frees the old one): a call that would have to grow scratch while
@@ -318,7 +318,8 @@ int fbq_act8_unpack(const int8_t *codes, const float *scales, void *x, int M, in
  * dy [M][N], x and dx [M][K], dA [rank][K], dB [N][rank], all in the activation type (act_is_bf16).  x is given so or, with x == NULL, as
  * x8 [M][K] with x8_scales (fbq_act8_pack).  dx may be NULL, and dA and dB may both be (x then as well); rank == 0 has neither.
  * M == 0: dA and dB are set to zero.  Sums are fp32; s, t and the dequantised weights are rounded once to the activation type where they
- * become operands, and so is x of x8: in fp16 s and t are infinite above 65504 and lose bits below 2^-14, so scale the loss such that dy's products stay between.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, N <= 2^21, K <= 2^30,
+ * become operands, and so is x of x8: in fp16 s and t are infinite above 65504 and lose bits below 2^-14, so scale the loss such that dy's
+ * products stay between.  The order of summation is fixed for a shape (no atomics).  Domain: group 128, N and rank multiples of 8, N <= 2^21, K <= 2^30,
  * M <= 2^22, rank <= 256; else FBQ_ERR_UNSUPPORTED.  Every pointer is 16-byte aligned; outputs overlap no input and not each other.
  * Scratch per stream: above 768 tokens a 16-bit copy of the weights (up to 512 MB; none where N is above 2^20), up to there the sums that
  * CTAs share (up to 29 MB); M x (2 rank, rounded up to 64) and, for x8, M x K values of 16 bits, and partial sums of s, t, dA and dB; it grows as described at fbq_linear, and a call that would grow it during a capture returns
