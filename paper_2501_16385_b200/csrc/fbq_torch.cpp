@@ -2,6 +2,7 @@
 // that a decode loop runs once per linear.  A linear at one token takes the GPU about five microseconds; marshalling
 // its fourteen arguments in Python and through ctypes took the host more than ten (4096 -> 4096, INT4, rank 32, call
 // after call: 15.2 us per call before, 4.2 us to issue and 5.7 us in all now).
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
@@ -119,8 +120,8 @@ PyObject *py_linear(PyObject *, PyObject *const *v, Py_ssize_t n)
         if (rc == FBQ_OK) return y;
         Py_DECREF(y);
         return PyLong_FromLong(rc);
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        torch::translate_exception_to_python(std::current_exception());   // (memory that is used up is torch.OutOfMemoryError)
         return nullptr;
     }
 }
@@ -246,8 +247,8 @@ template <typename F> PyObject *guarded(Py_ssize_t n, Py_ssize_t want, F f)
         return f();
     } catch (const BadOperand &) {
         return nullptr;
-    } catch (const std::exception &e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        torch::translate_exception_to_python(std::current_exception());   // (memory that is used up is torch.OutOfMemoryError)
         return nullptr;
     }
 }

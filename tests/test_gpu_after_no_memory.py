@@ -27,3 +27,16 @@ def test_small_calls_after_a_refused_one():
             got = call()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, w))
+
+
+def test_no_memory_for_results_is_torchs_error():
+    M, K, N, dt = 1024, 65536, 131072, torch.float16
+    x = torch.zeros((4 * M, K), dtype=dt, device="cuda")        # 537 MB; its codes are 268
+    layer = Layer(fbq, N, 256, 4, 0, dt, seed=1, gated=True)
+    few = torch.zeros((M, 256), dtype=dt, device="cuda")        # 134 MB of h, 268 of y
+    fbq.act8_pack(x[:8]), fbq.linear(few[:8], *layer.tensors, N, 128, 4)
+    with free_megabytes(fbq, 50):
+        for call in (lambda: fbq.act8_pack(x), lambda: fbq.gated(few, *layer.tensors, N, 128, 4), lambda: fbq.linear(few, *layer.tensors, N, 128, 4)):
+            with pytest.raises(torch.OutOfMemoryError):
+                call()
+        assert bool((fbq.act8_pack(few[:4])[0] == 0).all())
