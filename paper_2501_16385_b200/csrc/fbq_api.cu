@@ -174,7 +174,7 @@ int select_kernel(int M, int N, int K, int group, int bits, int rank, bool bf16)
 
 // Grows a device buffer; zero-fills it on `s` (the invariants of the decode
 // kernel's scratch space start from zero).  The old buffer is released only
-// after the stream has drained.  What fails is told by the return value alone: the runtime's last error is cleared, or the next launch of this host
+// after the stream has drained; where the new one cannot be had ptr and have are none, and must be seen to be by the next call, so they are the workspace's own.  What fails is told by the return value alone: the runtime's last error is cleared, or the next launch of this host
 // thread, anybody's, would be told of it.
 template <typename P>
 cudaError_t grow(P *&ptr, size_t &have, size_t need, size_t elem, cudaStream_t s)
@@ -248,14 +248,10 @@ int check_args(const LinearArgs &a)
 // One problem or several, for which there is a plan, in one launch of the split kernel.
 int run_split(const LinearArgs *a, int count, const GemvTuning &gt, Workspace *ws, cudaStream_t s)
 {
-    size_t have_c = (size_t)ws->n_counters;
     int launches = 0;
-    char *scratch = static_cast<char *>(ws->split);
-    cudaError_t e = grow(scratch, ws->split_bytes, split_scratch_bytes(a, count), 1, s);
-    ws->split = scratch;
+    cudaError_t e = grow(ws->split, ws->split_bytes, split_scratch_bytes(a, count), 1, s);
     if (e != cudaSuccess) return grow_status(e);
-    if ((e = grow(ws->counters, have_c, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-    ws->n_counters = (int)have_c;
+    if ((e = grow(ws->counters, ws->n_counters, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
     if (g_opt.test_split_launches != 0) {
         const unsigned long long launches_so_far = (unsigned long long)(unsigned)g_opt.test_split_launches << 32;
         g_opt.test_split_launches = 0;
@@ -300,11 +296,9 @@ int run_gemv_batch(const LinearArgs *a, int count, cudaStream_t s)
     int nc = 0, launches = 0;
     if (!batch_plan_exists(a, count, gt, &slots, &nc)) return FBQ_ERR_UNSUPPORTED;
     if (a[0].M > kGemvMaxM) return run_split(a, count, gt, ws.get(), s);
-    size_t have_c = (size_t)ws->n_counters;
     cudaError_t e;
     if ((e = grow(ws->tslots, ws->tslots_floats, slots, sizeof(float), s)) != cudaSuccess) return grow_status(e);
-    if ((e = grow(ws->counters, have_c, (size_t)nc, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-    ws->n_counters = (int)have_c;
+    if ((e = grow(ws->counters, ws->n_counters, (size_t)nc, sizeof(int), s)) != cudaSuccess) return grow_status(e);
     if (launch_gemv_batch(a, count, *ws, gt, s, &launches) != cudaSuccess) return FBQ_ERR_CUDA;
     g_launches += launches;
     return FBQ_OK;
@@ -359,16 +353,12 @@ int run_gated_even(const LinearArgs &a, Workspace *ws, cudaStream_t s)
     ThinArgs t{};
     t.x = a.x; t.A = a.A;
     t.M = a.M; t.N = a.N; t.K = a.K; t.rank = a.rank; t.bf16 = a.bf16;
-    char *scratch = static_cast<char *>(ws->grad);
-    t.t = scratch;                                               // (any address: where it will be is not known yet)
-    if (!t.t) t.t = ws;
+    t.t = ws;                                                    // (any address: where it will be is not known yet)
     const size_t thin = thin_bytes(a.M, a.rank), thin_part = a.rank > 0 ? padded256(thin_part_bytes(t)) : 0;
-    cudaError_t e = grow(scratch, ws->grad_bytes, thin + thin_part + even_part_bytes(a.M, a.N, a.K), 1, s);
-    ws->grad = scratch;
+    cudaError_t e = grow(ws->grad, ws->grad_bytes, thin + thin_part + even_part_bytes(a.M, a.N, a.K), 1, s);
     if (e != cudaSuccess) return grow_status(e);
-    size_t have_c = (size_t)ws->n_counters;
-    if ((e = grow(ws->counters, have_c, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-    ws->n_counters = (int)have_c;
+    char *scratch = static_cast<char *>(ws->grad);
+    if ((e = grow(ws->counters, ws->n_counters, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
     int launches = 0;
     if (a.rank > 0) {
         t.t = scratch;
@@ -415,10 +405,8 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         size_t pf = 0;
         int nc = 0;
         gemv_workspace_need(a, gt, &pf, &nc);
-        size_t have_c = (size_t)ws->n_counters;
         if ((e = grow(ws->tslots, ws->tslots_floats, pf, sizeof(float), s)) != cudaSuccess) return grow_status(e);
-        if ((e = grow(ws->counters, have_c, (size_t)nc, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-        ws->n_counters = (int)have_c;
+        if ((e = grow(ws->counters, ws->n_counters, (size_t)nc, sizeof(int), s)) != cudaSuccess) return grow_status(e);
         if (g_opt.decode_trace && !ws->trace) {
             if (cudaMalloc(&ws->trace, kTraceBytes) != cudaSuccess) return FBQ_ERR_CUDA;
             cudaMemset(ws->trace, 0, kTraceBytes);
@@ -436,11 +424,9 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         size_t pf = 0;
         int nc = 0;
         decode_workspace_need(a, tune, &pf, &nc);
-        size_t have_c = (size_t)ws->n_counters;
         if ((e = grow(ws->partial, ws->partial_floats, pf, sizeof(float), s)) != cudaSuccess) return grow_status(e);
         if ((e = grow(ws->t, ws->t_floats, (size_t)kDecodeMaxM * kMaxRank, sizeof(float), s)) != cudaSuccess) return grow_status(e);
-        if ((e = grow(ws->counters, have_c, (size_t)nc, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-        ws->n_counters = (int)have_c;
+        if ((e = grow(ws->counters, ws->n_counters, (size_t)nc, sizeof(int), s)) != cudaSuccess) return grow_status(e);
         if (g_opt.decode_trace && !ws->trace) {
             if (cudaMalloc(&ws->trace, kTraceBytes) != cudaSuccess) return FBQ_ERR_CUDA;
         }
@@ -461,7 +447,7 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
     }
     if (a.gate >= 0 && kernel == FBQ_KERNEL_PREFILL && gated_even_takes(a)) return run_gated_even(a, ws.get(), s);
     if (kernel == FBQ_KERNEL_PREFILL) {
-        size_t have_c = (size_t)ws->n_counters, need_t = 0, need_p = 0;
+        size_t need_t = 0, need_p = 0;
         int need_c = 0;
         prefill_workspace_need(a, &need_c, &need_t, &need_p);
         // The dense kernel's matrix of weights is the largest scratch by far and the other kernel computes the same call without
@@ -471,17 +457,14 @@ int run_linear(const LinearArgs &a, cudaStream_t s, int decode_ctas = 0)
         if (dense) {
             size_t need_w = 0, need_tags = 0, tf = 0;
             dense_workspace_need(a, &need_w, &need_tags, &tf);
-            char *w16 = static_cast<char *>(ws->w16);
-            e = grow(w16, ws->w16_bytes, need_w, 1, s);
-            ws->w16 = w16;
+            e = grow(ws->w16, ws->w16_bytes, need_w, 1, s);
             if (e == cudaSuccess) e = grow(ws->tags, ws->n_tags, need_tags, sizeof(uint32_t), s);
             dense = e == cudaSuccess;
             if (!dense && e != cudaErrorMemoryAllocation && e != cudaErrorStreamCaptureUnsupported) return FBQ_ERR_CUDA;
             if (!dense && a.kept) return grow_status(e);
             if (dense) need_t = std::max(need_t, tf);
         }
-        if ((e = grow(ws->counters, have_c, (size_t)need_c, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-        ws->n_counters = (int)have_c;
+        if ((e = grow(ws->counters, ws->n_counters, (size_t)need_c, sizeof(int), s)) != cudaSuccess) return grow_status(e);
         if (need_t > 0 && (e = grow(ws->t_gen, ws->t_gen_floats, need_t, sizeof(float), s)) != cudaSuccess) return grow_status(e);
         if (need_p > 0 && (e = grow(ws->partial, ws->partial_floats, need_p, sizeof(float), s)) != cudaSuccess) return grow_status(e);
         e = launch_prefill(a, dense, *ws, s, &launches);
@@ -536,21 +519,16 @@ int run_backward(Backward &b, cudaStream_t s)
     const size_t x_at = place(unpack ? M * g.K * 2 : 0), dy_at = place(b.kept ? M * g.N * 2 : 0), s_at = place(thin), t_at = place(factors ? thin : 0),
                  part_at = place(factors ? factor_grad_scratch_bytes(g.M, g.N, g.K, g.rank) : 0), thin_at = place(thin_first ? thin_part_bytes(t) : 0), even_at = place(even && g.dx ? even_part_bytes(g.M, g.K, g.N) : 0);
     cudaError_t e;
-    size_t have_c = (size_t)ws->n_counters, need_w = 0, need_tags = 0;
-    char *scratch = static_cast<char *>(ws->grad), *w16 = static_cast<char *>(ws->w16);
-    e = grow(scratch, ws->grad_bytes, std::max<size_t>(need, 256), 1, s);
-    ws->grad = scratch;
-    if (e != cudaSuccess) return grow_status(e);
+    size_t need_w = 0, need_tags = 0;
+    if ((e = grow(ws->grad, ws->grad_bytes, std::max<size_t>(need, 256), 1, s)) != cudaSuccess) return grow_status(e);
+    char *scratch = static_cast<char *>(ws->grad);
     grad_workspace_need(g, &need_w, &need_tags);
     if (even || !g.dx) {
         need_w = need_tags = 0;
     }
-    e = grow(w16, ws->w16_bytes, need_w, 1, s);
-    ws->w16 = w16;
-    if (e != cudaSuccess) return grow_status(e);
+    if ((e = grow(ws->w16, ws->w16_bytes, need_w, 1, s)) != cudaSuccess) return grow_status(e);
     if ((e = grow(ws->tags, ws->n_tags, need_tags, sizeof(uint32_t), s)) != cudaSuccess) return grow_status(e);
-    if ((e = grow(ws->counters, have_c, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
-    ws->n_counters = (int)have_c;
+    if ((e = grow(ws->counters, ws->n_counters, 16, sizeof(int), s)) != cudaSuccess) return grow_status(e);
     int launches = 0;
     if (unpack) {
         if (launch_act8_unpack(b.x8, b.x8_scales, scratch + x_at, g.M, g.K, g.bf16, s) != cudaSuccess) return FBQ_ERR_CUDA;
@@ -593,14 +571,11 @@ int with_scratch(N need, cudaStream_t s, F f, void *spare = nullptr, size_t spar
     const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     int launches = 0, rc = FBQ_ERR_CUDA;
-    size_t have_c = (size_t)ws->n_counters;
-    if (grow(ws->counters, have_c, 16, sizeof(int), s) == cudaSuccess) ws->n_counters = (int)have_c;
+    (void)grow(ws->counters, ws->n_counters, 16, sizeof(int), s);          // (without them there is no status word)
     int *status = ws->counters ? ws->counters + kCtrStatus : nullptr;
     const size_t most = g_opt.scratch_mb > 0 ? (size_t)g_opt.scratch_mb << 20 : kScratchMost;
     for (size_t budget : {most, most / 8, (size_t)0}) {
-        char *rec = static_cast<char *>(ws->rec);
-        const cudaError_t e = grow(rec, ws->rec_bytes, need(budget), 1, s);
-        ws->rec = rec;
+        const cudaError_t e = grow(ws->rec, ws->rec_bytes, need(budget), 1, s);
         if (e == cudaSuccess) {
             rc = f(budget, ws->rec, status, &launches);
             g_launches += launches;
@@ -1013,10 +988,8 @@ static int place_batch_x(LinearArgs *a, int count, int M, Workspace *ws, cudaStr
         }
         which[i] = k;
     }
+    if (const cudaError_t e = grow(ws->stage_x, ws->stage_x_bytes, b.total, 1, s); e != cudaSuccess) return grow_status(e);
     char *sx = static_cast<char *>(ws->stage_x);
-    const cudaError_t e = grow(sx, ws->stage_x_bytes, b.total, 1, s);
-    ws->stage_x = sx;
-    if (e != cudaSuccess) return grow_status(e);
     for (int i = 0; i < count; ++i) a[i].x = sx + off[which[i]];
     for (int k = 0; k < b.n; ++k) b.dst[k] = sx + off[k];
     return FBQ_OK;
@@ -1034,8 +1007,6 @@ static int host_batch(const LinearArgs *in, const fbq_problem *problems, int cou
     std::copy(in, in + count, a);
     BatchX x;
     if (const int rc = place_batch_x(a, count, M, ws.get(), s, x); rc != FBQ_OK) return rc;
-    char *sy = static_cast<char *>(ws->stage_y);
-    cudaError_t e;
     bool staged[FBQ_BATCH_MAX];
     for (int i = 0; i < count; ++i) {
         void *alias = direct_y_alias(a[i].y, (size_t)M * a[i].N * 2);
@@ -1044,10 +1015,9 @@ static int host_batch(const LinearArgs *in, const fbq_problem *problems, int cou
         if (staged[i]) y_bytes += padded((size_t)M * a[i].N * 2);
     }
     if (y_bytes > 0) {
-        e = grow(sy, ws->stage_y_bytes, y_bytes, 1, s);
-        ws->stage_y = sy;
-        if (e != cudaSuccess) return grow_status(e);
+        if (const cudaError_t e = grow(ws->stage_y, ws->stage_y_bytes, y_bytes, 1, s); e != cudaSuccess) return grow_status(e);
     }
+    char *sy = static_cast<char *>(ws->stage_y);
     for (int i = 0; i < count; ++i)
         if (staged[i]) a[i].y = sy + reinterpret_cast<size_t>(a[i].y);
     {                                                                      // before anything is queued
@@ -1100,10 +1070,8 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
             la.y = alias;                             // the kernel writes the caller's buffer itself
             return FBQ_OK;
         }
-        char *sy = static_cast<char *>(ws->stage_y);
-        if (grow(sy, ws->stage_y_bytes, yb, 1, st) != cudaSuccess) return FBQ_ERR_CUDA;
-        ws->stage_y = sy;
-        la.y = sy;
+        if (grow(ws->stage_y, ws->stage_y_bytes, yb, 1, st) != cudaSuccess) return FBQ_ERR_CUDA;
+        la.y = ws->stage_y;
         return FBQ_OK;
     };
     auto stage_in = [&](LinearArgs &la, cudaStream_t st) -> int {
@@ -1188,11 +1156,9 @@ static int linear_batch_common(const fbq_problem *problems, int count, int M, in
         size_t pf = 0, tf = 0;
         int nc = 0;
         if (decode_batch_need(a, count, ctas, g_opt.decode, &pf, &tf, &nc)) {
-            size_t have_c = (size_t)ws->n_counters;
             if (grow(ws->partial, ws->partial_floats, pf, sizeof(float), main) != cudaSuccess) return FBQ_ERR_CUDA;
             if (grow(ws->t, ws->t_floats, tf, sizeof(float), main) != cudaSuccess) return FBQ_ERR_CUDA;
-            if (grow(ws->counters, have_c, (size_t)nc, sizeof(int), main) != cudaSuccess) return FBQ_ERR_CUDA;
-            ws->n_counters = (int)have_c;
+            if (grow(ws->counters, ws->n_counters, (size_t)nc, sizeof(int), main) != cudaSuccess) return FBQ_ERR_CUDA;
             int launches = 0;
             const cudaError_t e = launch_decode_batch(a, count, ctas, *ws, g_opt.decode, main, &launches);
             if (e != cudaSuccess) return FBQ_ERR_CUDA;
@@ -1248,16 +1214,15 @@ int fbq_linear_hostio(const void *x_host, const uint32_t *qweight, const void *s
     const HeldWorkspace ws = workspace_for(s);
     if (!ws) return FBQ_ERR_CUDA;
     const size_t xb = (size_t)M * K * 2, yb = (size_t)M * N * 2;
-    char *sx = static_cast<char *>(ws->stage_x), *sy = static_cast<char *>(ws->stage_y);
-    if (grow(sx, ws->stage_x_bytes, xb, 1, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    ws->stage_x = sx;
+    if (grow(ws->stage_x, ws->stage_x_bytes, xb, 1, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    void *sx = ws->stage_x;
     const void *from[1] = {x_host};
     void *to[1] = {sx};
     if (copy_in(1, from, to, &xb, s) != cudaSuccess) return FBQ_ERR_CUDA;
     if (void *alias = direct_y_alias(y_host, yb))       // the kernel writes the caller's buffer itself
         return linear_common(sx, qweight, scales, zeros, A, B, alias, M, N, K, group, bits, rank, act_is_bf16 != 0, stream);
-    if (grow(sy, ws->stage_y_bytes, yb, 1, s) != cudaSuccess) return FBQ_ERR_CUDA;
-    ws->stage_y = sy;
+    if (grow(ws->stage_y, ws->stage_y_bytes, yb, 1, s) != cudaSuccess) return FBQ_ERR_CUDA;
+    void *sy = ws->stage_y;
     const int rc = linear_common(sx, qweight, scales, zeros, A, B, sy, M, N, K, group, bits, rank, act_is_bf16 != 0, stream);
     if (rc != FBQ_OK) return rc;
     if (cudaMemcpyAsync(y_host, sy, yb, cudaMemcpyDeviceToHost, s) != cudaSuccess) return FBQ_ERR_CUDA;
@@ -1340,7 +1305,7 @@ int fbq_poll_status(void *stream)
     if (cudaMemcpy(&st, ws->counters + kCtrStatus, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return FBQ_ERR_CUDA;
     if (st != 0) {
         // a kernel gave up half way: its bookkeeping is unfinished, start from a clean slate
-        cudaMemset(ws->counters, 0, sizeof(int) * (size_t)ws->n_counters);
+        cudaMemset(ws->counters, 0, sizeof(int) * ws->n_counters);
         if (ws->t) cudaMemset(ws->t, 0, sizeof(float) * ws->t_floats);
         if (ws->tslots) cudaMemset(ws->tslots, 0, sizeof(float) * ws->tslots_floats);
         if (ws->tags) cudaMemset(ws->tags, 0, sizeof(uint32_t) * ws->n_tags);

@@ -127,7 +127,7 @@ extern "C" int fbq_linear_noalloc(const void *x, const uint32_t *qweight, const 
 
     Workspace ws{};
     ws.counters = reinterpret_cast<int *>(base);
-    ws.n_counters = (int)kMaxCounters;
+    ws.n_counters = kMaxCounters;
     ws.t = reinterpret_cast<float *>(base + kCtrBytes);
     ws.t_floats = kTBytes / sizeof(float);
     ws.partial = reinterpret_cast<float *>(base + kCtrBytes + kTBytes);
