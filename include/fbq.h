@@ -446,7 +446,8 @@ int fbq_poll_status(void *stream);
  * timer at kernel entry.  Zero where a mark was not reached.  bytes <= 512*18*16*8.  Synchronises the stream. */
 int fbq_debug_read_trace(void *stream, void *host_buf, size_t bytes);
 
-/* Frees every per-stream scratch buffer (synchronises the device first). */
+/* Frees every per-stream scratch buffer (synchronises the device first).  Graphs captured before have their addresses: they must not be
+ * replayed after. */
 int fbq_release_workspaces(void);
 
 const char *fbq_status_string(int status);
